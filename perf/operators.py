@@ -323,7 +323,7 @@ def _own_update(s):
     ws = _kept(s, "ws", lambda: _space(spo.spo_orthogonalize_workspace_bytes(s["L"], s["m"], s["n"], products)))
     if s["path"] == "orthogonalize":
         return dict(out=spo.spo_orthogonalize(s["grad"], steps=STEPS, coeffs=COEFFS, eps=EPS, products=products, workspace=ws))
-    spo.spo_muon_update(s["W"], s["momentum"], s["grad"], lr=LR, momentum=MOMENTUM, weight_decay=WEIGHT_DECAY, scale=_muon_scale(s),
+    spo.spo_muon_update(s["W"], s["momentum"], s["grad"], lr=LR, mu=MOMENTUM, weight_decay=WEIGHT_DECAY, scale=_muon_scale(s),
                         steps=STEPS, coeffs=COEFFS, eps=EPS, products=products, workspace=ws)
     return dict(W=s["W"], momentum=s["momentum"])
 
