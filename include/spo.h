@@ -345,6 +345,66 @@ int spo_pg_loss_fwd_bwd(const spo_pg_desc *d, float grad_loss, float *loss, floa
                         void *ws, size_t ws_bytes, spo_stream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Log-probs of given tokens, their entropy, and the alternatives that were most likely,
+ * with the gradient of all three: entropy bonuses and their monitoring, terms towards a
+ * reference or a teacher, scoring of responses, the log-probs that a server reports.
+ *
+ * For token t with logits z = z_t (row t of `logits`, or W^T h_t), p = softmax(z):
+ *   lse      = log sum_v exp z[v];  logp = z[target] - lse
+ *   entropy  = - sum_v p_v log p_v       (an entry of -inf adds nothing)
+ *   top_id   = the top_k largest logits' ids, the largest first, ties to the lowest id;
+ *   top_logp = z[top_id] - lse
+ * and, with a = d_logp[t], e = d_entropy[t], b_k = d_top_logp[t][k] the derivatives of a total
+ * with respect to them,
+ *   d_logits[v] = a [v == target] + sum_k b_k [v == top_id_k]
+ *                 - p_v (a + sum_k b_k + e (log p_v + entropy)).
+ * Logits-in form (logits != NULL; hidden and W ignored): rows of V values, logits_stride apart.
+ * Head form (logits == NULL): the [T x V] logits are never written to memory; top_k must be 0.
+ * Tokens that the mask leaves out (mask[t] == 0) are not read: logp, lse, entropy, top_logp are 0,
+ * top_id is -1, their gradients are zeros.  (The head form multiplies them along with the others in
+ * the forward, not in the backward.)
+ * A row whose logits are all -inf has lse = -inf, and logp, entropy, top_logp NaN; its top_id are
+ * the lowest ids.  A row with a NaN has NaN in all of them, and some ids.
+ * ------------------------------------------------------------------------- */
+#define SPO_MAX_TOP_K 64
+typedef struct {
+    size_t struct_size;      /* sizeof(spo_logprob_desc), checked                         */
+    int dtype;               /* SPO_BF16 or SPO_FP32: element type of hidden, W, logits   */
+    int w_layout;            /* SPO_W_VH or SPO_W_HV                                      */
+    int64_t T, H, V;         /* tokens, hidden size, vocabulary size                      */
+    const void *hidden;      /* [T, H] row-major                                          */
+    const void *W;           /* H*V elements in w_layout                                  */
+    const void *logits;      /* [T] rows of V elements, or NULL                           */
+    int64_t logits_stride;   /* elements from one row of logits to the next; 0: V         */
+    const int32_t *target;   /* [T] token ids in [0, V), or NULL: no logp.  An id outside
+                                that range gives a NaN logp and no one-hot term           */
+    const uint8_t *mask;     /* [T] 0/1, or NULL for all ones                             */
+    int32_t top_k;           /* alternatives per token, 0..SPO_MAX_TOP_K, at most V       */
+} spo_logprob_desc;
+
+/* Forward.  lse [T] fp32; logp [T] fp32 where target is given, otherwise ignored; entropy [T] fp32
+ * or NULL; top_id [T][top_k] int32 and top_logp [T][top_k] fp32 where top_k > 0.
+ * All sums in fp32 in a fixed order.  The workspace size never shrinks with T or V.
+ * Head form: H a multiple of 64, H <= 65536, hidden and W 16-byte aligned. */
+size_t spo_logprob_fwd_workspace_bytes(const spo_logprob_desc *d);
+int spo_logprob_fwd(const spo_logprob_desc *d, float *logp, float *lse, float *entropy, int32_t *top_id,
+                    float *top_logp, void *ws, size_t ws_bytes, spo_stream_t stream);
+
+/* Backward.  lse, entropy, top_id: from the forward of the same desc; entropy is needed with
+ * d_entropy, top_id with d_top_logp.  d_logp, d_entropy [T] and d_top_logp [T][top_k] fp32: each may
+ * be NULL for zeros; d_logp needs a target.
+ * Logits-in form: d_logits [T, V] in desc dtype, rows V apart; ws is not needed.
+ * Head form: d_hidden, d_W, accumulate_dW, chunk_tokens and the workspace are those of
+ * spo_pg_loss_bwd; tokens whose factors are both zero are left out of all contractions.  Logit
+ * gradients are rounded to bf16 between the contractions, so desc dtype has to be SPO_BF16
+ * (SPO_FP32 -> SPO_EUNSUPPORTED: form the logits and use the logits-in form). */
+size_t spo_logprob_bwd_workspace_bytes(const spo_logprob_desc *d, int64_t chunk_tokens);
+int spo_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *entropy, const float *d_logp,
+                    const float *d_entropy, const int32_t *top_id, const float *d_top_logp, void *d_hidden,
+                    int d_hidden_dtype, void *d_W, int d_W_dtype, int accumulate_dW, void *d_logits,
+                    int64_t chunk_tokens, void *ws, size_t ws_bytes, spo_stream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Per-kernel timing (measurement aid, not part of the method; with the static
  * buffer of spo_sample_prompts_static the only state the library keeps).  While enabled, the loss entry points bracket each launch
  * of their heavy kernels with a pair of HIP events on the launch stream.

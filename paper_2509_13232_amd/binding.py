@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libspo_hip.so")
 SPO_FP32, SPO_BF16 = 0, 1
 SPO_W_VH, SPO_W_HV = 0, 1
 SPO_SAMPLE_STATIC_MAX_N = 1 << 20
+SPO_MAX_TOP_K = 64
 
 EXPORTS = (
     "spo_status_string", "spo_sample_prompts_workspace_bytes", "spo_sample_prompts",
@@ -27,6 +28,8 @@ EXPORTS = (
     "spo_pg_loss_fwd_workspace_bytes", "spo_pg_loss_fwd",
     "spo_pg_loss_bwd_workspace_bytes", "spo_pg_loss_bwd",
     "spo_pg_loss_fwd_bwd_workspace_bytes", "spo_pg_loss_fwd_bwd",
+    "spo_logprob_fwd_workspace_bytes", "spo_logprob_fwd",
+    "spo_logprob_bwd_workspace_bytes", "spo_logprob_bwd",
     "spo_kernel_timing_enable", "spo_kernel_timing_read",
 )
 TIMING_CLASSES = ("fwd_sweep", "bwd_recompute", "bwd_dhidden", "bwd_dw", "logits_fwd", "logits_bwd", "logits_to_dz")
@@ -46,6 +49,15 @@ class PgDesc(C.Structure):
         ("target", C.c_void_p), ("old_logp", C.c_void_p), ("mask", C.c_void_p),
         ("adv_norm", C.c_void_p), ("cu_seqlens", C.c_void_p),
         ("eps_low", C.c_float), ("eps_high", C.c_float),
+    ]
+
+
+class LogprobDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_size_t), ("dtype", C.c_int), ("w_layout", C.c_int),
+        ("T", C.c_int64), ("H", C.c_int64), ("V", C.c_int64),
+        ("hidden", C.c_void_p), ("W", C.c_void_p), ("logits", C.c_void_p), ("logits_stride", C.c_int64),
+        ("target", C.c_void_p), ("mask", C.c_void_p), ("top_k", C.c_int32),
     ]
 
 
@@ -99,6 +111,15 @@ def lib():
         L.spo_pg_loss_fwd_bwd.restype = C.c_int
         L.spo_pg_loss_fwd_bwd.argtypes = [C.POINTER(PgDesc), f32, vp, vp, vp, vp, vp, C.c_int, vp, C.c_int, C.c_int,
                                           i64, vp, sz, vp]
+        L.spo_logprob_fwd_workspace_bytes.restype = sz
+        L.spo_logprob_fwd_workspace_bytes.argtypes = [C.POINTER(LogprobDesc)]
+        L.spo_logprob_fwd.restype = C.c_int
+        L.spo_logprob_fwd.argtypes = [C.POINTER(LogprobDesc), vp, vp, vp, vp, vp, vp, sz, vp]
+        L.spo_logprob_bwd_workspace_bytes.restype = sz
+        L.spo_logprob_bwd_workspace_bytes.argtypes = [C.POINTER(LogprobDesc), i64]
+        L.spo_logprob_bwd.restype = C.c_int
+        L.spo_logprob_bwd.argtypes = [C.POINTER(LogprobDesc), vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, C.c_int, C.c_int, vp, i64,
+                                      vp, sz, vp]
         L.spo_kernel_timing_enable.restype = C.c_int
         L.spo_kernel_timing_enable.argtypes = [C.c_int]
         L.spo_kernel_timing_read.restype = C.c_int
@@ -458,3 +479,95 @@ def spo_pg_loss_fwd_bwd(desc, grad_loss=1.0, d_hidden_dtype=None, d_W_dtype=torc
                                      _dt(d_W.dtype) if d_W is not None else 0, int(bool(accumulate_dW)),
                                      int(chunk_tokens), _ptr(ws), ws.numel(), _stream()), "spo_pg_loss_fwd_bwd")
     return loss, logp, lse, stats, dx, d_W
+
+
+# ------------------------------------- log-probs, entropy, alternatives
+def make_logprob_desc(hidden, W, target, mask=None, w_layout=SPO_W_VH, logits=None, top_k=0):
+    """Builds the C descriptor; returns (desc, keepalive tuple).  logits: [T, V], rows of consecutive elements, any distance
+    of at least V apart.  target: int32[T] or None (no log-probs, and no gradient of them)."""
+    d = LogprobDesc()
+    d.struct_size = C.sizeof(LogprobDesc)
+    if logits is not None:
+        T, V = logits.shape
+        H = 0
+        apart = logits.stride(0) if T > 1 else V
+        if not logits.is_cuda or (V > 1 and logits.stride(1) != 1) or apart < V or logits.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("logits: expected a CUDA tensor [T, V] of torch.float32 or torch.bfloat16 with consecutive rows")
+        if T == 0:  # no memory, but a pointer says that the logits are given
+            logits = torch.empty((1, V), dtype=logits.dtype, device=logits.device)
+        d.dtype, d.logits_stride = _dt(logits.dtype), apart
+        dev = logits.device
+    else:
+        _want(hidden, hidden.dtype, "hidden")
+        _want(W, hidden.dtype, "W")
+        T, H = hidden.shape
+        V, W_H = W.shape if w_layout == SPO_W_VH else W.shape[::-1]
+        if W_H != H:
+            raise ValueError(f"W: expected {'[V, H]' if w_layout == SPO_W_VH else '[H, V]'} with H = {H}, got {tuple(W.shape)}")
+        d.dtype = _dt(hidden.dtype)
+        dev = hidden.device
+    _want(target, torch.int32, "target", T)
+    _want(mask, torch.uint8, "mask", T)
+    d.w_layout = w_layout
+    d.T, d.H, d.V, d.top_k = T, H, V, int(top_k)
+    d.hidden, d.W, d.logits, d.target, d.mask = (_ptr(t) for t in (hidden, W, logits, target, mask))
+    return d, (hidden, W, logits, target, mask, dev)
+
+
+def spo_logprob_fwd_workspace_bytes(desc) -> int:
+    return int(lib().spo_logprob_fwd_workspace_bytes(C.byref(desc[0])))
+
+
+def spo_logprob_fwd(desc, workspace=None, want_entropy=True):
+    """Returns (logp[T] or None, lse[T], entropy[T] or None, top_id[T, top_k] or None, top_logp[T, top_k] or None)."""
+    d, keep = desc
+    dev = keep[5]
+    lse = _per_token(d.T, dev)
+    logp = _per_token(d.T, dev) if keep[3] is not None else None
+    entropy = _per_token(d.T, dev) if want_entropy else None
+    ids = top = None
+    if d.top_k > 0:
+        ids = torch.empty((d.T, d.top_k), dtype=torch.int32, device=dev)
+        top = torch.empty((d.T, d.top_k), dtype=torch.float32, device=dev)
+    ws = _workspace(lib().spo_logprob_fwd_workspace_bytes(C.byref(d)), dev, workspace)
+    _check(lib().spo_logprob_fwd(C.byref(d), _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(ids), _ptr(top), _ptr(ws), ws.numel(),
+                                 _stream()), "spo_logprob_fwd")
+    return logp, lse, entropy, ids, top
+
+
+def spo_logprob_bwd_workspace_bytes(desc, chunk_tokens=0) -> int:
+    return int(lib().spo_logprob_bwd_workspace_bytes(C.byref(desc[0]), int(chunk_tokens)))
+
+
+def spo_logprob_bwd(desc, lse, entropy=None, d_logp=None, d_entropy=None, top_id=None, d_top_logp=None, d_hidden_dtype=None,
+                    d_W_dtype=torch.float32, d_W=None, accumulate_dW=False, want_d_hidden=True, want_d_W=True, chunk_tokens=0,
+                    workspace=None):
+    """Gradients of sum(d_logp * logp) + sum(d_entropy * entropy) + sum(d_top_logp * top_logp); each may be None.
+    Head form: returns (d_hidden[T, H] or None, d_W in W's layout or None).  Logits-in form: returns d_logits[T, V]."""
+    d, keep = desc
+    dev = keep[5]
+    for t, name, n in ((lse, "lse", d.T), (entropy, "entropy", d.T), (d_logp, "d_logp", d.T), (d_entropy, "d_entropy", d.T),
+                       (d_top_logp, "d_top_logp", d.T * d.top_k)):
+        _want(t, torch.float32, name, n)
+    _want(top_id, torch.int32, "top_id", d.T * d.top_k)
+    L = lib()
+    if d.logits:
+        dl = torch.empty((d.T, d.V), dtype=keep[2].dtype, device=dev)
+        _check(L.spo_logprob_bwd(C.byref(d), _ptr(lse), _ptr(entropy), _ptr(d_logp), _ptr(d_entropy), _ptr(top_id), _ptr(d_top_logp),
+                                 None, 0, None, 0, 0, _ptr(dl), int(chunk_tokens), None, 0, _stream()), "spo_logprob_bwd")
+        return dl
+    hidden, W = keep[0], keep[1]
+    ws = _workspace(L.spo_logprob_bwd_workspace_bytes(C.byref(d), int(chunk_tokens)), dev, workspace)
+    dx = torch.empty((d.T, d.H), dtype=d_hidden_dtype or hidden.dtype, device=dev) if want_d_hidden else None
+    if not want_d_W:
+        d_W = None
+    elif d_W is not None:
+        _want_d_W(d_W, d)
+    elif accumulate_dW:
+        raise ValueError("accumulate_dW needs an existing d_W")
+    else:
+        d_W = torch.empty(W.shape, dtype=d_W_dtype, device=dev)
+    _check(L.spo_logprob_bwd(C.byref(d), _ptr(lse), _ptr(entropy), _ptr(d_logp), _ptr(d_entropy), None, None, _ptr(dx),
+                             _dt(dx.dtype) if dx is not None else 0, _ptr(d_W), _dt(d_W.dtype) if d_W is not None else 0,
+                             int(bool(accumulate_dW)), None, int(chunk_tokens), _ptr(ws), ws.numel(), _stream()), "spo_logprob_bwd")
+    return dx, d_W

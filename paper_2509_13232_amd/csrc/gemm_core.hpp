@@ -33,7 +33,28 @@
 namespace spo {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+// The kernels use more dynamic LDS than the default limit allows.  The attribute belongs
+// to the current device's copy of the kernel, so it is set on every call (a host-side
+// table lookup) rather than remembered in a process-wide flag.
+template <typename K>
+static int allow_lds(K kernel, int bytes) {
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess
+               ? SPO_OK : SPO_EHIP;
+}
+
+// Exchange between neighbouring groups of 16 lanes: v_permlane16_swap(a, b) swaps the odd groups
+// of a with the even groups of b.  With a, b the values a lane holds for two consecutive MFMA
+// blocks q, q+1, lane group g ends up with (in a, b) the values of block q + (g & 1) from lane
+// groups (g & 2) and (g & 2) + 1.
+__device__ __forceinline__ void swap_lane_groups(uint32_t &a, uint32_t &b) {
+    typedef unsigned v2u __attribute__((ext_vector_type(2)));
+    const v2u t = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = t.x;
+    b = t.y;
+}
 
 constexpr int kBK = 64;      // contraction elements per stage
 constexpr int kStages = 2;   // LDS stages
@@ -52,7 +73,9 @@ __device__ __forceinline__ int swz(int row) {
 // MI is the edge of the MFMA block: 16 for v_mfma_f32_16x16x32_bf16, the instruction the
 // main loop is written for.  (The same tile on v_mfma_f32_32x32x16_bf16, with two
 // phase-shifted groups of wavefronts, was 4-6 % slower on the same chip.)
-template <int BM_, int BN_, int WGM_, int WGN_, int MI_ = 16>
+// Elt: __bf16, or _Float16 (v_mfma_f32_16x16x32_f16, of the same shape and rate): 16 bits each, so all but the
+// instruction is the same.
+template <int BM_, int BN_, int WGM_, int WGN_, typename Elt = __bf16, int MI_ = 16>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, MI = MI_;
     static_assert(MI == 16, "the main loop issues 16x16x32 MFMAs");
@@ -316,6 +339,10 @@ struct Tile {
 
     template <bool Across>
     __device__ static __forceinline__ AccBlock mfma(const bf16x8_t &a, const bf16x8_t &b, const AccBlock &c) {
+        if constexpr (std::is_same_v<Elt, _Float16>) {
+            const f16x8_t x = __builtin_bit_cast(f16x8_t, a), y = __builtin_bit_cast(f16x8_t, b);
+            return Across ? __builtin_amdgcn_mfma_f32_16x16x32_f16(y, x, c, 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+        }
         return Across ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
 

@@ -1,0 +1,631 @@
+// Log-probs of given tokens, their entropy and the top alternatives from existing logits, the gradient of all of them, and the
+// C entry points of both the logits-in and the head form (whose kernels are the sweeps of pg_fused.hip).
+//
+//   forward   one pass over the rows keeps (max, sum of exp, sum of x exp) per thread and joins them; for the alternatives
+//             every thread also leaves the largest logit it met, and a second kernel finds the K largest of a row from
+//             those: the K-th largest of 256 such maxima is a lower bound on the K-th largest logit, and few logits pass it;
+//   backward  dz_i = a [i = y] + sum_k b_k [i = id_k] - p_i (a + sum_k b_k + e (log p_i + H)), one read and one write.
+#include <algorithm>
+
+#include "logprob.hpp"
+#include "row_stream.hpp"
+#include "timing.hpp"
+
+namespace spo {
+
+constexpr int kScoreGroup = 4, kScoreRounds = 2, kScoreGradGroup = 2;
+constexpr int kScoreNarrow = 5, kScoreGradNarrow = 4;  // see row_grid
+constexpr float kLowestFloat = -3.402823466e38f;       // starts a maximum: finite, and no logit but -inf is below it
+
+// What every row carries besides its logits.
+struct ScoreRows {
+    int64_t T, V, stride;   // stride: elements from row to row
+    const int32_t *target;  // NULL: no log-prob
+    const uint8_t *mask;    // NULL: every row counts
+};
+struct ScoreOut {
+    float *logp, *lse, *entropy;  // logp, entropy: NULL where not asked for
+    int32_t *top_id;
+    float *top_logp;
+    int K;
+};
+
+template <typename T>
+__device__ __forceinline__ float target_logit(const T *row, const ScoreRows &r, int64_t t) {
+    const int64_t y = r.target[t];  // an id outside [0, V) gives NaN instead of a read out of bounds
+    return y >= 0 && y < r.V ? Vec<T>::get(row + y) : __builtin_nanf("");
+}
+
+__device__ __forceinline__ void store_scores(const ScoreOut &o, int64_t t, float zt, float m, float s, float u) {
+    const float l = logf(s);
+    o.lse[t] = m + l;
+    if (o.logp) o.logp[t] = (zt - m) - l;  // (beside a logit of 1e8 the sum m + l has lost l)
+    if (o.entropy) o.entropy[t] = score_entropy(s, u);
+}
+// a row that the mask leaves out: nothing of it is read
+__device__ __forceinline__ void store_left_out(const ScoreOut &o, int64_t t) {
+    o.lse[t] = 0.0f;
+    if (o.logp) o.logp[t] = 0.0f;
+    if (o.entropy) o.entropy[t] = 0.0f;
+}
+
+// (max, sum of 2^x, sum of x 2^x) of one segment of a row by TR threads, a workgroup or one wavefront of it, and with Top each
+// thread's own maximum, group_max[row][segment * TR + thread].  Rows of one segment (whole) are finished here unless
+// alternatives are asked for.
+template <typename T, int TR, int Rounds, bool Stream, bool Top>
+__global__ void __launch_bounds__(kRowThreads)
+score_rows_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, float *__restrict__ part, float *__restrict__ group_max,
+                  ScoreOut out) {
+    constexpr int N = Vec<T>::N, U = kScoreGroup;
+    const int64_t unit = group_unit<TR>();
+    const int tid = threadIdx.x % TR;
+    if (unit >= grid.units()) return;  // TR < kRowThreads only: no barrier below in that case
+    const uint32_t nseg = static_cast<uint32_t>(grid.nseg), seg = static_cast<uint32_t>(unit) % nseg;
+    const int64_t t = static_cast<uint32_t>(unit) / nseg, e0 = seg * grid.seg_len;
+    const bool whole = !Top && nseg == 1;
+    if (rows.mask && !rows.mask[t]) {
+        if (whole && tid == 0) store_left_out(out, t);
+        return;
+    }
+    const T *row = logits + t * rows.stride, *p = row + e0;
+    const Span sp(p, static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len));
+    float zt = 0.0f;
+    if (whole && tid == 0 && rows.target) zt = target_logit(row, rows, t);
+    // the few elements outside the whole vectors, one per thread
+    float m = kLowestFloat, s = 0.0f, u2 = 0.0f;
+    if (tid < sp.head + sp.tail) {
+        const float x = Vec<T>::get(p + (tid < sp.head ? tid : tid + sp.nvec * N));
+        m = fmaxf(m, x);
+        const float d = fmaxf((x - m) * kLog2e, kLowest2);
+        s = __builtin_amdgcn_exp2f((x - m) * kLog2e);
+        u2 = s * d;
+    }
+    const T *body = p + sp.head;
+    auto request = [&](uint4 (&v)[U], int i0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * TR < sp.nvec) v[u] = load16<Stream>(body + (i0 + u * TR) * N);
+    };
+    auto take = [&](const uint4 (&v)[U], int i0) {
+        // one new maximum and one rescaling of the running sums for the whole group
+        float x[U][N], mx = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * TR >= sp.nvec) break;
+            Vec<T>::unpack(v[u], x[u]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) mx = fmaxf(mx, x[u][i]);
+        }
+        const float nm2 = -mx * kLog2e;
+        float a[U] = {}, w[U] = {};
+        auto add = [&](auto exponent) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * TR >= sp.nvec) break;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float d = exponent(x[u][i]), e = __builtin_amdgcn_exp2f(d);
+                    a[u] += e;
+                    w[u] = fmaf(e, fmaxf(d, kLowest2), w[u]);
+                }
+            }
+        };
+        if (__any(i0 < sp.nvec && fabsf(mx) > kFarLogit)) add([&](float v) { return (v - mx) * kLog2e; });
+        else add([&](float v) { return fmaf(v, kLog2e, nm2); });
+        const float d = fmaxf((m - mx) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d);
+        u2 = f * fmaf(d, s, u2) + ((w[0] + w[1]) + (w[2] + w[3]));
+        s = s * f + ((a[0] + a[1]) + (a[2] + a[3]));
+        m = mx;
+    };
+    uint4 cur[U];
+    request(cur, tid);
+    if constexpr (Rounds > 1) {
+        uint4 nxt[U];
+        for (int i0 = tid; i0 < sp.nvec; i0 += U * TR) {
+            request(nxt, i0 + U * TR);
+            take(cur, i0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) cur[u] = nxt[u];
+        }
+    } else {
+        take(cur, tid);
+    }
+    if constexpr (Top) group_max[(t * nseg + seg) * TR + tid] = m;
+    // one maximum for the wavefront, then one rescaling and the sums
+    float top = m;
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    const float d = fmaxf((m - top) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d);
+    u2 = wave_sum(f * fmaf(d, s, u2));
+    s = wave_sum(s * f);
+    m = top;
+    if constexpr (TR > kWave) {
+        __shared__ float sm[TR / kWave], ss[TR / kWave], su[TR / kWave];
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) { sm[wave] = m; ss[wave] = s; su[wave] = u2; }
+        __syncthreads();
+        m = sm[0]; s = ss[0]; u2 = su[0];
+        for (int w = 1; w < TR / kWave; ++w) score_join(m, s, u2, sm[w], ss[w], su[w]);
+    }
+    if (tid != 0) return;
+    if (whole) return store_scores(out, t, zt, m, s, u2);
+    float *q = part + (t * nseg + seg) * 3;
+    q[0] = m;
+    q[1] = s;
+    q[2] = u2;
+}
+
+// The segments of row t joined by one wavefront; every lane receives the result.
+__device__ __forceinline__ void join_segments(const float *__restrict__ part, int nseg, int64_t t, float &m, float &s, float &u) {
+    const int lane = threadIdx.x & 63;
+    m = kLowestFloat;
+    s = u = 0.0f;
+    for (int i = lane; i < nseg; i += kWave) {
+        const float *q = part + (t * nseg + i) * 3;
+        score_join(m, s, u, q[0], q[1], q[2]);
+    }
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+        // (the lower lane's pair first, so that both lanes of a pair form the same sum)
+        const float om = __shfl_xor(m, o, kWave), os = __shfl_xor(s, o, kWave), ou = __shfl_xor(u, o, kWave);
+        float a = lane & o ? om : m, b = lane & o ? os : s, c = lane & o ? ou : u;
+        score_join(a, b, c, lane & o ? m : om, lane & o ? s : os, lane & o ? u : ou);
+        m = a; s = b; u = c;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+score_join_kernel(const T *__restrict__ logits, ScoreRows rows, int nseg, const float *__restrict__ part, ScoreOut out) {
+    const int64_t t = flat_block() * 4 + (threadIdx.x >> 6);
+    if (t >= rows.T) return;
+    const int lane = threadIdx.x & 63;
+    if (rows.mask && !rows.mask[t]) {
+        if (lane == 0) store_left_out(out, t);
+        return;
+    }
+    float zt = 0.0f, m, s, u;
+    if (lane == 0 && rows.target) zt = target_logit(logits + t * rows.stride, rows, t);
+    join_segments(part, nseg, t, m, s, u);
+    if (lane == 0) store_scores(out, t, zt, m, s, u);
+}
+
+// ----------------------------------------------------------------------------
+// the K largest logits of a row
+// ----------------------------------------------------------------------------
+// Order: by value, ties to the lowest id; -0 and +0 tie.  As one whole number, the larger the better: the value's bits made
+// monotone, then the id from above.  A NaN has no place in the order (it gets one by its bits).
+__device__ __forceinline__ uint32_t order_key(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t k) {
+    return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+__device__ __forceinline__ uint64_t order_of(float x, uint32_t id) { return static_cast<uint64_t>(order_key(x)) << 32 | static_cast<uint32_t>(~id); }
+
+constexpr int kPickThreads = 256;
+constexpr int kPickGroups = 512;             // groups of a row that are looked into at a time
+constexpr int kPickStep = kPickThreads * 8;  // logits of the step by step way
+constexpr int kPickRoom = kPickStep + SPO_MAX_TOP_K;
+
+// Places of cand[0..n) in their order, `put(place, candidate)` for each of the first K.  n <= kPickRoom; keys are distinct.
+template <typename F>
+__device__ __forceinline__ void rank_candidates(const uint64_t *cand, int n, int K, F put) {
+    for (int i = threadIdx.x; i < n; i += kPickThreads) {
+        const uint64_t mine = cand[i];
+        int place = 0;
+        for (int j = 0; j < n; ++j) place += cand[j] > mine ? 1 : 0;
+        if (place < K) put(place, mine);
+    }
+}
+
+// One workgroup per row: joins its segments and finds its K largest logits.
+//   1. Every thread takes the maximum of its share of group_max; the K-th largest of these 256 maxima of disjoint sets bounds
+//      the K-th largest logit from below.
+//   2. The groups whose maximum reaches the bound, somewhat more than K, are looked into: a thread per vector of a group.
+//   3. What reaches the bound is ranked by counting.
+// Rows with more ties at the bound than there is room, or with fewer groups than K, are walked step by step from the first
+// logit on, with the K best so far kept; later ones have to beat the last of these, so ties cost little after the first step.
+template <typename T, int TR>
+__global__ void __launch_bounds__(kPickThreads)
+score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, const float *__restrict__ part,
+                  const float *__restrict__ group_max, ScoreOut out) {
+    constexpr int N = Vec<T>::N, VPG = kScoreGroup * kScoreRounds;  // vectors of a thread's group, at most
+    __shared__ float best[kPickThreads];
+    __shared__ uint64_t cand[kPickRoom], kept[SPO_MAX_TOP_K];
+    __shared__ int groups[kPickGroups];
+    __shared__ int n_cand, n_group;
+    __shared__ float bound, row_max, row_log;
+    const int64_t t = flat_block();
+    if (t >= rows.T) return;
+    const int tid = threadIdx.x, K = out.K, nseg = grid.nseg;
+    if (rows.mask && !rows.mask[t]) {
+        if (tid == 0) store_left_out(out, t);
+        if (tid < K) {
+            out.top_id[t * K + tid] = -1;
+            out.top_logp[t * K + tid] = 0.0f;
+        }
+        return;
+    }
+    const T *row = logits + t * rows.stride;
+    const float *gm = group_max + t * nseg * TR;
+    const int G = nseg * TR;
+    float mine = -INFINITY;
+    for (int g = tid; g < G; g += kPickThreads) mine = fmaxf(mine, gm[g]);
+    best[tid] = mine;
+    if (tid == 0) n_cand = n_group = 0;
+    if (tid < kWave) {  // meanwhile the first wavefront joins the segments
+        float zt = 0.0f, m, s, u;
+        if (tid == 0 && rows.target) zt = target_logit(row, rows, t);
+        join_segments(part, nseg, t, m, s, u);
+        if (tid == 0) {
+            store_scores(out, t, zt, m, s, u);
+            row_max = m;
+            row_log = logf(s);
+        }
+    }
+    __syncthreads();
+    int place = 0;
+    for (int j = 0; j < kPickThreads; ++j) place += best[j] > mine || (best[j] == mine && j < tid) ? 1 : 0;
+    if (place == K - 1) bound = mine;
+    __syncthreads();
+    // the start of a maximum says nothing about a group (it may be empty, or all -inf)
+    const float tau = bound;
+    bool by_step = !(tau > kLowestFloat);
+    if (!by_step) {
+        for (int g = tid; g < G; g += kPickThreads)
+            if (gm[g] >= tau) {
+                const int at = atomicAdd(&n_group, 1);
+                if (at < kPickGroups) groups[at] = g;
+            }
+        __syncthreads();
+        const int ng = n_group;
+        by_step = ng > kPickGroups;
+        if (!by_step) {
+            auto offer = [&](float x, int64_t id) {
+                if (!(x >= tau)) return;
+                const int at = atomicAdd(&n_cand, 1);
+                if (at < kPickRoom) cand[at] = order_of(x, static_cast<uint32_t>(id));
+            };
+            for (int i = tid; i < ng * (VPG + 1); i += kPickThreads) {
+                const int g = groups[i / (VPG + 1)], v = i % (VPG + 1), th = g % TR;
+                const int64_t e0 = (g / TR) * grid.seg_len;
+                const Span sp(row + e0, static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len));
+                if (v == VPG) {  // the thread's element outside the whole vectors
+                    if (th < sp.head + sp.tail) {
+                        const int64_t e = e0 + (th < sp.head ? th : th + sp.nvec * N);
+                        offer(Vec<T>::get(row + e), e);
+                    }
+                } else if (th + v * TR < sp.nvec) {
+                    const int64_t e = e0 + sp.head + (th + v * TR) * N;
+                    float x[N];
+                    Vec<T>::unpack(load16<false>(row + e), x);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) offer(x[j], e + j);
+                }
+            }
+            __syncthreads();
+            by_step = n_cand > kPickRoom || n_cand < K;  // (fewer than K: NaNs, which reach no bound)
+        }
+    }
+    auto put = [&](int place, uint64_t c) {
+        out.top_id[t * K + place] = static_cast<int32_t>(~static_cast<uint32_t>(c));
+        out.top_logp[t * K + place] = (order_value(static_cast<uint32_t>(c >> 32)) - row_max) - row_log;
+    };
+    if (!by_step) return rank_candidates(cand, n_cand, K, put);
+    uint64_t least = 0;  // of the K kept so far; no logit's number is 0
+    int n_kept = 0;
+    for (int64_t e0 = 0; e0 < rows.V; e0 += kPickStep) {
+        __syncthreads();  // kept and cand are no longer read
+        if (tid == 0) n_cand = n_kept;
+        if (tid < n_kept) cand[tid] = kept[tid];
+        __syncthreads();
+        for (int j = 0; j < kPickStep / kPickThreads; ++j) {
+            const int64_t e = e0 + j * kPickThreads + tid;
+            if (e >= rows.V) break;
+            const uint64_t c = order_of(Vec<T>::get(row + e), static_cast<uint32_t>(e));
+            if (c > least) cand[atomicAdd(&n_cand, 1)] = c;
+        }
+        __syncthreads();
+        const int n = n_cand;
+        if (n == n_kept) continue;
+        rank_candidates(cand, n, K, [&](int place, uint64_t c) { kept[place] = c; });
+        __syncthreads();
+        n_kept = n < K ? n : K;
+        if (n_kept == K) least = kept[K - 1];
+    }
+    __syncthreads();
+    if (tid < n_kept) put(tid, kept[tid]);
+}
+
+// ----------------------------------------------------------------------------
+// backward
+// ----------------------------------------------------------------------------
+struct ScoreGrads {
+    const float *lse, *entropy, *d_logp, *d_entropy;  // d_logp, d_entropy: NULL: zeros
+    const int32_t *top_id;
+    const float *d_top;                               // NULL: zeros
+    int K;
+};
+
+// (max, log of the sum of exp(x - max)) of a whole row by a group of TR threads.
+template <typename T, int TR>
+__device__ __forceinline__ void row_max_log(const T *row, int64_t V, float &m, float &l) {
+    __shared__ float wm[kRowThreads / kWave], wu[kRowThreads / kWave];
+    const int tid = threadIdx.x % TR, wave = threadIdx.x >> 6;
+    m = kLowestFloat;
+    for (int64_t i = tid; i < V; i += TR) m = fmaxf(m, Vec<T>::get(row + i));
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+    if constexpr (TR > kWave) {
+        wm[wave] = m;
+        __syncthreads();
+        for (int w = 0; w < TR / kWave; ++w) m = fmaxf(m, wm[w]);
+    }
+    float s = 0.0f;
+    for (int64_t i = tid; i < V; i += TR) s += __builtin_amdgcn_exp2f((Vec<T>::get(row + i) - m) * kLog2e);
+    s = wave_sum(s);
+    if constexpr (TR > kWave) {
+        wu[wave] = s;
+        __syncthreads();
+        s = 0.0f;
+        for (int w = 0; w < TR / kWave; ++w) s += wu[w];
+    }
+    l = logf(s);
+}
+
+// One segment of a row of d_logits (at most kScoreGradGroup vectors per thread).  Rows that the mask leaves out or whose
+// factors are all zero are written as zeros without being read.  Vectors are aligned on the output side.
+template <typename T, int TR, bool Stream>
+__global__ void __launch_bounds__(kRowThreads)
+score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, ScoreGrads gr, T *__restrict__ d_logits) {
+    constexpr int N = Vec<T>::N, U = kScoreGradGroup;
+    const int64_t unit = group_unit<TR>();
+    const int tid = threadIdx.x % TR, lane = threadIdx.x & 63;
+    if (unit >= grid.units()) return;
+    const uint32_t nseg = static_cast<uint32_t>(grid.nseg);
+    const int64_t t = static_cast<uint32_t>(unit) / nseg, e0 = (static_cast<uint32_t>(unit) % nseg) * grid.seg_len;
+    const T *p = logits + t * rows.stride + e0;
+    T *out = d_logits + t * rows.V + e0;
+    const int len = static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len);
+    const Span sp(out, len);
+    T *body_out = out + sp.head;
+    uint4 *dst = reinterpret_cast<uint4 *>(body_out);
+    const bool left_out = rows.mask && !rows.mask[t];
+    float a = 0.0f, e = 0.0f, b = 0.0f;
+    int id = -1;  // lane k: the k-th alternative's place in the segment, and its factor
+    if (!left_out) {
+        if (gr.d_logp) a = gr.d_logp[t];
+        if (gr.d_entropy) e = gr.d_entropy[t];
+        if (gr.d_top && lane < gr.K) {
+            b = gr.d_top[t * gr.K + lane];
+            const int64_t at = static_cast<int64_t>(gr.top_id[t * gr.K + lane]) - e0;
+            id = at >= 0 && at < len ? static_cast<int>(at) : -1;
+        }
+    }
+    const float total = a + (gr.d_top ? wave_sum(b) : 0.0f);
+    uint64_t hot = gr.d_top ? __ballot(id >= 0 && b != 0.0f) : 0u;
+    // (b's of both signs may add up to zero)
+    const bool some = gr.d_top ? __any(b != 0.0f) : false;
+    if (left_out || (a == 0.0f && e == 0.0f && total == 0.0f && !some)) {
+        if (tid < sp.head + sp.tail) Vec<T>::put(out + (tid < sp.head ? tid : tid + sp.nvec * N), 0.0f);
+        for (int i = tid; i < sp.nvec; i += TR) store16<Stream>(dst + i, make_uint4(0u, 0u, 0u, 0u));
+        return;
+    }
+    const float lse = gr.lse[t], nl = -lse * kLog2e;
+    const float c = -fmaf(e, e != 0.0f ? gr.entropy[t] : 0.0f, total), c2 = -e * kLn2;  // dz = p (c + c2 log2 p) + ...
+    // Beside a large log-sum-exp its rounding is no longer small (a row of 1e30: the logarithm of the sum is gone): such a
+    // row's own maximum and sum are formed again, by every segment.
+    const bool far = fabsf(lse) > kFarLogit;
+    float top = 0.0f, log_sum = 0.0f;
+    if (far) row_max_log<T, TR>(logits + t * rows.stride, rows.V, top, log_sum);
+    auto grad = [&](float x) {
+        const float d = far ? ((x - top) - log_sum) * kLog2e : fmaf(x, kLog2e, nl);
+        return __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, kLowest2), c2, c);
+    };
+    int y = -1;
+    if (gr.d_logp && rows.target) {
+        const int64_t yl = static_cast<int64_t>(rows.target[t]) - e0;
+        y = yl >= 0 && yl < len ? static_cast<int>(yl) : -1;
+    }
+    // what element i of the segment gets beside its share of the softmax
+    auto extra = [&](int i, float v) {
+        if (i == y) v += a;
+        for (uint64_t h = hot; h; h &= h - 1) {
+            const int k = __builtin_ctzll(h);
+            if (i == __builtin_amdgcn_readlane(id, k)) v += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b), k));
+        }
+        return v;
+    };
+    {
+        const bool mine = tid < sp.head + sp.tail;
+        const int i = mine ? (tid < sp.head ? tid : tid + sp.nvec * N) : 0;
+        const float v = extra(i, grad(Vec<T>::get(p + i)));
+        if (mine) Vec<T>::put(out + i, v);
+    }
+    const T *body = p + sp.head;
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (tid + u * TR < sp.nvec) v[u] = load16<Stream>(body + (tid + u * TR) * N);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int iv = tid + u * TR;
+        const int first = sp.head + iv * N;
+        float x[N];
+        if (iv < sp.nvec) {
+            Vec<T>::unpack(v[u], x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = grad(x[i]);
+        }
+        auto at = [&](int place, float add) {
+            if (static_cast<unsigned>(place - first) < static_cast<unsigned>(N))
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (place - first == i) x[i] += add;
+        };
+        at(y, a);
+        for (uint64_t h = hot; h; h &= h - 1) {
+            const int k = __builtin_ctzll(h);
+            at(__builtin_amdgcn_readlane(id, k), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b), k)));
+        }
+        if (iv < sp.nvec) store16<Stream>(dst + iv, Vec<T>::pack(x));
+    }
+}
+
+// ----------------------------------------------------------------------------
+// host side
+// ----------------------------------------------------------------------------
+static ScoreRows score_rows(const spo_logprob_desc *d) {
+    return ScoreRows{d->T, d->V, d->logits_stride ? d->logits_stride : d->V, d->target, d->mask};
+}
+
+static bool streams(const spo_logprob_desc *d) { return d->T * d->V * (d->dtype == SPO_FP32 ? 4 : 2) > kStreamBytes; }
+
+// one round per segment where two would leave compute units without their eight workgroups
+static RowGrid score_grid(const spo_logprob_desc *d) {
+    const RowGrid g = row_grid(d->T, d->V, d->dtype, kScoreGroup, kScoreRounds, kScoreNarrow);
+    return g.units() >= 2048 ? g : row_grid(d->T, d->V, d->dtype, kScoreGroup, 1, kScoreNarrow);
+}
+
+struct ScorePlan {
+    RowGrid grid;
+    float *part, *group_max;
+    size_t bytes;
+};
+static ScorePlan plan_scores(const spo_logprob_desc *d, void *ws) {
+    ScorePlan p;
+    const int64_t T = std::max<int64_t>(d->T, 1);
+    p.grid = score_grid(d);
+    Arena a(ws);
+    // room for the shortest segments and groups of either type: those in use get longer with T and V, and room sized for the
+    // largest batch is to serve every smaller one
+    p.part = a.take<float>(static_cast<size_t>(T * ceil_div(d->V, kWave * kScoreGroup * Vec<float>::N)) * 3);
+    p.group_max = d->top_k ? a.take<float>(static_cast<size_t>(T * (ceil_div(d->V, kScoreGroup * Vec<float>::N) + kRowThreads))) : nullptr;
+    p.bytes = a.used;
+    return p;
+}
+
+template <typename T, int TR, bool Stream, bool Top>
+static void launch_score_rows(const spo_logprob_desc *d, const ScorePlan &p, const ScoreOut &o, hipStream_t s) {
+    auto *kernel = p.grid.seg_len <= TR * kScoreGroup * Vec<T>::N ? score_rows_kernel<T, TR, 1, Stream, Top>
+                                                                 : score_rows_kernel<T, TR, kScoreRounds, Stream, Top>;
+    kernel<<<p.grid.blocks(), kRowThreads, 0, s>>>(static_cast<const T *>(d->logits), score_rows(d), p.grid, p.part, p.group_max, o);
+}
+template <typename T, bool Top>
+static void launch_scores(const spo_logprob_desc *d, const ScorePlan &p, const ScoreOut &o, hipStream_t s) {
+    const bool narrow = p.grid.per_wg > 1;
+    if (narrow) streams(d) ? launch_score_rows<T, kWave, true, Top>(d, p, o, s) : launch_score_rows<T, kWave, false, Top>(d, p, o, s);
+    else if (streams(d)) launch_score_rows<T, kRowThreads, true, Top>(d, p, o, s);
+    else launch_score_rows<T, kRowThreads, false, Top>(d, p, o, s);
+    const T *z = static_cast<const T *>(d->logits);
+    if constexpr (Top) {
+        auto *pick = narrow ? score_pick_kernel<T, kWave> : score_pick_kernel<T, kRowThreads>;
+        pick<<<fold_grid(d->T), kPickThreads, 0, s>>>(z, score_rows(d), p.grid, p.part, p.group_max, o);
+    } else if (p.grid.nseg > 1) {
+        score_join_kernel<T><<<fold_grid(ceil_div(d->T, 4)), 256, 0, s>>>(z, score_rows(d), p.grid.nseg, p.part, o);
+    }
+}
+
+static int logits_logprob_fwd(const spo_logprob_desc *d, const ScoreOut &o, void *ws, size_t ws_bytes, hipStream_t s) {
+    const ScorePlan p = plan_scores(d, ws);
+    if (ws_bytes < p.bytes) return SPO_EWORKSPACE;
+    if (d->T == 0) return SPO_OK;
+    ScopedKernelTimer timer(kTimeLogitsFwd, s);
+    if (d->dtype == SPO_BF16) o.K ? launch_scores<bf16_t, true>(d, p, o, s) : launch_scores<bf16_t, false>(d, p, o, s);
+    else o.K ? launch_scores<float, true>(d, p, o, s) : launch_scores<float, false>(d, p, o, s);
+    return launch_status();
+}
+
+template <typename T>
+static void launch_score_grad(const spo_logprob_desc *d, const ScoreGrads &g, void *d_logits, hipStream_t s) {
+    const RowGrid grid = row_grid(d->T, d->V, d->dtype, kScoreGradGroup, 1, kScoreGradNarrow);
+    auto *kernel = grid.per_wg > 1 ? score_grad_kernel<T, kWave, false>
+                 : streams(d)      ? score_grad_kernel<T, kRowThreads, true>
+                                   : score_grad_kernel<T, kRowThreads, false>;
+    kernel<<<grid.blocks(), kRowThreads, 0, s>>>(static_cast<const T *>(d->logits), score_rows(d), grid, g, static_cast<T *>(d_logits));
+}
+
+}  // namespace spo
+
+using namespace spo;
+
+static int validate(const spo_logprob_desc *d) {
+    if (!d) return SPO_ENULL;
+    if (d->struct_size != sizeof(spo_logprob_desc)) return SPO_EINVAL;
+    if (d->dtype != SPO_BF16 && d->dtype != SPO_FP32) return SPO_EINVAL;
+    if (d->T < 0 || d->V < 1) return SPO_EINVAL;
+    if (d->T >= (int64_t(1) << 31) || d->V >= (int64_t(1) << 31)) return SPO_ERANGE;
+    if (d->top_k < 0 || d->top_k > d->V) return SPO_EINVAL;
+    if (d->top_k > SPO_MAX_TOP_K) return SPO_ERANGE;
+    const uintptr_t elt = d->dtype == SPO_FP32 ? 4 : 2;
+    if (d->logits) {
+        if (d->logits_stride != 0 && d->logits_stride < d->V) return SPO_EINVAL;
+        if (reinterpret_cast<uintptr_t>(d->logits) % elt) return SPO_EINVAL;
+        return SPO_OK;
+    }
+    if (d->w_layout != SPO_W_VH && d->w_layout != SPO_W_HV) return SPO_EINVAL;
+    if (!d->W || (d->T > 0 && !d->hidden)) return SPO_ENULL;
+    if (d->H < 1) return SPO_EINVAL;
+    if (d->H % 64 != 0 || d->top_k != 0) return SPO_EUNSUPPORTED;
+    if (d->H > 65536) return SPO_ERANGE;
+    if (reinterpret_cast<uintptr_t>(d->hidden) % 16 || reinterpret_cast<uintptr_t>(d->W) % 16) return SPO_EINVAL;
+    return SPO_OK;
+}
+
+extern "C" size_t spo_logprob_fwd_workspace_bytes(const spo_logprob_desc *d) {
+    if (validate(d) != SPO_OK) return 0;
+    size_t b = 0;
+    if (d->logits) b = plan_scores(d, nullptr).bytes;
+    else head_logprob_fwd_workspace(d, &b);
+    return b;
+}
+
+extern "C" int spo_logprob_fwd(const spo_logprob_desc *d, float *logp, float *lse, float *entropy, int32_t *top_id, float *top_logp,
+                               void *ws, size_t ws_bytes, spo_stream_t stream) {
+    const int rc = validate(d);
+    if (rc) return rc;
+    if (d->T > 0 && (!lse || (d->target && !logp) || (d->top_k && (!top_id || !top_logp)))) return SPO_ENULL;
+    if (!ws) return SPO_EWORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) % 256 != 0) return SPO_EINVAL;
+    if (!d->target) logp = nullptr;
+    if (!d->logits) return head_logprob_fwd(d, logp, lse, entropy, ws, ws_bytes, as_stream(stream));
+    return logits_logprob_fwd(d, ScoreOut{logp, lse, entropy, top_id, top_logp, d->top_k}, ws, ws_bytes, as_stream(stream));
+}
+
+extern "C" size_t spo_logprob_bwd_workspace_bytes(const spo_logprob_desc *d, int64_t chunk_tokens) {
+    if (validate(d) != SPO_OK || chunk_tokens < 0) return 0;
+    size_t b = 256;  // the logits-in form needs none; a size that serves as one
+    if (!d->logits) head_logprob_bwd_workspace(d, chunk_tokens, &b);
+    return b;
+}
+
+extern "C" int spo_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *entropy, const float *d_logp,
+                               const float *d_entropy, const int32_t *top_id, const float *d_top_logp, void *d_hidden,
+                               int d_hidden_dtype, void *d_W, int d_W_dtype, int accumulate_dW, void *d_logits, int64_t chunk_tokens,
+                               void *ws, size_t ws_bytes, spo_stream_t stream) {
+    const int rc = validate(d);
+    if (rc) return rc;
+    if (chunk_tokens < 0) return SPO_EINVAL;
+    if (d->T > 0 && (!lse || (d_entropy && !entropy) || (d_logp && !d->target) || (d_top_logp && !top_id))) return SPO_ENULL;
+    if (d_top_logp && !d->top_k) return SPO_EINVAL;
+    if (d->logits) {
+        if (d->T == 0) return SPO_OK;
+        if (!d_logits) return SPO_ENULL;
+        const uintptr_t elt = d->dtype == SPO_FP32 ? 4 : 2;
+        if (reinterpret_cast<uintptr_t>(d_logits) % elt) return SPO_EINVAL;
+        const ScoreGrads g{lse, entropy, d_logp, d_entropy, top_id, d_top_logp, d->top_k};
+        ScopedKernelTimer timer(kTimeLogitsBwd, as_stream(stream));
+        if (d->dtype == SPO_BF16) launch_score_grad<bf16_t>(d, g, d_logits, as_stream(stream));
+        else launch_score_grad<float>(d, g, d_logits, as_stream(stream));
+        return launch_status();
+    }
+    if (!ws) return SPO_EWORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) % 256 != 0) return SPO_EINVAL;
+    auto type_ok = [](int t) { return t == SPO_FP32 || t == SPO_BF16; };
+    if ((d_hidden && !type_ok(d_hidden_dtype)) || (d_W && !type_ok(d_W_dtype))) return SPO_EINVAL;
+    if (reinterpret_cast<uintptr_t>(d_hidden) % 16 || reinterpret_cast<uintptr_t>(d_W) % 16) return SPO_EINVAL;
+    return head_logprob_bwd(d, lse, entropy, d_logp, d_entropy, d_hidden, d_hidden_dtype, d_W, d_W_dtype, accumulate_dW, chunk_tokens, ws,
+                            ws_bytes, as_stream(stream));
+}

@@ -23,6 +23,7 @@
 
 #include "gemm_core.hpp"
 #include "head_form.hpp"
+#include "logprob.hpp"
 #include "pg_common.hpp"
 #include "tile_choice.hpp"
 #include "timing.hpp"
@@ -317,11 +318,33 @@ __device__ __forceinline__ int64_t active_rows(const int32_t *n_act, int64_t row
 // Rows past the last active token are filled with zeros and (0, -inf, no target): every
 // exponential underflows to an exact zero.  A wavefront per row.  The first zero_rows rows of `zero`, of
 // zero_bytes each, are cleared on the way (d_hidden: rows of tokens without a gradient stay zero).
-template <typename T_>
+struct LossRecords {
+    const int32_t *target;
+    const float *lse, *g;
+    __device__ __forceinline__ float4 operator()(int64_t, bool live, int64_t src) const {
+        const float gs = live ? g[src] : 0.0f;
+        const uint32_t ts = live ? (static_cast<uint32_t>(target[src]) & 0x7fffffffu) | (gs > 0.0f ? 0x80000000u : 0u)
+                                 : 0x7fffffffu;
+        return make_float4(fabsf(gs), live ? log2f(fabsf(gs)) - lse[src] * kLog2e : -INFINITY, __uint_as_float(ts), 0.0f);
+    }
+};
+// Log-probs and entropies: (c, -lse * log2(e), target, c2) with the gradient's softmax part p (c + c2 log2 p),
+// c = -(a + e H), c2 = -e ln 2, and a itself beside it in hot[r].
+struct ScoreRecords {
+    const int32_t *target;
+    const float *lse, *entropy, *d_logp, *d_entropy;
+    float *hot;
+    __device__ __forceinline__ float4 operator()(int64_t r, bool live, int64_t src) const {
+        const float a = live && d_logp ? d_logp[src] : 0.0f, e = live && d_entropy ? d_entropy[src] : 0.0f;
+        hot[r] = a;
+        const uint32_t ts = live && d_logp ? static_cast<uint32_t>(target[src]) & 0x7fffffffu : 0x7fffffffu;
+        return make_float4(-fmaf(e, e != 0.0f ? entropy[src] : 0.0f, a), live ? -lse[src] * kLog2e : -INFINITY, __uint_as_float(ts), -e * kLn2);
+    }
+};
+template <typename T_, typename Records>
 __global__ void __launch_bounds__(256)
 gather_chunk_kernel(const T_ *__restrict__ X, int64_t H, const int32_t *__restrict__ act_idx,
-                    const int32_t *__restrict__ n_act, int64_t row_base, int64_t rows,
-                    const int32_t *__restrict__ target, const float *__restrict__ lse, const float *__restrict__ g,
+                    const int32_t *__restrict__ n_act, int64_t row_base, int64_t rows, Records record,
                     bf16_t *__restrict__ Xc, bf16_t *__restrict__ Xs, float4 *__restrict__ tok, char *__restrict__ zero,
                     int64_t zero_rows, int64_t zero_bytes) {
     const int64_t r = flat_block() * 4 + (threadIdx.x >> 6);
@@ -344,12 +367,7 @@ gather_chunk_kernel(const T_ *__restrict__ X, int64_t H, const int32_t *__restri
             if (Xs) store_split<1>(Xs + r * (kSplitTerms * H) + i * 8, H, x);
         }
     }
-    if (lane == 0) {
-        const float gs = live ? g[src] : 0.0f;
-        const uint32_t ts = live ? (static_cast<uint32_t>(target[src]) & 0x7fffffffu) | (gs > 0.0f ? 0x80000000u : 0u)
-                                 : 0x7fffffffu;
-        tok[r] = make_float4(fabsf(gs), live ? log2f(fabsf(gs)) - lse[src] * kLog2e : -INFINITY, __uint_as_float(ts), 0.0f);
-    }
+    if (lane == 0) tok[r] = record(r, live, src);
 }
 
 // ----------------------------------------------------------------------------
@@ -667,20 +685,10 @@ struct SweepMap {
     __host__ __device__ int64_t first_tile(int split) const { return split * nVt / ns; }
 };
 
-constexpr int kEmitNone = 0, kEmitLogits = 1, kEmitProbs = 2;  // see fwd_sweep_kernel
-// operand stages + the per-thread running state (+ the per-token references)
-template <typename T> constexpr int kSweepLds(int emit) { return T::LDS_BYTES + T::NT * (emit == kEmitProbs ? 48 : 32); }
-
-// Exchange between neighbouring groups of 16 lanes: v_permlane16_swap(a, b) swaps the odd groups
-// of a with the even groups of b.  With a, b the values a lane holds for two consecutive MFMA
-// blocks q, q+1, lane group g ends up with (in a, b) the values of block q + (g & 1) from lane
-// groups (g & 2) and (g & 2) + 1.
-__device__ __forceinline__ void swap_lane_groups(uint32_t &a, uint32_t &b) {
-    typedef unsigned v2u __attribute__((ext_vector_type(2)));
-    const v2u t = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-    a = t.x;
-    b = t.y;
-}
+constexpr int kEmitNone = 0, kEmitLogits = 1, kEmitProbs = 2, kEmitEntropy = 3;  // see fwd_sweep_kernel
+// operand stages + the per-thread running state (+ the per-token references, or the sums that an entropy needs)
+constexpr int sweep_slots_of(int emit) { return emit == kEmitProbs || emit == kEmitEntropy ? 3 : 2; }
+template <typename T> constexpr int kSweepLds(int emit) { return T::LDS_BYTES + T::NT * 16 * sweep_slots_of(emit); }
 
 // two floats as a pair of IEEE halves, round to nearest even
 __device__ __forceinline__ uint32_t pack_f16x2_rn(float lo, float hi) {
@@ -690,6 +698,8 @@ __device__ __forceinline__ uint32_t pack_f16x2_rn(float lo, float hi) {
 }
 
 // Emit = kEmitNone: the forward proper; the logits exist in registers only.
+// Emit = kEmitEntropy: the same with a third running sum, of x 2^x with x = (logit - maximum) log2(e), which goes to offs as
+// the others go to part_max and part_sum; two operations more per logit.
 // The other two forms serve the one-call forward + backward: every finished tile is also
 // written out, in the blocked layout of the logit gradients (token n of this launch, vocabulary
 // entry v at Z + (v / 64) * z_blk + n * 64 + v % 64).
@@ -726,10 +736,12 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
     auto state = [&] {
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));  // not to be traced: the address is formed anew at every use
-        return reinterpret_cast<float4 *>(lds + TT::LDS_BYTES) + (Emit == kEmitProbs ? 3 : 2) * tid;
+        return reinterpret_cast<float4 *>(lds + TT::LDS_BYTES) + sweep_slots_of(Emit) * tid;
     };
+    constexpr bool kStored = Emit == kEmitLogits || Emit == kEmitProbs;
     state()[0] = make_float4(kNegBig, kNegBig, kNegBig, kNegBig);
     state()[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (Emit == kEmitEntropy) state()[2] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (Emit == kEmitProbs) {  // the references of this lane's four tokens: the workgroup keeps its token tile
         const float *r = offs + n0 + TT::wave_n0() + (lane & 15);
         state()[2] = make_float4(r[0], r[TT::MI], r[2 * TT::MI], r[3 * TT::MI]);
@@ -760,8 +772,8 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
         float4 *st = state();
         const float4 m4 = st[0], s4 = st[1];
         float m_run[TT::FN] = {m4.x, m4.y, m4.z, m4.w}, s_run[TT::FN] = {s4.x, s4.y, s4.z, s4.w};
-        float ref[TT::FN] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (Emit == kEmitProbs) {
+        float ref[TT::FN] = {0.0f, 0.0f, 0.0f, 0.0f};  // kEmitEntropy: the third running sum
+        if (Emit == kEmitProbs || Emit == kEmitEntropy) {
             const float4 r4 = st[2];
             ref[0] = r4.x; ref[1] = r4.y; ref[2] = r4.z; ref[3] = r4.w;
         }
@@ -787,8 +799,8 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
                 if (grp == 0)
                     offs[(vt * TT::WGM + TT::wave_m0() / TT::WM) * T_pad + n0 + TT::wave_n0() + fn * TT::MI + col] = off;
             }
-            float s = 0.0f;
-            uint16_t *row = Emit ? Z + (n0 + TT::wave_n0() + fn * TT::MI + col) * kBlockK + piece : nullptr;
+            float s = 0.0f, w = 0.0f;
+            uint16_t *row = kStored ? Z + (n0 + TT::wave_n0() + fn * TT::MI + col) * kBlockK + piece : nullptr;
 #pragma unroll
             for (int b = 0; b < TT::FM / 4; ++b) {
                 uint32_t lo[4], hi[4];
@@ -797,8 +809,10 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
                     float e[4], v[4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        e[r] = __builtin_amdgcn_exp2f(fmaf(acc[4 * b + q][fn][r], kLog2e, c));
+                        const float x = fmaf(acc[4 * b + q][fn][r], kLog2e, c);
+                        e[r] = __builtin_amdgcn_exp2f(x);
                         s += e[r];
+                        if (Emit == kEmitEntropy) w = fmaf(e[r], fmaxf(x, kLowest2), w);
                         v[r] = Emit == kEmitProbs ? e[r] * a : acc[4 * b + q][fn][r] - off;
                     }
                     if (Emit == kEmitProbs) {
@@ -810,7 +824,7 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
                         hi[q] = pack_f16x2_rn(v[2], v[3]);
                     }
                 }
-                if (Emit) {
+                if (kStored) {
                     swap_lane_groups(lo[0], lo[1]);
                     swap_lane_groups(hi[0], hi[1]);
                     swap_lane_groups(lo[2], lo[3]);
@@ -820,9 +834,14 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
                     *reinterpret_cast<uint4 *>(out + kBlockK / 2) = make_uint4(lo[2], hi[2], lo[3], hi[3]);
                 }
             }
+            if (Emit == kEmitEntropy) {
+                const float d = fmaxf((m_run[fn] - nm) * kLog2e, kLowest2);
+                ref[fn] = __builtin_amdgcn_exp2f(d) * fmaf(d, s_run[fn], ref[fn]) + w;
+            }
             s_run[fn] = s_run[fn] * __builtin_amdgcn_exp2f((m_run[fn] - nm) * kLog2e) + s;
             m_run[fn] = nm;
         }
+        if (Emit == kEmitEntropy) st[2] = make_float4(ref[0], ref[1], ref[2], ref[3]);
         st[0] = make_float4(m_run[0], m_run[1], m_run[2], m_run[3]);
         st[1] = make_float4(s_run[0], s_run[1], s_run[2], s_run[3]);
     };
@@ -833,7 +852,7 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
     // values between two tiles than registers: scaled probabilities spill 4 of them (a head [H,V] read as it is 20, its logits
     // 13; without stores 8, the recompute 3), which come back in up to 10 four-byte loads per tile, none inside the loop over the
     // steps.
-    constexpr bool kRun = Emit != kEmitNone;
+    constexpr bool kRun = kStored;
     constexpr int kStores = kRun ? TT::FN * (TT::FM / 4) * 2 : 0;
     typedef typename TT::template Loop<WCols, false> Tiles;
     auto tile = [&](int64_t vt) {
@@ -858,6 +877,34 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
     float *red_s = red_m + TT::WGM * TT::BN;
     const float4 m4 = state()[0], s4 = state()[1];
     const float m_run[TT::FN] = {m4.x, m4.y, m4.z, m4.w}, s_run[TT::FN] = {s4.x, s4.y, s4.z, s4.w};
+    if constexpr (Emit == kEmitEntropy) {
+        float *red_u = red_s + TT::WGM * TT::BN;
+        const float4 u4 = state()[2];
+        const float u_run[TT::FN] = {u4.x, u4.y, u4.z, u4.w};
+        __syncthreads();  // operand stages are no longer read
+#pragma unroll
+        for (int fn = 0; fn < TT::FN; ++fn) {
+            float m = m_run[fn], sum = s_run[fn], u = u_run[fn];
+#pragma unroll
+            for (int o = TT::MI; o < kWave; o <<= 1) score_join(m, sum, u, __shfl_xor(m, o, kWave), __shfl_xor(sum, o, kWave), __shfl_xor(u, o, kWave));
+            if (lane < TT::MI) {
+                const int slot = (TT::wave_id() % TT::WGM) * TT::BN + TT::acc_col(fn);
+                red_m[slot] = m;
+                red_s[slot] = sum;
+                red_u[slot] = u;
+            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < TT::BN; c += TT::NT) {
+            float m = red_m[c], sum = red_s[c], u = red_u[c];
+#pragma unroll
+            for (int w = 1; w < TT::WGM; ++w) score_join(m, sum, u, red_m[w * TT::BN + c], red_s[w * TT::BN + c], red_u[w * TT::BN + c]);
+            part_max[split * T_pad + n0 + c] = m;
+            part_sum[split * T_pad + n0 + c] = sum;
+            offs[split * T_pad + n0 + c] = u;
+        }
+        return;
+    }
     __syncthreads();  // operand stages are no longer read
 #pragma unroll
     for (int fn = 0; fn < TT::FN; ++fn) {
@@ -904,12 +951,15 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
 // Workgroups map to (token tile, vocabulary split) as in the forward sweep (SweepMap).  The
 // gradients go from the accumulators to memory without a detour through LDS.
 
-template <typename TT, bool WCols>
+// Scores: the gradient of log-probs and entropies instead (see gather_chunk_kernel for the records):
+// dz[t][v] = a [v == target] + p (c + c2 log2 p), three operations more per logit; a comes from hot[t], looked up by the
+// one lane group that needs it.
+template <typename TT, bool WCols, bool Scores = false>
 __global__ void __launch_bounds__(TT::NT, 2)
 recompute_dz_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V,
                     const char *__restrict__ X, int64_t ldx_bytes, int64_t T_valid, int KT,
                     const float4 *__restrict__ tok, int64_t nVt, bf16_t *__restrict__ dZ,
-                    int64_t dz_blk, const int32_t *__restrict__ n_act, int64_t row_base) {
+                    int64_t dz_blk, const int32_t *__restrict__ n_act, int64_t row_base, const float *__restrict__ hot) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     static_assert(TT::BM % kBlockK == 0 && kBlockK == 4 * TT::MI && TT::FM % 4 == 0,
                   "a block of dZ is four MFMA blocks of vocabulary rows");
@@ -952,8 +1002,13 @@ recompute_dz_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V,
             const int src = fn * TT::MI + col;
             const float ag = __shfl(rec.x, src, kWave), nl = __shfl(rec.y, src, kWave);
             const uint32_t ts = __float_as_uint(__shfl(rec.z, src, kWave));
+            const float c2 = Scores ? __shfl(rec.w, src, kWave) : 0.0f;
+            auto value = [&](float z) {  // Scores: ag is c
+                const float x = fmaf(z, kLog2e, nl), e = __builtin_amdgcn_exp2f(x);
+                return Scores ? e * fmaf(fmaxf(x, kLowest2), c2, ag) : e;
+            };
             // the values are formed as |g| * p >= 0; the sign of -g is put on afterwards, two at a time
-            const uint32_t sgn = (ts & 0x80000000u) ? 0x80008000u : 0u;
+            const uint32_t sgn = !Scores && (ts & 0x80000000u) ? 0x80008000u : 0u;
             // where the target's vocabulary row sits among this wave's rows, if it does
             const int dy = static_cast<int>(ts & 0x7fffffffu) - (m0 + TT::wave_m0());
             int fq = 0, rq = 0, gq = 0;
@@ -968,7 +1023,7 @@ recompute_dz_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V,
                 for (int q = 0; q < 4; ++q) {
                     float e[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(acc[4 * b + q][fn][i], kLog2e, nl));
+                    for (int i = 0; i < 4; ++i) e[i] = value(acc[4 * b + q][fn][i]);
                     lo[q] = pack_bf16x2_rn(e[0], e[1]);
                     hi[q] = pack_bf16x2_rn(e[2], e[3]);
                 }
@@ -979,7 +1034,8 @@ recompute_dz_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V,
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             if ((fq & 3) == q && rq == i) x = acc[4 * b + q][fn][i];
-                    const uint32_t v = f32_to_bf16(__builtin_amdgcn_exp2f(fmaf(x, kLog2e, nl)) - ag);
+                    const float add = Scores ? hot[n0 + TT::wave_n0() + src] : -ag;
+                    const uint32_t v = f32_to_bf16(value(x) + add);
                     const uint32_t keep = (rq & 1) ? 0x0000ffffu : 0xffff0000u, put = (rq & 1) ? v << 16 : v;
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
@@ -988,11 +1044,12 @@ recompute_dz_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V,
                             else lo[q] = (lo[q] & keep) | put;
                         }
                 }
+                if (!Scores)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    lo[q] ^= sgn;
-                    hi[q] ^= sgn;
-                }
+                    for (int q = 0; q < 4; ++q) {
+                        lo[q] ^= sgn;
+                        hi[q] ^= sgn;
+                    }
                 swap_lane_groups(lo[0], lo[1]);
                 swap_lane_groups(hi[0], hi[1]);
                 swap_lane_groups(lo[2], lo[3]);
@@ -1441,15 +1498,6 @@ scale_rows_kernel(const T_ *__restrict__ src, const float *__restrict__ c, int64
 // ----------------------------------------------------------------------------
 // host side
 // ----------------------------------------------------------------------------
-// The kernels use more dynamic LDS than the default limit allows.  The attribute belongs
-// to the current device's copy of the kernel, so it is set on every call (a host-side
-// table lookup) rather than remembered in a process-wide flag.
-template <typename K>
-static int allow_lds(K kernel, int bytes) {
-    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess
-               ? SPO_OK : SPO_EHIP;
-}
-
 static inline int64_t round_up(int64_t x, int64_t a) { return ceil_div(x, a) * a; }
 static inline unsigned grid1(int64_t n, int per = 256) { return static_cast<unsigned>(ceil_div(n, per)); }
 
@@ -1699,41 +1747,42 @@ static int launch_gemm(const Gemm &g, hipStream_t s, int nsplit, float *partials
 }
 
 // The gathered rows of a chunk (see gather_chunk_kernel), and d_hidden[0..zero_rows) (NULL: not) cleared.
-static void launch_gather(const spo_pg_desc *d, const void *X, const int32_t *act_idx, const int32_t *n_act, int64_t row_base,
-                          int64_t rows, const int32_t *target, const float *lse, const float *g, bf16_t *Xc, bf16_t *Xs,
-                          float4 *tok, void *d_hidden, int d_hidden_dtype, int64_t zero_rows, hipStream_t s) {
+template <typename Records>
+static void launch_gather(int dtype, int64_t H, const void *X, const int32_t *act_idx, const int32_t *n_act, int64_t row_base,
+                          int64_t rows, const Records &record, bf16_t *Xc, bf16_t *Xs, float4 *tok, void *d_hidden, int d_hidden_dtype,
+                          int64_t zero_rows, hipStream_t s) {
     if (!d_hidden) zero_rows = 0;
     const dim3 grid = fold_grid(ceil_div(std::max(rows, zero_rows), 4));
-    const int64_t zero_bytes = d->H * (d_hidden_dtype == SPO_FP32 ? 4 : 2);
-    if (d->dtype == SPO_FP32)
-        gather_chunk_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(X), d->H, act_idx, n_act, row_base, rows,
-                                                        target, lse, g, Xc, Xs, tok, static_cast<char *>(d_hidden), zero_rows,
-                                                        zero_bytes);
+    const int64_t zero_bytes = H * (d_hidden_dtype == SPO_FP32 ? 4 : 2);
+    if (dtype == SPO_FP32)
+        gather_chunk_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(X), H, act_idx, n_act, row_base, rows, record, Xc, Xs,
+                                                        tok, static_cast<char *>(d_hidden), zero_rows, zero_bytes);
     else
-        gather_chunk_kernel<bf16_t><<<grid, 256, 0, s>>>(static_cast<const bf16_t *>(X), d->H, act_idx, n_act, row_base, rows,
-                                                         target, lse, g, Xc, Xs, tok, static_cast<char *>(d_hidden), zero_rows,
-                                                         zero_bytes);
+        gather_chunk_kernel<bf16_t><<<grid, 256, 0, s>>>(static_cast<const bf16_t *>(X), H, act_idx, n_act, row_base, rows, record, Xc, Xs,
+                                                         tok, static_cast<char *>(d_hidden), zero_rows, zero_bytes);
 }
 
 // The logit gradients of the active ones of Tcp gathered rows X; W: the head as it reads it (cols: [H,V]).
-template <typename TT, bool WCols>
+// hot: see recompute_dz_kernel (Scores); NULL: of the loss.
+template <typename TT, bool WCols, bool Scores>
 static int launch_recompute(const spo_pg_desc *d, const void *W, const bf16_t *X, int64_t Kc, int64_t Tcp, const float4 *tok, bf16_t *dZ,
-                            const int32_t *n_act, int64_t row_base, hipStream_t s) {
-    auto *kernel = recompute_dz_kernel<TT, WCols>;
+                            const int32_t *n_act, int64_t row_base, const float *hot, hipStream_t s) {
+    auto *kernel = recompute_dz_kernel<TT, WCols, Scores>;
     if (int rc = allow_lds(kernel, TT::LDS_BYTES)) return rc;
     const int64_t nVt = ceil_div(d->V, TT::BM), wgs = sweep_blocks_max(Tcp / TT::BN, nVt);
     ScopedKernelTimer timer(kTimeRecompute, s);
     kernel<<<static_cast<unsigned>(wgs), TT::NT, TT::LDS_BYTES, s>>>(
         static_cast<const char *>(W), (WCols ? d->V : Kc) * 2, d->V, reinterpret_cast<const char *>(X), Kc * 2, Tcp,
-        static_cast<int>(Kc / kBK), tok, nVt, dZ, Tcp * kBlockK, n_act, row_base);
+        static_cast<int>(Kc / kBK), tok, nVt, dZ, Tcp * kBlockK, n_act, row_base, hot);
     return SPO_OK;
 }
+template <bool Scores>
 static int launch_recompute(const spo_pg_desc *d, const void *W, bool cols, const bf16_t *X, int64_t Kc, int64_t Tcp, bool small,
-                            const float4 *tok, bf16_t *dZ, const int32_t *n_act, int64_t row_base, hipStream_t s) {
-    if (small) return cols ? launch_recompute<TS, true>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, s)
-                           : launch_recompute<TS, false>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, s);
-    return cols ? launch_recompute<TL, true>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, s)
-                : launch_recompute<TL, false>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, s);
+                            const float4 *tok, bf16_t *dZ, const int32_t *n_act, int64_t row_base, const float *hot, hipStream_t s) {
+    if (small) return cols ? launch_recompute<TS, true, Scores>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, hot, s)
+                           : launch_recompute<TS, false, Scores>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, hot, s);
+    return cols ? launch_recompute<TL, true, Scores>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, hot, s)
+                : launch_recompute<TL, false, Scores>(d, W, X, Kc, Tcp, tok, dZ, n_act, row_base, hot, s);
 }
 
 // dHidden of M rows (of Tcp in the blocks of dZ): every part of the vocabulary, the head as WT, or as it was given (NULL).
@@ -1844,10 +1893,10 @@ int fused_bwd(const spo_pg_desc *d, const float *logp, const float *lse, float g
         const bool small = small_sweep(Tv, V, p.Kc);
         const int64_t edge = tile_edge(small), Tcp = round_up(Tv, edge);
         // (the first chunk's launch also clears d_hidden: later ones would clear what earlier ones wrote)
-        launch_gather(d, d->hidden, p.act_idx, p.n_act, t0, Tcp, d->target, lse, p.g, d->dtype == SPO_BF16 || d_W ? p.Xc : nullptr,
-                      p.Xs, p.tok, c == 0 ? d_hidden : nullptr, d_hidden_dtype, T, s);
+        launch_gather(d->dtype, H, d->hidden, p.act_idx, p.n_act, t0, Tcp, LossRecords{d->target, lse, p.g},
+                      d->dtype == SPO_BF16 || d_W ? p.Xc : nullptr, p.Xs, p.tok, c == 0 ? d_hidden : nullptr, d_hidden_dtype, T, s);
         const bf16_t *Xk = d->dtype == SPO_FP32 ? p.Xs : p.Xc, *Xrows = p.Xc;  // operands of the recompute and of dW
-        if ((rc = launch_recompute(d, Wk, direct && hv, Xk, p.Kc, Tcp, small, p.tok, p.dZ, p.n_act, t0, s))) return rc;
+        if ((rc = launch_recompute<false>(d, Wk, direct && hv, Xk, p.Kc, Tcp, small, p.tok, p.dZ, p.n_act, t0, nullptr, s))) return rc;
         if (d_hidden && (rc = launch_dhidden(d, p.dZ, Tcp, Tcp, direct ? nullptr : p.WT, p.V_pad, d_hidden, d_hidden_dtype, p.n_act, t0,
                                              p.act_idx + t0, nullptr, p.part_tiles, s)))
             return rc;
@@ -2049,12 +2098,12 @@ int fused_fwd_bwd(const spo_pg_desc *d, float grad_loss, float *loss, float *log
             continue;
         }
         compact_active_kernel<<<1, 1024, 0, s>>>(p.g + t0, Tv, p.act_idx, p.n_act);
-        launch_gather(d, Xpiece, p.act_idx, p.n_act, 0, Tzp, d->target + t0, lse + t0, p.g + t0,
+        launch_gather(d->dtype, H, Xpiece, p.act_idx, p.n_act, 0, Tzp, LossRecords{d->target + t0, lse + t0, p.g + t0},
                       d->dtype == SPO_BF16 || d_W ? p.Xc : nullptr, nullptr, p.tok,
                       d_hidden ? static_cast<char *>(d_hidden) + t0 * H * dx_elt : nullptr, d_hidden_dtype, Tv, s);
         const bf16_t *Xrows = p.Xc;
         if (again) {
-            if ((rc = launch_recompute(d, Wk, direct && hv, Xrows, p.Kc, Tzp, p.small, p.tok, p.dZ, p.n_act, 0, s))) return rc;
+            if ((rc = launch_recompute<false>(d, Wk, direct && hv, Xrows, p.Kc, Tzp, p.small, p.tok, p.dZ, p.n_act, 0, nullptr, s))) return rc;
         } else {
             constexpr int per_wg = 8;
             const int64_t n_blk = p.V_blk / kBlockK;
@@ -2067,6 +2116,175 @@ int fused_fwd_bwd(const spo_pg_desc *d, float grad_loss, float *loss, float *log
                                              d_hidden_dtype, p.n_act, 0, p.act_idx, nullptr, p.part_tiles, s)))
             return rc;
         if (d_W && (rc = launch_dW(d, p.dZ, Xrows, Tzp, edge, dW_sum, dW_sum_dtype, (c > 0 || accumulate_dW) ? 1 : 0, p.n_act, 0,
+                                   p.part_tiles, s)))
+            return rc;
+    }
+    if (need_acc) f32_to_bf16_kernel<<<grid1(V * H / 8), 256, 0, s>>>(p.dW_acc, static_cast<bf16_t *>(d_W), V * H);
+    return launch_status();
+}
+
+// ----------------------------------------------------------------------------
+// log-probs and entropies from hidden states and the head, and their gradient
+// ----------------------------------------------------------------------------
+// The forward is the loss's sweep with a third running sum; the backward is the loss's with other records.
+
+// lse, log-prob and entropy of each token from the splits' partial results, `ways` wavefronts per block of 64 tokens.
+__global__ void __launch_bounds__(kTokWaves * kWave)
+head_scores_kernel(const float *__restrict__ part_max, const float *__restrict__ part_sum, const float *__restrict__ part_u, int nsplit,
+                   int64_t split_stride, const float *__restrict__ z_target, const uint8_t *__restrict__ mask, int64_t T,
+                   float *__restrict__ logp, float *__restrict__ lse_out, float *__restrict__ entropy) {
+    __shared__ float sm[kTokWaves][kWave], ss[kTokWaves][kWave], su[kTokWaves][kWave];
+    const int lane = threadIdx.x & 63, way = threadIdx.x >> 6, ways = blockDim.x >> 6;
+    const int64_t t = flat_block() * kTokThreads + lane;
+    const bool live = t < T && (!mask || mask[t]);
+    float m = kNegBig, s = 0.0f, u = 0.0f;
+    if (live) {
+        constexpr int U = 8;  // pairs requested at a time
+        for (int i0 = way; i0 < nsplit; i0 += U * ways) {
+            float pm[U], ps[U], pu[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int i = i0 + k * ways;
+                pm[k] = i < nsplit ? part_max[i * split_stride + t] : kNegBig;
+                ps[k] = i < nsplit ? part_sum[i * split_stride + t] : 0.0f;
+                pu[k] = i < nsplit ? part_u[i * split_stride + t] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) score_join(m, s, u, pm[k], ps[k], pu[k]);
+        }
+    }
+    sm[way][lane] = m;
+    ss[way][lane] = s;
+    su[way][lane] = u;
+    __syncthreads();
+    if (way != 0 || t >= T) return;
+    if (live)
+        for (int w = 1; w < ways; ++w) score_join(m, s, u, sm[w][lane], ss[w][lane], su[w][lane]);
+    const float lse = live ? m + logf(s) : 0.0f;
+    lse_out[t] = lse;
+    if (logp) logp[t] = live ? z_target[t] - lse : 0.0f;
+    if (entropy) entropy[t] = live ? score_entropy(s, u) : 0.0f;
+}
+
+// The tokens that carry a gradient, in order (see compact_active_kernel).
+__global__ void __launch_bounds__(1024)
+compact_scored_kernel(const uint8_t *__restrict__ mask, const float *__restrict__ d_logp, const float *__restrict__ d_entropy, int64_t T,
+                      int32_t *__restrict__ act_idx, int32_t *__restrict__ n_act) {
+    __shared__ int wave_cnt[1024 / kWave];
+    compact_tokens<1024>(T, [&](int64_t t) {
+        if (mask && !mask[t]) return 0.0f;
+        const float a = d_logp ? d_logp[t] : 0.0f, e = d_entropy ? d_entropy[t] : 0.0f;
+        return a != 0.0f ? a : e;
+    }, act_idx, n_act, wave_cnt);
+}
+
+// What the loss's plans and launches read of a batch.
+static spo_pg_desc as_pg_desc(const spo_logprob_desc *d) {
+    spo_pg_desc p{};
+    p.struct_size = sizeof p;
+    p.dtype = d->dtype;
+    p.w_layout = d->w_layout;
+    p.T = d->T;
+    p.H = d->H;
+    p.V = d->V;
+    p.B = 1;
+    p.hidden = d->hidden;
+    p.W = d->W;
+    p.target = d->target;
+    p.mask = d->mask;
+    return p;
+}
+
+struct HeadScorePlan {
+    FwdPlan f;
+    float *part_u;
+    size_t bytes;
+};
+static HeadScorePlan plan_head_scores(const spo_pg_desc *d, void *ws) {
+    HeadScorePlan p;
+    p.f = plan_fwd(d, ws, true);
+    Arena a(ws ? static_cast<char *>(ws) + p.f.bytes : nullptr);
+    p.part_u = a.take<float>(static_cast<size_t>(sweep_room(d->T, d->V, true)));
+    p.bytes = p.f.bytes + a.used;
+    return p;
+}
+
+int head_logprob_fwd_workspace(const spo_logprob_desc *d, size_t *bytes) {
+    const spo_pg_desc pg = as_pg_desc(d);
+    *bytes = plan_head_scores(&pg, nullptr).bytes;
+    return SPO_OK;
+}
+
+int head_logprob_fwd(const spo_logprob_desc *d, float *logp, float *lse, float *entropy, void *ws, size_t ws_bytes, hipStream_t s) {
+    const spo_pg_desc pg = as_pg_desc(d);
+    const HeadScorePlan p = plan_head_scores(&pg, ws);
+    if (ws_bytes < p.bytes) return SPO_EWORKSPACE;
+    if (d->T == 0) return SPO_OK;
+    const bool fp32 = d->dtype == SPO_FP32, direct = direct_head(&pg), hv = d->w_layout == SPO_W_HV;
+    void *Wvh = direct ? nullptr : p.f.Wvh;
+    PrepJobs jobs = prep_head_jobs(&pg, Wvh, p.f.Ws, nullptr);
+    prep_rows(jobs, &pg, d->hidden, d->T, p.f.Xs);
+    if (d->target) launch_prep_with_targets(&pg, jobs, p.f.z_target, nullptr, 0, nullptr, s);
+    else launch_prep(&pg, jobs, s);
+    Sweep w{};
+    w.W = fp32 ? p.f.Ws : Wvh ? Wvh : d->W;
+    w.V = d->V;
+    w.Kc = p.f.Kc;
+    w.cols = direct && hv;
+    w.X = fp32 ? static_cast<const void *>(p.f.Xs) : d->hidden;
+    w.T = d->T;
+    w.part_max = p.f.part_max;
+    w.part_sum = p.f.part_sum;
+    w.offs = p.part_u;
+    if (int rc = launch_sweep<kEmitEntropy>(w, p.f.small, SweepMap(p.f.nTt, p.f.nVt, p.f.nsplit), s)) return rc;
+    const int ways = token_shape(p.f.nsplit, p.f.nblk_tok).ways;
+    head_scores_kernel<<<fold_grid(p.f.nblk_tok), ways * kWave, 0, s>>>(p.f.part_max, p.f.part_sum, p.part_u, p.f.nsplit, p.f.T_pad,
+                                                                      p.f.z_target, d->mask, d->T, logp, lse, entropy);
+    return launch_status();
+}
+
+int head_logprob_bwd_workspace(const spo_logprob_desc *d, int64_t chunk_tokens, size_t *bytes) {
+    const spo_pg_desc pg = as_pg_desc(d);
+    return fused_bwd_workspace(&pg, chunk_tokens, bytes);
+}
+
+int head_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *entropy, const float *d_logp, const float *d_entropy,
+                     void *d_hidden, int d_hidden_dtype, void *d_W, int d_W_dtype, int accumulate_dW, int64_t chunk_tokens, void *ws,
+                     size_t ws_bytes, hipStream_t s) {
+    if (d->dtype != SPO_BF16) return SPO_EUNSUPPORTED;
+    if (accumulate_dW && d_W && d_W_dtype != SPO_FP32) return SPO_EINVAL;
+    const spo_pg_desc pg = as_pg_desc(d);
+    const BwdPlan p = plan_bwd(&pg, chunk_tokens, ws, d_W && d_W_dtype == SPO_BF16);
+    if (ws_bytes < p.bytes) return SPO_EWORKSPACE;
+    const bool need_acc = p.dW_acc != nullptr;  // a bf16 d_W of several chunks (see fused_bwd)
+    const int64_t H = d->H, V = d->V, T = d->T;
+    void *dW_sum = need_acc ? p.dW_acc : d_W;
+    const int dW_sum_dtype = need_acc ? SPO_FP32 : d_W_dtype;
+    if (T == 0) {
+        if (d_W && !accumulate_dW) {
+            const int64_t words = d_W_dtype == SPO_FP32 ? V * H : V * H / 2;
+            fill_zero_kernel<<<grid1(words), 256, 0, s>>>(static_cast<uint32_t *>(d_W), words);
+        }
+        return launch_status();
+    }
+    const bool direct = direct_head(&pg), hv = d->w_layout == SPO_W_HV;
+    void *Wvh = direct ? nullptr : p.Wvh;
+    launch_prep(&pg, prep_head_jobs(&pg, Wvh, nullptr, d_hidden && !direct ? p.WT : nullptr), s);
+    compact_scored_kernel<<<1, 1024, 0, s>>>(d->mask, d_logp, d_entropy, T, p.act_idx, p.n_act);
+    const void *Wk = Wvh ? Wvh : d->W;
+    for (int64_t t0 = 0, c = 0; t0 < T; t0 += p.Tc, ++c) {  // chunks of the list of active tokens, as in fused_bwd
+        const int64_t Tv = std::min(p.Tc, T - t0);
+        const bool small = small_sweep(Tv, V, p.Kc);
+        const int64_t edge = tile_edge(small), Tcp = round_up(Tv, edge);
+        float *hot = p.g;  // of the chunk's rows
+        launch_gather(d->dtype, H, d->hidden, p.act_idx, p.n_act, t0, Tcp, ScoreRecords{d->target, lse, entropy, d_logp, d_entropy, hot}, p.Xc,
+                      nullptr, p.tok, c == 0 ? d_hidden : nullptr, d_hidden_dtype, T, s);
+        int rc;
+        if ((rc = launch_recompute<true>(&pg, Wk, direct && hv, p.Xc, p.Kc, Tcp, small, p.tok, p.dZ, p.n_act, t0, hot, s))) return rc;
+        if (d_hidden && (rc = launch_dhidden(&pg, p.dZ, Tcp, Tcp, direct ? nullptr : p.WT, p.V_pad, d_hidden, d_hidden_dtype, p.n_act, t0,
+                                             p.act_idx + t0, nullptr, p.part_tiles, s)))
+            return rc;
+        if (d_W && (rc = launch_dW(&pg, p.dZ, p.Xc, Tcp, edge, dW_sum, dW_sum_dtype, (c > 0 || accumulate_dW) ? 1 : 0, p.n_act, t0,
                                    p.part_tiles, s)))
             return rc;
     }
