@@ -405,6 +405,46 @@ int spo_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *en
                     int64_t chunk_tokens, void *ws, size_t ws_bytes, spo_stream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Orthogonalised updates of weight matrices (what becomes of a weight gradient, by Newton-Schulz
+ * products in the way of the Muon optimiser).  For each of `batch` matrices U of rows x cols:
+ *   X <- U / (|U|_F + eps);  `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X
+ * (A = X^T X on the other side where rows > cols), which moves every singular value towards one
+ * and keeps the singular vectors.  A zero matrix stays zero.
+ * products  SPO_PRODUCTS_FP16: the operands of the products are rounded to 11 bits, X itself is
+ *           kept in 22: results to about 1.5e-3 relative (in 2-norm over the matrix; matrices
+ *           whose smaller side is at most 64 are worked on as with SPO_PRODUCTS_SPLIT);
+ *           SPO_PRODUCTS_SPLIT: operands of 22 bits, three products for one: about 1e-6.
+ * Sums are in fp32 in a fixed order: results are bitwise reproducible.
+ * ------------------------------------------------------------------------- */
+#define SPO_PRODUCTS_FP16 0
+#define SPO_PRODUCTS_SPLIT 1
+typedef struct {
+    size_t struct_size;      /* sizeof(spo_orth_desc), checked                            */
+    int64_t batch, rows, cols;  /* batch >= 1; 1 <= rows, cols <= 65536                   */
+    int32_t steps;           /* 0..64; 5 in common use (0: only the division by the norm) */
+    int products;
+    float a, b, c;           /* in common use 3.4445, -4.7750, 2.0315                     */
+    float eps;               /* >= 0                                                      */
+} spo_orth_desc;
+
+/* The workspace size never shrinks with batch, rows or cols. */
+size_t spo_orthogonalize_workspace_bytes(const spo_orth_desc *d);
+
+/* out [batch][rows][cols] contiguous in out_dtype.  G in g_dtype: rows g_stride elements apart
+ * (0: cols), matrices g_batch_stride apart (0: rows * g_stride).  out may be G if both are contiguous and of one type. */
+int spo_orthogonalize(const spo_orth_desc *d, const void *G, int g_dtype, int64_t g_stride, int64_t g_batch_stride,
+                      void *out, int out_dtype, void *ws, size_t ws_bytes, spo_stream_t stream);
+
+/* The whole momentum step, in place on W and momentum; all arrays [batch][rows][cols] contiguous:
+ *   M <- mu M + G;  U = G + mu M (nesterov = 1) or M;  O = U orthogonalised;
+ *   W <- (1 - lr weight_decay) W - lr scale O
+ * W in w_dtype (one rounding of the fp32 result), momentum fp32, grad in g_dtype.
+ * Errors: mu outside [0, 1), lr or weight_decay negative -> SPO_EINVAL. */
+int spo_muon_update(const spo_orth_desc *d, void *W, int w_dtype, float *momentum, const void *grad, int g_dtype,
+                    float mu, int nesterov, float lr, float weight_decay, float scale, void *ws, size_t ws_bytes,
+                    spo_stream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Per-kernel timing (measurement aid, not part of the method; with the static
  * buffer of spo_sample_prompts_static the only state the library keeps).  While enabled, the loss entry points bracket each launch
  * of their heavy kernels with a pair of HIP events on the launch stream.

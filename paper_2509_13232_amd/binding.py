@@ -18,6 +18,7 @@ SPO_FP32, SPO_BF16 = 0, 1
 SPO_W_VH, SPO_W_HV = 0, 1
 SPO_SAMPLE_STATIC_MAX_N = 1 << 20
 SPO_MAX_TOP_K = 64
+SPO_PRODUCTS_FP16, SPO_PRODUCTS_SPLIT = 0, 1
 
 EXPORTS = (
     "spo_status_string", "spo_sample_prompts_workspace_bytes", "spo_sample_prompts",
@@ -30,6 +31,7 @@ EXPORTS = (
     "spo_pg_loss_fwd_bwd_workspace_bytes", "spo_pg_loss_fwd_bwd",
     "spo_logprob_fwd_workspace_bytes", "spo_logprob_fwd",
     "spo_logprob_bwd_workspace_bytes", "spo_logprob_bwd",
+    "spo_orthogonalize_workspace_bytes", "spo_orthogonalize", "spo_muon_update",
     "spo_kernel_timing_enable", "spo_kernel_timing_read",
 )
 TIMING_CLASSES = ("fwd_sweep", "bwd_recompute", "bwd_dhidden", "bwd_dw", "logits_fwd", "logits_bwd", "logits_to_dz")
@@ -58,6 +60,14 @@ class LogprobDesc(C.Structure):
         ("T", C.c_int64), ("H", C.c_int64), ("V", C.c_int64),
         ("hidden", C.c_void_p), ("W", C.c_void_p), ("logits", C.c_void_p), ("logits_stride", C.c_int64),
         ("target", C.c_void_p), ("mask", C.c_void_p), ("top_k", C.c_int32),
+    ]
+
+
+class OrthDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_size_t), ("batch", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64),
+        ("steps", C.c_int32), ("products", C.c_int),
+        ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float),
     ]
 
 
@@ -120,6 +130,12 @@ def lib():
         L.spo_logprob_bwd.restype = C.c_int
         L.spo_logprob_bwd.argtypes = [C.POINTER(LogprobDesc), vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, C.c_int, C.c_int, vp, i64,
                                       vp, sz, vp]
+        L.spo_orthogonalize_workspace_bytes.restype = sz
+        L.spo_orthogonalize_workspace_bytes.argtypes = [C.POINTER(OrthDesc)]
+        L.spo_orthogonalize.restype = C.c_int
+        L.spo_orthogonalize.argtypes = [C.POINTER(OrthDesc), vp, C.c_int, i64, i64, vp, C.c_int, vp, sz, vp]
+        L.spo_muon_update.restype = C.c_int
+        L.spo_muon_update.argtypes = [C.POINTER(OrthDesc), vp, C.c_int, vp, vp, C.c_int, f32, C.c_int, f32, f32, f32, vp, sz, vp]
         L.spo_kernel_timing_enable.restype = C.c_int
         L.spo_kernel_timing_enable.argtypes = [C.c_int]
         L.spo_kernel_timing_read.restype = C.c_int
@@ -571,3 +587,68 @@ def spo_logprob_bwd(desc, lse, entropy=None, d_logp=None, d_entropy=None, top_id
                              _dt(dx.dtype) if dx is not None else 0, _ptr(d_W), _dt(d_W.dtype) if d_W is not None else 0,
                              int(bool(accumulate_dW)), None, int(chunk_tokens), _ptr(ws), ws.numel(), _stream()), "spo_logprob_bwd")
     return dx, d_W
+
+
+# ------------------------------------------------- orthogonalised updates
+def _orth_desc(batch, rows, cols, steps, coeffs, eps, products):
+    d = OrthDesc()
+    d.struct_size = C.sizeof(OrthDesc)
+    d.batch, d.rows, d.cols, d.steps, d.products = batch, rows, cols, int(steps), int(products)
+    d.a, d.b, d.c = (float(x) for x in coeffs)
+    d.eps = float(eps)
+    return d
+
+
+def _stack_shape(t, name):
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name}: expected [rows, cols] or [batch, rows, cols], got {tuple(t.shape)}")
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+def spo_orthogonalize_workspace_bytes(batch, rows, cols, products=SPO_PRODUCTS_FP16) -> int:
+    return int(lib().spo_orthogonalize_workspace_bytes(C.byref(_orth_desc(batch, rows, cols, 5, NEWTON_SCHULZ, 0.0, products))))
+
+
+def spo_orthogonalize(G, out=None, out_dtype=None, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, products=SPO_PRODUCTS_FP16, workspace=None):
+    """G [rows, cols] or [batch, rows, cols], each row consecutive: returns each matrix's singular vectors with singular values
+    moved towards one, in out (contiguous) or a new tensor of out_dtype (G's)."""
+    batch, rows, cols = _stack_shape(G, "G")
+    if not G.is_cuda or G.dtype not in (torch.float32, torch.bfloat16) or (cols > 1 and G.stride(-1) != 1):
+        raise TypeError("G: expected a CUDA tensor of torch.float32 or torch.bfloat16 with consecutive rows")
+    stride = G.stride(-2) if rows > 1 else cols
+    step = G.stride(0) if G.dim() == 3 and batch > 1 else 0
+    if stride < cols or (batch > 1 and step < (rows - 1) * stride + cols):
+        raise TypeError("G: rows and matrices must not overlap")
+    if out is None:
+        out = torch.empty(G.shape, dtype=out_dtype or G.dtype, device=G.device)
+    else:
+        _want(out, out.dtype, "out", batch * rows * cols)
+    d = _orth_desc(batch, rows, cols, steps, coeffs, eps, products)
+    ws = _workspace(lib().spo_orthogonalize_workspace_bytes(C.byref(d)), G.device, workspace)
+    _check(lib().spo_orthogonalize(C.byref(d), _ptr(G), _dt(G.dtype), stride, step, _ptr(out), _dt(out.dtype), _ptr(ws), ws.numel(),
+                                   _stream()), "spo_orthogonalize")
+    return out
+
+
+def spo_muon_update(W, momentum, grad, lr, mu=0.95, nesterov=True, weight_decay=0.0, scale=None, steps=5, coeffs=NEWTON_SCHULZ,
+                    eps=1e-7, products=SPO_PRODUCTS_FP16, workspace=None):
+    """The momentum step, IN PLACE on W and momentum ([rows, cols] or [batch, rows, cols], contiguous).  scale: factor of
+    the orthogonalised update beside lr; None: sqrt(max(1, rows / cols))."""
+    batch, rows, cols = _stack_shape(W, "W")
+    n = batch * rows * cols
+    _want(W, W.dtype, "W")
+    _want(momentum, torch.float32, "momentum", n)
+    _want(grad, grad.dtype, "grad", n)
+    for t, name in ((W, "W"), (grad, "grad")):
+        if t.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16")
+    if scale is None:
+        scale = max(1.0, rows / cols) ** 0.5
+    d = _orth_desc(batch, rows, cols, steps, coeffs, eps, products)
+    ws = _workspace(lib().spo_orthogonalize_workspace_bytes(C.byref(d)), W.device, workspace)
+    _check(lib().spo_muon_update(C.byref(d), _ptr(W), _dt(W.dtype), _ptr(momentum), _ptr(grad), _dt(grad.dtype), float(mu),
+                                 int(bool(nesterov)), float(lr), float(weight_decay), float(scale), _ptr(ws), ws.numel(), _stream()),
+           "spo_muon_update")
