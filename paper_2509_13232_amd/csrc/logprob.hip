@@ -49,6 +49,17 @@ __device__ __forceinline__ void store_left_out(const ScoreOut &o, int64_t t) {
     if (o.entropy) o.entropy[t] = 0.0f;
 }
 
+// The lanes' running values joined, for every lane: one maximum, then one rescaling and the sums.
+__device__ __forceinline__ void join_lanes(float &m, float &s, float &u) {
+    float top = m;
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    const float d = fmaxf((m - top) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d);
+    u = wave_sum(f * fmaf(d, s, u));
+    s = wave_sum(s * f);
+    m = top;
+}
+
 // (max, sum of 2^x, sum of x 2^x) of one segment of a row by TR threads, a workgroup or one wavefront of it, and with Top each
 // thread's own maximum, group_max[row][segment * TR + thread].  Rows of one segment (whole) are finished here unless
 // alternatives are asked for.
@@ -96,9 +107,15 @@ score_rows_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, fl
 #pragma unroll
             for (int i = 0; i < N; ++i) mx = fmaxf(mx, x[u][i]);
         }
+        // What bounds rows of bf16 is this sum: besides the exponential (four operations' time) a logit takes half an operation
+        // for the maximum and one each for its value, exponent, sum and weighted sum.  The weighted sum goes without kLowest2:
+        // a NaN in it says that there was a logit of -inf (or a NaN), and then it is formed again with it.  (8192 rows of
+        // 151936: with kLowest2 for every logit 376 us, without 354.)
         const float nm2 = -mx * kLog2e;
         float a[U] = {}, w[U] = {};
-        auto add = [&](auto exponent) {
+        auto add = [&](auto exponent, auto bound) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) a[u] = w[u] = 0.0f;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (i0 + u * TR >= sp.nvec) break;
@@ -106,39 +123,30 @@ score_rows_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, fl
                 for (int i = 0; i < N; ++i) {
                     const float d = exponent(x[u][i]), e = __builtin_amdgcn_exp2f(d);
                     a[u] += e;
-                    w[u] = fmaf(e, fmaxf(d, kLowest2), w[u]);
+                    w[u] = fmaf(e, bound(d), w[u]);
                 }
             }
         };
-        if (__any(i0 < sp.nvec && fabsf(mx) > kFarLogit)) add([&](float v) { return (v - mx) * kLog2e; });
-        else add([&](float v) { return fmaf(v, kLog2e, nm2); });
+        const bool far = fabsf(mx) > kFarLogit;
+        if (!__any(i0 < sp.nvec && far)) add([&](float v) { return fmaf(v, kLog2e, nm2); }, [](float d) { return d; });
+        const float sum = (w[0] + w[1]) + (w[2] + w[3]);
+        if (__any(i0 < sp.nvec && (far || sum != sum)))
+            add([&](float v) { return (v - mx) * kLog2e; }, [](float d) { return fmaxf(d, kLowest2); });
         const float d = fmaxf((m - mx) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d);
         u2 = f * fmaf(d, s, u2) + ((w[0] + w[1]) + (w[2] + w[3]));
         s = s * f + ((a[0] + a[1]) + (a[2] + a[3]));
         m = mx;
     };
-    uint4 cur[U];
-    request(cur, tid);
-    if constexpr (Rounds > 1) {
-        uint4 nxt[U];
-        for (int i0 = tid; i0 < sp.nvec; i0 += U * TR) {
-            request(nxt, i0 + U * TR);
-            take(cur, i0);
-#pragma unroll
-            for (int u = 0; u < U; ++u) cur[u] = nxt[u];
-        }
-    } else {
-        take(cur, tid);
-    }
+    // a segment is at most Rounds rounds: all of it is requested at once
+    static_assert(Rounds <= 2, "two sets of registers");
+    uint4 first[U], second[U];
+    request(first, tid);
+    if constexpr (Rounds > 1) request(second, tid + U * TR);
+    take(first, tid);
+    if constexpr (Rounds > 1)
+        if (U * TR < sp.nvec) take(second, tid + U * TR);
     if constexpr (Top) group_max[(t * nseg + seg) * TR + tid] = m;
-    // one maximum for the wavefront, then one rescaling and the sums
-    float top = m;
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-    const float d = fmaxf((m - top) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d);
-    u2 = wave_sum(f * fmaf(d, s, u2));
-    s = wave_sum(s * f);
-    m = top;
+    join_lanes(m, s, u2);
     if constexpr (TR > kWave) {
         __shared__ float sm[TR / kWave], ss[TR / kWave], su[TR / kWave];
         const int wave = threadIdx.x >> 6;
@@ -164,14 +172,7 @@ __device__ __forceinline__ void join_segments(const float *__restrict__ part, in
         const float *q = part + (t * nseg + i) * 3;
         score_join(m, s, u, q[0], q[1], q[2]);
     }
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-        // (the lower lane's pair first, so that both lanes of a pair form the same sum)
-        const float om = __shfl_xor(m, o, kWave), os = __shfl_xor(s, o, kWave), ou = __shfl_xor(u, o, kWave);
-        float a = lane & o ? om : m, b = lane & o ? os : s, c = lane & o ? ou : u;
-        score_join(a, b, c, lane & o ? m : om, lane & o ? s : os, lane & o ? u : ou);
-        m = a; s = b; u = c;
-    }
+    join_lanes(m, s, u);
 }
 
 template <typename T>
@@ -207,24 +208,32 @@ __device__ __forceinline__ uint64_t order_of(float x, uint32_t id) { return stat
 constexpr int kPickThreads = 256;
 constexpr int kPickGroups = 512;             // groups of a row that are looked into at a time
 constexpr int kPickStep = kPickThreads * 8;  // logits of the step by step way
-constexpr int kPickRoom = kPickStep + SPO_MAX_TOP_K;
+constexpr int kPickRoom = kPickStep + SPO_MAX_TOP_K;  // a multiple of kRankStep
 
 // Places of cand[0..n) in their order, `put(place, candidate)` for each of the first K.  n <= kPickRoom; keys are distinct.
+// Counted kRankStep at a time (a read by itself takes as long as sixteen): the room behind the last candidate is filled up.
+constexpr int kRankStep = 8;
 template <typename F>
-__device__ __forceinline__ void rank_candidates(const uint64_t *cand, int n, int K, F put) {
+__device__ __forceinline__ void rank_candidates(uint64_t *cand, int n, int K, F put) {
+    if (threadIdx.x < kRankStep && n + threadIdx.x < kPickRoom) cand[n + threadIdx.x] = 0;  // behind every logit's number
+    __syncthreads();
     for (int i = threadIdx.x; i < n; i += kPickThreads) {
         const uint64_t mine = cand[i];
         int place = 0;
-        for (int j = 0; j < n; ++j) place += cand[j] > mine ? 1 : 0;
+        for (int j = 0; j < n; j += kRankStep)
+#pragma unroll
+            for (int k = 0; k < kRankStep; ++k) place += cand[j + k] > mine ? 1 : 0;
         if (place < K) put(place, mine);
     }
 }
 
 // One workgroup per row: joins its segments and finds its K largest logits.
 //   1. Every thread takes the maximum of its share of group_max; the K-th largest of these 256 maxima of disjoint sets bounds
-//      the K-th largest logit from below.
-//   2. The groups whose maximum reaches the bound, somewhat more than K, are looked into: a thread per vector of a group.
+//      the K-th largest logit from below, and few shares (K, and those that tie) reach it.
+//   2. The groups of these shares whose maximum reaches the bound, somewhat more than K, are looked into: a thread per vector.
 //   3. What reaches the bound is ranked by counting.
+// Bound by latency, of loads and of instructions not yet in a cache (one row of 151936 in bf16 with 20 alternatives: 16.8 us;
+// with loads eight at a time, a second look at these shares instead of all groups and one atomic per vector 7.2).
 // Rows with more ties at the bound than there is room, or with fewer groups than K, are walked step by step from the first
 // logit on, with the K best so far kept; later ones have to beat the last of these, so ties cost little after the first step.
 template <typename T, int TR>
@@ -232,10 +241,11 @@ __global__ void __launch_bounds__(kPickThreads)
 score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, const float *__restrict__ part,
                   const float *__restrict__ group_max, ScoreOut out) {
     constexpr int N = Vec<T>::N, VPG = kScoreGroup * kScoreRounds;  // vectors of a thread's group, at most
-    __shared__ float best[kPickThreads];
-    __shared__ uint64_t cand[kPickRoom], kept[SPO_MAX_TOP_K];
-    __shared__ int groups[kPickGroups];
-    __shared__ int n_cand, n_group;
+    __shared__ __attribute__((aligned(16))) float best[kPickThreads];
+    __shared__ __attribute__((aligned(16))) uint64_t cand[kPickRoom];
+    __shared__ uint64_t kept[SPO_MAX_TOP_K];
+    __shared__ int groups[kPickGroups], share[kPickThreads];
+    __shared__ int n_cand, n_group, n_share;
     __shared__ float bound, row_max, row_log;
     const int64_t t = flat_block();
     if (t >= rows.T) return;
@@ -251,11 +261,19 @@ score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, co
     const T *row = logits + t * rows.stride;
     const float *gm = group_max + t * nseg * TR;
     const int G = nseg * TR;
-    float mine = -INFINITY;
-    for (int g = tid; g < G; g += kPickThreads) mine = fmaxf(mine, gm[g]);
+    float mine = -INFINITY;  // share of thread i: groups i, i + 256, ...; eight on their way at a time
+    constexpr int U = 8;
+    for (int g0 = tid; g0 < G; g0 += U * kPickThreads) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = gm[g0 + u * kPickThreads < G ? g0 + u * kPickThreads : g0];
+#pragma unroll
+        for (int u = 0; u < U; ++u) mine = fmaxf(mine, x[u]);
+    }
     best[tid] = mine;
-    if (tid == 0) n_cand = n_group = 0;
-    if (tid < kWave) {  // meanwhile the first wavefront joins the segments
+    if (tid == 0) n_cand = n_group = n_share = 0;
+    __syncthreads();
+    if (tid < kWave) {  // the first wavefront joins the segments meanwhile
         float zt = 0.0f, m, s, u;
         if (tid == 0 && rows.target) zt = target_logit(row, rows, t);
         join_segments(part, nseg, t, m, s, u);
@@ -264,45 +282,68 @@ score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, co
             row_max = m;
             row_log = logf(s);
         }
+    } else if (tid < 2 * kWave) {
+        // The K-th largest by the second wavefront, bit by bit from the highest: the largest number that K of the 256 reach.
+        // (Every thread counting the larger ones: 1024 wavefront operations per compute unit, 2 us.)
+        uint32_t key[kPickThreads / kWave], kth = 0;
+#pragma unroll
+        for (int i = 0; i < kPickThreads / kWave; ++i) key[i] = order_key(best[i * kWave + tid - kWave]);
+#pragma unroll 4
+        for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+            int reach = 0;
+#pragma unroll
+            for (int i = 0; i < kPickThreads / kWave; ++i) reach += __popcll(__ballot(key[i] >= (kth | bit)));
+            if (reach >= K) kth |= bit;
+        }
+        if (tid == kWave) bound = order_value(kth);
     }
-    __syncthreads();
-    int place = 0;
-    for (int j = 0; j < kPickThreads; ++j) place += best[j] > mine || (best[j] == mine && j < tid) ? 1 : 0;
-    if (place == K - 1) bound = mine;
     __syncthreads();
     // the start of a maximum says nothing about a group (it may be empty, or all -inf)
     const float tau = bound;
     bool by_step = !(tau > kLowestFloat);
     if (!by_step) {
-        for (int g = tid; g < G; g += kPickThreads)
-            if (gm[g] >= tau) {
+        if (mine >= tau) share[atomicAdd(&n_share, 1)] = tid;
+        __syncthreads();
+        const int ns = n_share, items = ns * ((G + kPickThreads - 1) / kPickThreads);
+        for (int i = tid; i < items; i += kPickThreads) {
+            const int g = i / ns * kPickThreads + share[i % ns];
+            if (g < G && gm[g] >= tau) {
                 const int at = atomicAdd(&n_group, 1);
                 if (at < kPickGroups) groups[at] = g;
             }
+        }
         __syncthreads();
         const int ng = n_group;
         by_step = ng > kPickGroups;
         if (!by_step) {
-            auto offer = [&](float x, int64_t id) {
-                if (!(x >= tau)) return;
-                const int at = atomicAdd(&n_cand, 1);
-                if (at < kPickRoom) cand[at] = order_of(x, static_cast<uint32_t>(id));
-            };
             for (int i = tid; i < ng * (VPG + 1); i += kPickThreads) {
                 const int g = groups[i / (VPG + 1)], v = i % (VPG + 1), th = g % TR;
                 const int64_t e0 = (g / TR) * grid.seg_len;
                 const Span sp(row + e0, static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len));
-                if (v == VPG) {  // the thread's element outside the whole vectors
+                float x[N];
+                int first, count = 0;  // elements of the segment that x holds
+                if (v == VPG) {        // the thread's element outside the whole vectors
+                    first = th < sp.head ? th : th + sp.nvec * N;
                     if (th < sp.head + sp.tail) {
-                        const int64_t e = e0 + (th < sp.head ? th : th + sp.nvec * N);
-                        offer(Vec<T>::get(row + e), e);
+                        x[0] = Vec<T>::get(row + e0 + first);
+                        count = 1;
                     }
-                } else if (th + v * TR < sp.nvec) {
-                    const int64_t e = e0 + sp.head + (th + v * TR) * N;
-                    float x[N];
-                    Vec<T>::unpack(load16<false>(row + e), x);
+                } else {
+                    first = sp.head + (th + v * TR) * N;
+                    if (th + v * TR < sp.nvec) {
+                        Vec<T>::unpack(load16<false>(row + e0 + first), x);
+                        count = N;
+                    }
+                }
+                uint32_t reach = 0;
 #pragma unroll
-                    for (int j = 0; j < N; ++j) offer(x[j], e + j);
+                for (int j = 0; j < N; ++j) reach |= j < count && x[j] >= tau ? 1u << j : 0u;
+                if (!reach) continue;
+                const int at = atomicAdd(&n_cand, __popc(reach));
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const int place = at + __popc(reach & ((1u << j) - 1));
+                    if ((reach >> j & 1) && place < kPickRoom) cand[place] = order_of(x[j], static_cast<uint32_t>(e0 + first + j));
                 }
             }
             __syncthreads();
@@ -375,8 +416,8 @@ __device__ __forceinline__ void row_max_log(const T *row, int64_t V, float &m, f
     l = logf(s);
 }
 
-// One segment of a row of d_logits (at most kScoreGradGroup vectors per thread).  Rows that the mask leaves out or whose
-// factors are all zero are written as zeros without being read.  Vectors are aligned on the output side.
+// One segment of a row of d_logits (at most kScoreGradGroup vectors per thread).  Rows that the mask leaves out are not read;
+// they and rows whose factors are all zero are written as zeros.  Vectors are aligned on the output side.
 template <typename T, int TR, bool Stream>
 __global__ void __launch_bounds__(kRowThreads)
 score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, ScoreGrads gr, T *__restrict__ d_logits) {
@@ -390,87 +431,85 @@ score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, Sc
     T *out = d_logits + t * rows.V + e0;
     const int len = static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len);
     const Span sp(out, len);
-    T *body_out = out + sp.head;
-    uint4 *dst = reinterpret_cast<uint4 *>(body_out);
-    const bool left_out = rows.mask && !rows.mask[t];
-    float a = 0.0f, e = 0.0f, b = 0.0f;
-    int id = -1;  // lane k: the k-th alternative's place in the segment, and its factor
-    if (!left_out) {
-        if (gr.d_logp) a = gr.d_logp[t];
-        if (gr.d_entropy) e = gr.d_entropy[t];
-        if (gr.d_top && lane < gr.K) {
-            b = gr.d_top[t * gr.K + lane];
-            const int64_t at = static_cast<int64_t>(gr.top_id[t * gr.K + lane]) - e0;
-            id = at >= 0 && at < len ? static_cast<int>(at) : -1;
-        }
-    }
-    const float total = a + (gr.d_top ? wave_sum(b) : 0.0f);
-    uint64_t hot = gr.d_top ? __ballot(id >= 0 && b != 0.0f) : 0u;
-    // (b's of both signs may add up to zero)
-    const bool some = gr.d_top ? __any(b != 0.0f) : false;
-    if (left_out || (a == 0.0f && e == 0.0f && total == 0.0f && !some)) {
-        if (tid < sp.head + sp.tail) Vec<T>::put(out + (tid < sp.head ? tid : tid + sp.nvec * N), 0.0f);
+    uint4 *dst = reinterpret_cast<uint4 *>(out + sp.head);
+    const bool edge = tid < sp.head + sp.tail;
+    const int at_edge = tid < sp.head ? tid : tid + sp.nvec * N;
+    auto zeros = [&] {
+        if (edge) Vec<T>::put(out + at_edge, 0.0f);
         for (int i = tid; i < sp.nvec; i += TR) store16<Stream>(dst + i, make_uint4(0u, 0u, 0u, 0u));
-        return;
-    }
-    const float lse = gr.lse[t], nl = -lse * kLog2e;
-    const float c = -fmaf(e, e != 0.0f ? gr.entropy[t] : 0.0f, total), c2 = -e * kLn2;  // dz = p (c + c2 log2 p) + ...
-    // Beside a large log-sum-exp its rounding is no longer small (a row of 1e30: the logarithm of the sum is gone): such a
-    // row's own maximum and sum are formed again, by every segment.
-    const bool far = fabsf(lse) > kFarLogit;
-    float top = 0.0f, log_sum = 0.0f;
-    if (far) row_max_log<T, TR>(logits + t * rows.stride, rows.V, top, log_sum);
-    auto grad = [&](float x) {
-        const float d = far ? ((x - top) - log_sum) * kLog2e : fmaf(x, kLog2e, nl);
-        return __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, kLowest2), c2, c);
     };
-    int y = -1;
-    if (gr.d_logp && rows.target) {
-        const int64_t yl = static_cast<int64_t>(rows.target[t]) - e0;
-        y = yl >= 0 && yl < len ? static_cast<int>(yl) : -1;
-    }
-    // what element i of the segment gets beside its share of the softmax
-    auto extra = [&](int i, float v) {
-        if (i == y) v += a;
-        for (uint64_t h = hot; h; h &= h - 1) {
-            const int k = __builtin_ctzll(h);
-            if (i == __builtin_amdgcn_readlane(id, k)) v += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b), k));
-        }
-        return v;
-    };
-    {
-        const bool mine = tid < sp.head + sp.tail;
-        const int i = mine ? (tid < sp.head ? tid : tid + sp.nvec * N) : 0;
-        const float v = extra(i, grad(Vec<T>::get(p + i)));
-        if (mine) Vec<T>::put(out + i, v);
-    }
+    if (rows.mask && !rows.mask[t]) return zeros();
+    // everything is requested before any of it is looked at
     const T *body = p + sp.head;
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (tid + u * TR < sp.nvec) v[u] = load16<Stream>(body + (tid + u * TR) * N);
+    const T x_edge = edge ? p[at_edge] : T(0);  // (as it is: a conversion would wait for it here)
+    const float lse = gr.lse[t], a = gr.d_logp ? gr.d_logp[t] : 0.0f, e = gr.d_entropy ? gr.d_entropy[t] : 0.0f;
+    const float h = gr.d_entropy ? gr.entropy[t] : 0.0f;
+    const int64_t yl = gr.d_logp ? static_cast<int64_t>(rows.target[t]) - e0 : -1;
+    float total = a;
+    int id = -1;  // lane k: the k-th alternative's place in the segment, and its factor
+    float b = 0.0f;
+    uint64_t hot = 0;
+    bool some = false;
+    if (gr.d_top) {
+        if (lane < gr.K) {
+            b = gr.d_top[t * gr.K + lane];
+            const int64_t at = static_cast<int64_t>(gr.top_id[t * gr.K + lane]) - e0;
+            id = at >= 0 && at < len ? static_cast<int>(at) : -1;
+        }
+        hot = __ballot(id >= 0 && b != 0.0f);
+        some = __any(b != 0.0f);  // (factors of both signs may add up to zero)
+        total += wave_sum(b);
+    }
+    if (a == 0.0f && e == 0.0f && !some) return zeros();
+    const int y = yl >= 0 && yl < len ? static_cast<int>(yl) : -1;
+    const float c = -(e != 0.0f ? fmaf(e, h, total) : total), c2 = -e * kLn2;  // dz = p (c + c2 log2 p) + ...
+    auto finish = [&](auto exponent) {
+        auto grad = [&](float z) {
+            const float d = exponent(z);
+            return __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, kLowest2), c2, c);
+        };
+        auto of_hot = [&](auto add) {  // add(place, what is added there)
+            add(y, a);
+            for (uint64_t k = hot; k; k &= k - 1) {
+                const int l = __builtin_ctzll(k);
+                add(__builtin_amdgcn_readlane(id, l), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b), l)));
+            }
+        };
+        if (edge) {
+            float g = grad(Vec<T>::get(&x_edge));
+            of_hot([&](int place, float w) { g += place == at_edge ? w : 0.0f; });
+            Vec<T>::put(out + at_edge, g);
+        }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int iv = tid + u * TR;
-        const int first = sp.head + iv * N;
-        float x[N];
-        if (iv < sp.nvec) {
+        for (int u = 0; u < U; ++u) {
+            const int iv = tid + u * TR, first = sp.head + iv * N;
+            if (iv >= sp.nvec) break;
+            float x[N];
             Vec<T>::unpack(v[u], x);
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = grad(x[i]);
-        }
-        auto at = [&](int place, float add) {
-            if (static_cast<unsigned>(place - first) < static_cast<unsigned>(N))
+            of_hot([&](int place, float w) {
+                const int at = place - first;
+                if (static_cast<unsigned>(at) < static_cast<unsigned>(N))  // (no branches inside: they would put x into memory)
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (place - first == i) x[i] += add;
-        };
-        at(y, a);
-        for (uint64_t h = hot; h; h &= h - 1) {
-            const int k = __builtin_ctzll(h);
-            at(__builtin_amdgcn_readlane(id, k), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b), k)));
+                    for (int i = 0; i < N; ++i) x[i] += at == i ? w : 0.0f;
+            });
+            store16<Stream>(dst + iv, Vec<T>::pack(x));
         }
-        if (iv < sp.nvec) store16<Stream>(dst + iv, Vec<T>::pack(x));
+    };
+    // Beside a large log-sum-exp its rounding is no longer small (a row of 1e30: the logarithm of the sum is gone): such a
+    // row's own maximum and sum are formed again, by every segment.
+    if (fabsf(lse) > kFarLogit) {
+        float top, log_sum;
+        row_max_log<T, TR>(logits + t * rows.stride, rows.V, top, log_sum);
+        finish([&](float z) { return ((z - top) - log_sum) * kLog2e; });
+    } else {
+        const float nl = -lse * kLog2e;
+        finish([&](float z) { return fmaf(z, kLog2e, nl); });
     }
 }
 
