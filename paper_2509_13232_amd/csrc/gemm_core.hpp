@@ -207,7 +207,7 @@ struct Tile {
     // LDS -> fragments: READS reads per k-slice of 32.
     template <int EDGE, int F, bool Cols>
     struct Side {
-        static_assert(EDGE == 256 || EDGE == 128, "swizzle of columns along k");
+        static_assert(!Cols || EDGE == 256 || EDGE == 128, "swizzle of columns along k");
         static constexpr int CHUNKS = Cols ? EDGE * 2 / 16 : kChunks;  // 16-byte chunks per row of a stage
         static constexpr int ROWB = CHUNKS * 16;
         static constexpr int LOADS = EDGE * kChunks / NT;              // DMA instructions per thread and stage

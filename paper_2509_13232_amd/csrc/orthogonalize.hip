@@ -1,5 +1,6 @@
-// Orthogonalised updates: X <- U / |U|, then `steps` times A = X X^T, B = b A + c A A, X <- a X + B X (on the other side for
-// matrices with more rows than columns), and the momentum step around it.
+// Orthogonalised updates: X <- U / |U|, then `steps` times A = X X^T, B = b A + c A A, X <- a X + B X, and the momentum step
+// around it.  Matrices with more rows than columns are worked on transposed: on their way into X, and on their way out of the
+// last product.
 //
 // Numbers.  The products run on fp16 matrix instructions (the rate of bf16, three bits more): every operand is scaled by a
 // power of two to where fp16 is exact to 11 bits.  What this costs was found in 64 bits on gaussian, decaying and nearly
@@ -18,7 +19,9 @@
 
 namespace spo {
 
+// Tiles that the wavefronts of a workgroup share; symmetric products also take the middle ones.
 typedef Tile<256, 256, 2, 4, _Float16> OL;
+typedef Tile<192, 192, 4, 2, _Float16> OM;
 typedef Tile<128, 128, 2, 2, _Float16> OS;
 
 constexpr float kLoScale = 2048.0f;   // lo parts are held that much larger: as far above fp16's smallest numbers as hi parts
@@ -26,19 +29,20 @@ constexpr float kGramScale = 256.0f;  // A and B: their entries stay below about
 
 typedef uint16_t half_t;  // raw IEEE half bits
 
-__device__ __forceinline__ float half_value(uint32_t bits) { return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits))); }
-__device__ __forceinline__ uint32_t half_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v)); }
-
 // eight consecutive values of an output row, as the parts they are stored in
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 struct Eight {
     float v[8];
+    // (written so that a pair takes five instructions: one conversion, and a mixed multiply-add for each difference and lo part)
     __device__ __forceinline__ void split(uint4 &hi, uint4 &lo) const {
         uint32_t h[4], l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t h0 = half_bits(v[2 * i]), h1 = half_bits(v[2 * i + 1]);
-            h[i] = h0 | h1 << 16;
-            l[i] = half_bits((v[2 * i] - half_value(h0)) * kLoScale) | half_bits((v[2 * i + 1] - half_value(h1)) * kLoScale) << 16;
+            const f16x2_t p = __builtin_convertvector((f32x2_t{v[2 * i], v[2 * i + 1]}), f16x2_t);
+            const float a = fmaf(static_cast<float>(p.x), -1.0f, v[2 * i]), b = fmaf(static_cast<float>(p.y), -1.0f, v[2 * i + 1]);
+            const f16x2_t q = {static_cast<_Float16>(a * kLoScale), static_cast<_Float16>(b * kLoScale)};
+            h[i] = __builtin_bit_cast(uint32_t, p);
+            l[i] = __builtin_bit_cast(uint32_t, q);
         }
         hi = make_uint4(h[0], h[1], h[2], h[3]);
         lo = make_uint4(l[0], l[1], l[2], l[3]);
@@ -47,9 +51,10 @@ struct Eight {
     __device__ __forceinline__ void add(float beta, const uint4 &hi, const uint4 &lo) {
         const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int sh = 16 * (i & 1);
-            v[i] = fmaf(beta, fmaf(half_value(l[i / 2] >> sh & 0xffffu), 1.0f / kLoScale, half_value(h[i / 2] >> sh & 0xffffu)), v[i]);
+        for (int i = 0; i < 4; ++i) {
+            const f16x2_t p = __builtin_bit_cast(f16x2_t, h[i]), q = __builtin_bit_cast(f16x2_t, l[i]);
+            v[2 * i] = fmaf(beta, fmaf(static_cast<float>(q.x), 1.0f / kLoScale, static_cast<float>(p.x)), v[2 * i]);
+            v[2 * i + 1] = fmaf(beta, fmaf(static_cast<float>(q.y), 1.0f / kLoScale, static_cast<float>(p.y)), v[2 * i + 1]);
         }
     }
 };
@@ -64,7 +69,7 @@ struct Stack {
 // Where the last product goes: out = value, or the weights' update W = keep W - rate value.
 struct OrthOut {
     void *out;       // NULL: not the last product
-    int dtype, update;
+    int dtype, update, across;  // across: X is the output's transpose
     int64_t ld, step;
     float keep, rate;
 };
@@ -74,6 +79,7 @@ struct OrthProduct {
     int64_t M, N, Mp, Np; // true and padded sides of the output
     int64_t batch;
     int KT, split;        // split: products of pairs
+    int symmetric;        // only tiles on and below the diagonal are formed, each stored on both sides
     float alpha, beta;    // value = alpha * (A B) + beta * D
     int d_lo, out_lo;     // D has, the output gets, a lo plane
     OrthOut last;
@@ -133,10 +139,33 @@ __device__ __forceinline__ void store_values(void *p, int dtype, int64_t at, int
     }
 }
 
-// eight values of row m from column n on, on their way out of the last product
+// eight values of row m of X from column n on (N: X's columns), on their way out of the last product
 __device__ __forceinline__ void store_last(const OrthOut &o, int64_t matrix, int64_t m, int64_t n, int64_t N, Eight &e) {
     const int count = N - n < 8 ? static_cast<int>(N - n) : 8;
     if (count <= 0) return;
+    if (o.across) {  // (neighbouring lanes hold neighbouring m)
+        const int64_t first = matrix * o.step + n * o.ld + m;
+        if (o.dtype == SPO_FP32) {
+            float *q = static_cast<float *>(o.out) + first;
+            float w[8];
+            if (o.update)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = q[(i < count ? i : 0) * o.ld];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) q[i * o.ld] = o.update ? fmaf(-o.rate, e.v[i], o.keep * w[i]) : e.v[i];
+        } else {
+            bf16_t *q = static_cast<bf16_t *>(o.out) + first;
+            bf16_t w[8];
+            if (o.update)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = q[(i < count ? i : 0) * o.ld];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) q[i * o.ld] = f32_to_bf16(o.update ? fmaf(-o.rate, e.v[i], o.keep * bf16_to_f32(w[i])) : e.v[i]);
+        }
+        return;
+    }
     const int64_t at = matrix * o.step + m * o.ld + n;
     if (o.update) {
         float w[8];
@@ -147,56 +176,195 @@ __device__ __forceinline__ void store_last(const OrthOut &o, int64_t matrix, int
     store_values(o.out, o.dtype, at, count, e.v);
 }
 
-template <typename TT>
-__device__ __forceinline__ void store_product(typename TT::Acc &acc, const OrthProduct &p, int64_t matrix, int64_t m0, int64_t n0) {
+// The tiles of a product in the order of their ids: those of TileOrder, or of a symmetric product (n x n tiles) the rows of the
+// lower triangle one after the other.
+struct OrthTiles {
+    int64_t nM, nN;
+    bool symmetric;
+    __host__ __device__ OrthTiles(int64_t M, int64_t N, int64_t edge, bool sym) : nM(ceil_div(M, edge)), nN(ceil_div(N, edge)), symmetric(sym) {}
+    __host__ __device__ int64_t tiles() const { return symmetric ? nM * (nM + 1) / 2 : nM * nN; }
+    __device__ __forceinline__ void at(uint32_t i, int64_t &tm, int64_t &tn) const {
+        if (!symmetric) return TileOrder(nM, nN).at(i, tm, tn);
+        uint32_t r = static_cast<uint32_t>((sqrtf(8.0f * static_cast<float>(i) + 1.0f) - 1.0f) * 0.5f);  // to one off
+        while (r * (r + 1) / 2 > i) --r;
+        while ((r + 1) * (r + 2) / 2 <= i) ++r;
+        tm = r;
+        tn = i - r * (r + 1) / 2;
+    }
+};
+
+// beta D added to eight values of row m from column n on
+__device__ __forceinline__ void add_addend(const OrthProduct &p, const half_t *d, int64_t m, int64_t n, Eight &e) {
+    if (!d) return;
+    const uint4 hi = *reinterpret_cast<const uint4 *>(d + m * p.d.ld + n);
+    const uint4 lo = p.d_lo ? *reinterpret_cast<const uint4 *>(d + p.d.plane + m * p.d.ld + n) : make_uint4(0u, 0u, 0u, 0u);
+    e.add(p.beta, hi, lo);
+}
+__device__ __forceinline__ void clear_padding(const OrthProduct &p, int64_t m, int64_t n, Eight &e) {
+    if (m < p.M && n + 8 <= p.N) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (m >= p.M || n + k >= p.N) e.v[k] = 0.0f;
+}
+
+template <typename TT> constexpr int kTurnPitch = TT::BM + 8;  // halves
+template <typename TT> constexpr int kOrthLds = TT::LDS_BYTES > TT::BN * kTurnPitch<TT> * 2 ? TT::LDS_BYTES : TT::BN * kTurnPitch<TT> * 2;
+
+// A finished tile, straight from the accumulators; of a symmetric product also its mirror image, which is turned in LDS, a
+// plane at a time (Plane: 0 the hi parts and all that goes straight out, 1 the mirror image's lo parts).
+template <typename TT, int Plane, bool Mirror>
+__device__ __forceinline__ void store_product(typename TT::Acc &acc, const OrthProduct &p, int64_t matrix, int64_t m0, int64_t n0, char *lds) {
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));  // not to be traced: nothing derived from it is to live through the main loop
     const int grp = lane >> 4, col = lane & 15;
-    const half_t *d = p.d.base ? p.d.of(matrix) : nullptr;
-    half_t *out = p.out.base ? p.out.of(matrix) : nullptr;
+    const bool mirror = Mirror && p.symmetric && m0 != n0;
+    if (Plane == 1 && !mirror) return;
+    // places inside the tile: in 32 bits (rows are at most 65600 halves)
+    const int d_ld = static_cast<int>(p.d.ld), out_ld = static_cast<int>(p.out.ld);
+    const half_t *d = p.d.base ? p.d.of(matrix) + m0 * p.d.ld + n0 : nullptr, *d_lo_plane = d + p.d.plane;
+    half_t *out = p.out.of(matrix) + m0 * p.out.ld + n0, *out_lo_plane = out + p.out.plane;
+    const int rows = static_cast<int>(p.M - m0), cols = static_cast<int>(p.N - n0);            // true sides, from the tile's corner
+    const int rows_p = static_cast<int>(p.Mp - m0), cols_p = static_cast<int>(p.Np - n0);      // padded ones, multiples of 64
+    half_t *turn = reinterpret_cast<half_t *>(lds);
+    // The addend of the next sixteen rows is requested before this sixteen are worked on.
+    constexpr int C = TT::FN / 2;
+    uint4 d_hi[2][C], d_lo[2][C];
+    auto row = [&](int i) { return TT::wave_m0() + i * TT::MI + col; };
+    auto column = [&](int j) { return TT::wave_n0() + 2 * j * TT::MI + (grp & 1) * TT::MI + (grp & 2) * 4; };
+    auto request = [&](int i) {
+        const int m = row(i);
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const int n = column(j), at = (m < rows_p ? m : 0) * d_ld + (n < cols_p ? n : 0);  // always a load
+            d_hi[i & 1][j] = *reinterpret_cast<const uint4 *>(d + at);
+            d_lo[i & 1][j] = p.d_lo ? *reinterpret_cast<const uint4 *>(d_lo_plane + at) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    };
+    if (d) request(0);
+    if (mirror) __syncthreads();  // operands, or the other plane, are no longer read
+    const bool inside = TT::wave_m0() + TT::WM <= rows && TT::wave_n0() + TT::WN <= cols;  // of the wavefront's part, all
 #pragma unroll
     for (int i = 0; i < TT::FM; ++i) {
-        const int64_t m = m0 + TT::wave_m0() + i * TT::MI + col;
+        if (d && i + 1 < TT::FM) request(i + 1);
 #pragma unroll
-        for (int j = 0; j < TT::FN; j += 2) {
+        for (int j = 0; j < C; ++j) {
             // after an exchange between neighbouring lane groups a lane holds eight consecutive columns of its row
             Eight e;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                uint32_t x = __float_as_uint(acc[i][j][r]), y = __float_as_uint(acc[i][j + 1][r]);
+                uint32_t x = __float_as_uint(acc[i][2 * j][r]), y = __float_as_uint(acc[i][2 * j + 1][r]);
                 swap_lane_groups(x, y);
                 e.v[r] = __uint_as_float(x) * p.alpha;
                 e.v[4 + r] = __uint_as_float(y) * p.alpha;
             }
-            const int64_t n = n0 + TT::wave_n0() + j * TT::MI + (grp & 1) * TT::MI + (grp & 2) * 4;
-            if (m >= p.Mp || n >= p.Np) continue;
-            if (d) {
-                const uint4 hi = *reinterpret_cast<const uint4 *>(d + m * p.d.ld + n);
-                const uint4 lo = p.d_lo ? *reinterpret_cast<const uint4 *>(d + p.d.plane + m * p.d.ld + n) : make_uint4(0u, 0u, 0u, 0u);
-                e.add(p.beta, hi, lo);
-            }
-            if (p.last.out) {
-                if (m < p.M) store_last(p.last, matrix, m, n, p.N, e);
-                continue;
-            }
+            const int m = row(i), n = column(j);
+            if (d) e.add(p.beta, d_hi[i & 1][j], d_lo[i & 1][j]);
+            if (!inside)
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (m >= p.M || n + k >= p.N) e.v[k] = 0.0f;
+                for (int k = 0; k < 8; ++k) e.v[k] = m < rows && n + k < cols ? e.v[k] : 0.0f;
             uint4 hi, lo;
             e.split(hi, lo);
-            *reinterpret_cast<uint4 *>(out + m * p.out.ld + n) = hi;
-            if (p.out_lo) *reinterpret_cast<uint4 *>(out + p.out.plane + m * p.out.ld + n) = lo;
+            if (inside || (m < rows_p && n < cols_p)) {
+                if (Plane == 0) {
+                    *reinterpret_cast<uint4 *>(out + (m * out_ld + n)) = hi;
+                    if (p.out_lo) *reinterpret_cast<uint4 *>(out_lo_plane + (m * out_ld + n)) = lo;
+                }
+                if (mirror) {
+                    const uint4 q = Plane ? lo : hi;
+                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) turn[(n + k) * kTurnPitch<TT> + m] = static_cast<half_t>(w[k / 2] >> (16 * (k & 1)));
+                }
+            }
         }
+    }
+    if (!mirror) return;
+    __syncthreads();
+    half_t *image = p.out.of(matrix) + n0 * p.out.ld + m0 + Plane * p.out.plane;
+    for (int i = threadIdx.x; i < TT::BN * TT::BM / 8; i += TT::NT) {
+        const int r = i / (TT::BM / 8), c = i % (TT::BM / 8) * 8;
+        if (r < cols_p && c < rows_p)
+            *reinterpret_cast<uint4 *>(image + (r * out_ld + c)) = *reinterpret_cast<const uint4 *>(turn + r * kTurnPitch<TT> + c);
     }
 }
 
-// value = alpha * sum_k A(m,k) B(n,k) + beta * D for every matrix of a stack.  ACols, BCols: the operand has the contraction
-// index as its row index.
-template <typename TT, bool ACols, bool BCols, bool Split>
+// A finished tile of the last product: a wavefront's part in LDS, 64 rows at a time, and from there in whole lines of the
+// output's rows, whichever way these run.  (Out of the accumulators this code, once per block, spilled all of them.)
+constexpr int kLastPitch = 64 + 4;  // floats
+template <typename TT> constexpr int kLastLds = TT::NWAVE * 64 * kLastPitch * 4;
+template <typename TT>
+__device__ __forceinline__ void store_last_product(const typename TT::Acc &acc, const OrthProduct &p, int64_t matrix, int64_t m0, int64_t n0,
+                                                   char *lds) {
+    static_assert(TT::WN == 64 && TT::WM % 64 == 0, "parts of 64 x 64");
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    float *part = reinterpret_cast<float *>(lds) + TT::wave_id() * 64 * kLastPitch;
+    const half_t *d = p.d.of(matrix);
+    __syncthreads();  // operands are no longer read; from here on every wavefront by itself
+#pragma unroll
+    for (int half = 0; half < TT::WM / 64; ++half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < TT::FN; ++j)
+                *reinterpret_cast<f32x4_t *>(part + (i * 16 + (lane & 15)) * kLastPitch + j * 16 + 4 * (lane >> 4)) = acc[half * 4 + i][j];
+        __builtin_amdgcn_wave_barrier();
+        const int64_t mp = m0 + TT::wave_m0() + half * 64, np = n0 + TT::wave_n0();
+        constexpr int U = 2;  // runs of eight values per lane that are worked on at a time, their loads together
+        for (int u0 = lane; u0 < 64 * 64 / 8; u0 += U * kWave) {
+            uint4 hi[U], lo[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int u = u0 + i * kWave;
+                const int64_t m = mp + u / 8, n = np + u % 8 * 8;
+                const half_t *q = d + (m < p.Mp ? m : p.Mp - 1) * p.d.ld + (n < p.Np ? n : p.Np - 8);
+                hi[i] = *reinterpret_cast<const uint4 *>(q);
+                lo[i] = *reinterpret_cast<const uint4 *>(q + p.d.plane);
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int u = u0 + i * kWave, r = u / 8, c = u % 8 * 8;
+                f32x4_t *q = reinterpret_cast<f32x4_t *>(part + r * kLastPitch + c);
+                const f32x4_t x = q[0], y = q[1];
+                Eight e;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    e.v[k] = x[k] * p.alpha;
+                    e.v[4 + k] = y[k] * p.alpha;
+                }
+                e.add(p.beta, hi[i], lo[i]);
+                if (p.last.across) {
+                    q[0] = f32x4_t{e.v[0], e.v[1], e.v[2], e.v[3]};
+                    q[1] = f32x4_t{e.v[4], e.v[5], e.v[6], e.v[7]};
+                } else if (mp + r < p.M) {
+                    store_last(p.last, matrix, mp + r, np + c, p.N, e);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (p.last.across && mp + lane < p.M)  // a row per lane: whole lines of the output's rows
+            for (int c = 0; c < 64; c += 8) {
+                const f32x4_t *q = reinterpret_cast<const f32x4_t *>(part + lane * kLastPitch + c);
+                const f32x4_t x = q[0], y = q[1];
+                Eight e;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    e.v[k] = x[k];
+                    e.v[4 + k] = y[k];
+                }
+                store_last(p.last, matrix, mp + lane, np + c, p.N, e);
+            }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// value = alpha * sum_k A(m,k) B(n,k) + beta * D for every matrix of a stack; rows of A lie along k, those of B too or
+// (BCols) its columns.
+template <typename TT, bool BCols, bool Split, bool Last>
 __global__ void __launch_bounds__(TT::NT, 2)
 orth_product_kernel(OrthProduct p) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const TileOrder ord(ceil_div(p.Mp, TT::BM), ceil_div(p.Np, TT::BN));
+    const OrthTiles ord(p.Mp, p.Np, TT::BM, p.symmetric);
     const uint32_t tiles = static_cast<uint32_t>(ord.tiles());
     uint32_t i;
     if (!TileOrder::item(blockIdx.x, static_cast<uint32_t>(tiles * p.batch), i)) return;
@@ -210,15 +378,192 @@ orth_product_kernel(OrthProduct p) {
     typename TT::Acc acc;
     TT::zero(acc);
     if constexpr (Split) {
-        TT::template mainloop<ACols, BCols, true>(A(0), B(1), p.KT, lds, acc);
-        TT::template mainloop<ACols, BCols, true>(A(1), B(0), p.KT, lds, acc);
+        TT::template mainloop<false, BCols, true>(A(0), B(1), p.KT, lds, acc);
+        TT::template mainloop<false, BCols, true>(A(1), B(0), p.KT, lds, acc);
 #pragma unroll
         for (int x = 0; x < TT::FM; ++x)
 #pragma unroll
             for (int y = 0; y < TT::FN; ++y) acc[x][y] *= 1.0f / kLoScale;
     }
-    TT::template mainloop<ACols, BCols, true>(A(0), B(0), p.KT, lds, acc);
-    store_product<TT>(acc, p, matrix, m0, n0);
+    TT::template mainloop<false, BCols, true>(A(0), B(0), p.KT, lds, acc);
+    if constexpr (Last) return store_last_product<TT>(acc, p, matrix, m0, n0, lds);
+    // (symmetric products have both operands along k)
+    store_product<TT, 0, !BCols>(acc, p, matrix, m0, n0, lds);
+    if constexpr (Split && !BCols) store_product<TT, 1, true>(acc, p, matrix, m0, n0, lds);
+}
+
+// ----------------------------------------------------------------------------
+// products with few tiles: every wavefront its own share of the contraction
+// ----------------------------------------------------------------------------
+// Tiles of 64 x 64, four wavefronts, each of which forms the whole tile over every fourth step of 64; their sums are added in
+// order at the end.  What bounds a small product is the way of its operands: a step of the main loop above cannot be
+// shorter than one round trip to the L2s (0.57 us), here each wavefront has a stage of its own, waits for nobody, and eight
+// steps are on their way per compute unit (two workgroups; with two stages per wavefront and one workgroup no product was
+// faster); a wavefront reads 16 KB of LDS per 32 matrix instructions (tiles shared between wavefronts: twice that).  The sides of all matrices are multiples of 64, so nothing here has an end to look after.
+constexpr int kFewEdge = 64, kFewWaves = 4, kFewThreads = kFewWaves * kWave;
+constexpr int kFewStage = 2 * kFewEdge * kRowBytes;  // bytes: 64 rows of both operands
+constexpr int kFewPitch = kFewEdge + 4;              // floats, of a wavefront's sums
+constexpr int kFewLds = kFewWaves * (kFewStage > kFewEdge * kFewPitch * 4 ? kFewStage : kFewEdge * kFewPitch * 4);
+
+template <bool BCols>
+__global__ void __launch_bounds__(kFewThreads, 2)
+orth_few_kernel(OrthProduct p) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    typedef Tile<256, 256, 2, 4, _Float16> T;  // its transfers and instruction
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef short v8s __attribute__((ext_vector_type(8)));
+    constexpr int E = kFewEdge, F = E / 16, ROWS = kRowBytes;
+    const OrthTiles ord(p.Mp, p.Np, E, p.symmetric);
+    const uint32_t tiles = static_cast<uint32_t>(ord.tiles());
+    uint32_t item;
+    if (!TileOrder::item(blockIdx.x, static_cast<uint32_t>(tiles * p.batch), item)) return;
+    const int64_t matrix = item / tiles;
+    int64_t tm, tn;
+    ord.at(item % tiles, tm, tn);
+    const int64_t m0 = tm * E, n0 = tn * E;
+    const int lane = threadIdx.x & 63, wave = T::wave_id();
+
+    // transfers: instruction i of an operand brings rows 8 i .. 8 i + 7 of its stage, lane l the chunk that belongs at its place
+    const int64_t lda = p.a.ld * 2, ldb = p.b.ld * 2;
+    const char *a = reinterpret_cast<const char *>(p.a.of(matrix)) + m0 * lda;
+    const char *b = reinterpret_cast<const char *>(p.b.of(matrix)) + (BCols ? n0 * 2 : n0 * ldb);
+    const int64_t step_a = ROWS, step_b = BCols ? E * ldb : ROWS;
+    const uint32_t ring = T::lds_address(lds) + wave * kFewStage;
+    auto cols_swizzle = [](int r) { return (r & 3) << 1; };  // columns along k: pieces of four rows on distinct banks
+    uint32_t off_a[2], off_b[2];  // of rows 0..7 and 8..15 of sixteen
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = 8 * h + (lane >> 3), c = lane & 7;
+        off_a[h] = static_cast<uint32_t>((lane >> 3) * lda) + static_cast<uint32_t>((c ^ swz(r)) * 16);
+        off_b[h] = static_cast<uint32_t>((lane >> 3) * ldb) + static_cast<uint32_t>((c ^ (BCols ? cols_swizzle(r) : swz(r))) * 16);
+    }
+    // step j of this wavefront: with pairs first all hi lo, then all lo hi, then all hi hi
+    const int mine = (p.KT - wave + kFewWaves - 1) / kFewWaves, terms = p.split ? 3 : 1, total = mine * terms;
+    auto request = [&](int j) {
+        const int term = p.split ? j / mine : 2, kt = wave + kFewWaves * (j - (p.split ? term * mine : 0));
+        const char *ga = T::uniform(a + (term == 1 ? p.a.plane * 2 : 0) + kt * step_a);
+        const char *gb = T::uniform(b + (term == 0 ? p.b.plane * 2 : 0) + kt * step_b);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(ring);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) T::dma(ga + i * 8 * lda, off_a[i & 1], to + i * 1024);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) T::dma(gb + i * 8 * ldb, off_b[i & 1], to + E * ROWS + i * 1024);
+    };
+    typename T::AccBlock acc[F][F];
+#pragma unroll
+    for (int x = 0; x < F; ++x)
+#pragma unroll
+        for (int y = 0; y < F; ++y) acc[x][y] = typename T::AccBlock{0.0f, 0.0f, 0.0f, 0.0f};
+    if (total > 0) request(0);
+    for (int j = 0; j < total; ++j) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const char *stage = lds + wave * kFewStage;
+        bf16x8_t fa[2][F], fb[2][F];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            const int chunk = ((4 * kk + (lane >> 4)) ^ swz(lane & 15)) * 16 + (lane & 15) * ROWS;
+#pragma unroll
+            for (int f = 0; f < F; ++f) fa[kk][f] = *reinterpret_cast<const bf16x8_t *>(stage + f * 16 * ROWS + chunk);
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                if constexpr (BCols) {  // see Tile::Side
+                    const int row = 32 * kk + 8 * (lane >> 4) + ((lane & 15) >> 2), col = f * 16 + 4 * (lane & 3);
+                    const uint32_t at = T::lds_address(stage) + E * ROWS + row * ROWS + (((col >> 3) ^ cols_swizzle(row)) << 4) + ((col >> 2) & 1) * 8;
+                    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(uintptr_t)at);
+                    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(uintptr_t)(at + 4 * ROWS));
+                    fb[kk][f] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                } else {
+                    fb[kk][f] = *reinterpret_cast<const bf16x8_t *>(stage + E * ROWS + f * 16 * ROWS + chunk);
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage is in registers: its place may be written
+        __builtin_amdgcn_sched_barrier(0);
+        if (j + 1 < total) request(j + 1);
+        if (p.split && j == 2 * mine)
+#pragma unroll
+            for (int x = 0; x < F; ++x)
+#pragma unroll
+                for (int y = 0; y < F; ++y) acc[x][y] *= 1.0f / kLoScale;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int x = 0; x < F; ++x)
+#pragma unroll
+                for (int y = 0; y < F; ++y) acc[x][y] = T::template mfma<true>(fa[kk][x], fb[kk][y], acc[x][y]);
+    }
+    // the wavefronts' sums in LDS: lane l holds row l % 16 and columns 4 (l / 16) .. of a block
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int x = 0; x < F; ++x)
+#pragma unroll
+        for (int y = 0; y < F; ++y)
+            *reinterpret_cast<f32x4_t *>(sums + (wave * E + x * 16 + (lane & 15)) * kFewPitch + y * 16 + 4 * (lane >> 4)) = acc[x][y];
+    __syncthreads();
+    const half_t *d = p.d.base ? p.d.of(matrix) : nullptr;
+    half_t *out = p.out.base ? p.out.of(matrix) : nullptr;
+    const bool mirror = p.symmetric && m0 != n0;
+    constexpr int U = E * E / 8 / kFewThreads;  // runs of eight values per thread
+    uint4 hi[U], lo[U];
+    int row[U], at[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int u = i * kFewThreads + threadIdx.x;
+        // (values that go out across: neighbouring lanes on neighbouring rows)
+        const int r = row[i] = p.last.across ? u % E : u / (E / 8), c = at[i] = (p.last.across ? u / E : u % (E / 8)) * 8;
+        Eight e;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e.v[k] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) {
+            const f32x4_t *q = reinterpret_cast<const f32x4_t *>(sums + (w * E + r) * kFewPitch + c);
+            const f32x4_t x = q[0], y = q[1];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                e.v[k] += x[k];
+                e.v[4 + k] += y[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e.v[k] *= p.alpha;
+        const int64_t m = m0 + r, n = n0 + c;
+        add_addend(p, d, m, n, e);
+        if (p.last.out) {
+            if (m < p.M) store_last(p.last, matrix, m, n, p.N, e);
+            continue;
+        }
+        clear_padding(p, m, n, e);
+        e.split(hi[i], lo[i]);
+        *reinterpret_cast<uint4 *>(out + m * p.out.ld + n) = hi[i];
+        if (p.out_lo) *reinterpret_cast<uint4 *>(out + p.out.plane + m * p.out.ld + n) = lo[i];
+    }
+    if (!mirror) return;
+    // the mirror image, turned in LDS (a pitch of 33 words: the writes of a wavefront on 32 different banks)
+    constexpr int P = E + 2;
+    half_t *turn = reinterpret_cast<half_t *>(lds);
+    __syncthreads();  // the sums are no longer read
+#pragma unroll
+    for (int plane = 0; plane < 2; ++plane) {
+        if (plane && !p.out_lo) break;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const uint4 q = plane ? lo[i] : hi[i];
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) turn[(plane * E + at[i] + k) * P + row[i]] = static_cast<half_t>(w[k / 2] >> (16 * (k & 1)));
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int plane = 0; plane < 2; ++plane) {
+        if (plane && !p.out_lo) break;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const uint32_t *q = reinterpret_cast<const uint32_t *>(turn + (plane * E + row[i]) * P + at[i]);
+            *reinterpret_cast<uint4 *>(out + plane * p.out.plane + (n0 + row[i]) * p.out.ld + m0 + at[i]) = make_uint4(q[0], q[1], q[2], q[3]);
+        }
+    }
 }
 
 // ----------------------------------------------------------------------------
@@ -234,7 +579,7 @@ struct OrthInput {
     int64_t rows, cols;
     float eps;
 };
-constexpr int kNormParts = 256;  // most workgroups per matrix, and threads that join their sums
+constexpr int kNormParts = 1024;  // most workgroups per matrix; 256 threads join their sums
 
 // U of eight entries from column c on; First: M <- mu M + G on the way (otherwise M is as it was left by that)
 template <bool First>
@@ -259,6 +604,7 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(OrthInput in, double *__
     __shared__ double scratch[4];
     const int64_t matrix = blockIdx.y, per_row = ceil_div(in.cols, 8), n = in.rows * per_row;
     double sum = 0.0;
+#pragma unroll 2
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
         float u[8], s = 0.0f;
         load_update<true>(in, matrix, i / per_row, i % per_row * 8, u);
@@ -270,14 +616,21 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(OrthInput in, double *__
     if (threadIdx.x == 0) part[matrix * gridDim.x + blockIdx.x] = sum;
 }
 
+// scale / (|U| + eps), and 0 for a matrix of zeros; by a whole workgroup
+__device__ __forceinline__ float scale_of(const OrthInput &in, const double *part, int parts, int64_t matrix, float scale, double *scratch) {
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 256) sum += part[matrix * parts + i];
+    const double norm = sqrt(block_sum(sum, scratch));
+    const double whole = norm + static_cast<double>(in.eps);
+    return whole > 0.0 ? static_cast<float>(scale / whole) : whole == 0.0 ? 0.0f : __builtin_nanf("");
+}
+
 // X = scale * U / (|U| + eps) as pairs of halves, zero in the padding; with last.out: U / (|U| + eps) goes there (no steps)
 __global__ void __launch_bounds__(256) orth_scale_kernel(OrthInput in, const double *__restrict__ part, int parts, float scale, Stack X,
                                                          int64_t rows_p, OrthOut last) {
     __shared__ double scratch[4];
     const int64_t matrix = blockIdx.y;
-    const double norm = sqrt(block_sum(static_cast<int>(threadIdx.x) < parts ? part[matrix * parts + threadIdx.x] : 0.0, scratch));
-    const double whole = norm + static_cast<double>(in.eps);
-    const float f = whole > 0.0 ? static_cast<float>((last.out ? 1.0 : scale) / whole) : whole == 0.0 ? 0.0f : __builtin_nanf("");
+    const float f = scale_of(in, part, parts, matrix, last.out ? 1.0f : scale, scratch);
     const int64_t per_row = X.ld / 8, n = rows_p * per_row;
     half_t *x = X.of(matrix);
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
@@ -302,13 +655,44 @@ __global__ void __launch_bounds__(256) orth_scale_kernel(OrthInput in, const dou
     }
 }
 
+// The same for matrices with more rows than columns: X gets their transpose, 64 x 64 entries by a workgroup through LDS.
+__global__ void __launch_bounds__(256) orth_scale_turned_kernel(OrthInput in, const double *__restrict__ part, int parts, float scale, Stack X,
+                                                                unsigned across) {
+    __shared__ double scratch[4];
+    __shared__ float turn[64][65];
+    const int64_t matrix = blockIdx.y;
+    const float f = scale_of(in, part, parts, matrix, scale, scratch);
+    const int64_t r0 = blockIdx.x % across * 64, c0 = blockIdx.x / across * 64;  // of U; across: tiles along X's rows
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int u = i * 256 + threadIdx.x, r = u / 8, c = u % 8 * 8;
+        float v[8] = {};
+        if (r0 + r < in.rows && c0 + c < in.cols) load_update<false>(in, matrix, r0 + r, c0 + c, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) turn[r][c + k] = v[k] * f;
+    }
+    __syncthreads();
+    half_t *x = X.of(matrix);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int u = i * 256 + threadIdx.x, r = u / 8, c = u % 8 * 8;  // of X
+        Eight e;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e.v[k] = turn[c + k][r];
+        uint4 hi, lo;
+        e.split(hi, lo);
+        *reinterpret_cast<uint4 *>(x + (c0 + r) * X.ld + r0 + c) = hi;
+        *reinterpret_cast<uint4 *>(x + X.plane + (c0 + r) * X.ld + r0 + c) = lo;
+    }
+}
+
 // ----------------------------------------------------------------------------
 // host side
 // ----------------------------------------------------------------------------
 static int64_t padded(int64_t n) { return ceil_div(n, kBK) * kBK; }
 
 struct OrthPlan {
-    int64_t rp, cp, k, kp;  // padded sides, the smaller side and the same padded
+    int64_t k, L, kp, Lp;  // the smaller and the larger side, and both padded: X is k x L
     int parts;
     double *norm;
     Stack X[2], A, B;
@@ -318,15 +702,15 @@ struct OrthPlan {
 
 static OrthPlan plan_orth(const spo_orth_desc *d, void *ws) {
     OrthPlan p;
-    p.rp = padded(d->rows);
-    p.cp = padded(d->cols);
     p.k = std::min(d->rows, d->cols);
+    p.L = std::max(d->rows, d->cols);
     p.kp = padded(p.k);
+    p.Lp = padded(p.L);
     // X's entries are about 1 / sqrt(longer side) once its singular values are near one
     p.x_scale = 1.0f;
-    for (int64_t n = std::max(d->rows, d->cols); n > 1; n /= 4) p.x_scale *= 2.0f;
+    for (int64_t n = p.L; n > 1; n /= 4) p.x_scale *= 2.0f;
     const int64_t vectors = d->rows * ceil_div(d->cols, 8);
-    p.parts = static_cast<int>(std::min<int64_t>(kNormParts, ceil_div(vectors, 256 * 4)));
+    p.parts = static_cast<int>(std::min<int64_t>(kNormParts, ceil_div(vectors, 256 * 2)));
     Arena a(ws);
     p.norm = a.take<double>(static_cast<size_t>(d->batch) * kNormParts);
     auto stack = [&](int64_t rows, int64_t ld) {
@@ -334,71 +718,141 @@ static OrthPlan plan_orth(const spo_orth_desc *d, void *ws) {
         s.base = a.take<half_t>(static_cast<size_t>(d->batch) * 2 * rows * ld);
         return s;
     };
-    p.X[0] = stack(p.rp, p.cp);
-    p.X[1] = stack(p.rp, p.cp);
+    p.X[0] = stack(p.kp, p.Lp);
+    p.X[1] = stack(p.kp, p.Lp);
     p.A = stack(p.kp, p.kp);
     p.B = stack(p.kp, p.kp);
     p.bytes = a.used;
     return p;
 }
 
-template <typename TT, bool ACols, bool BCols, bool Split>
-static int launch_product(const OrthProduct &p, hipStream_t s) {
-    auto *kernel = orth_product_kernel<TT, ACols, BCols, Split>;
-    if (int rc = allow_lds(kernel, TT::LDS_BYTES)) return rc;
-    const int64_t items = ceil_div(p.Mp, TT::BM) * ceil_div(p.Np, TT::BN) * p.batch;
-    kernel<<<static_cast<unsigned>(TileOrder::blocks(items)), TT::NT, TT::LDS_BYTES, s>>>(p);
+template <typename TT, bool BCols, bool Split>
+static int launch_tiles(const OrthProduct &p, hipStream_t s) {
+    auto *kernel = orth_product_kernel<TT, BCols, Split, false>;
+    int lds = kOrthLds<TT>;
+    if constexpr (BCols)
+        if (p.last.out) {
+            kernel = orth_product_kernel<TT, BCols, Split, true>;
+            lds = std::max(TT::LDS_BYTES, kLastLds<TT>);
+        }
+    if (int rc = allow_lds(kernel, lds)) return rc;
+    const int64_t items = OrthTiles(p.Mp, p.Np, TT::BM, p.symmetric).tiles() * p.batch;
+    kernel<<<static_cast<unsigned>(TileOrder::blocks(items)), TT::NT, lds, s>>>(p);
     return SPO_OK;
 }
-template <bool ACols, bool BCols>
+template <bool BCols>
+static int launch_few(const OrthProduct &p, hipStream_t s) {
+    auto *kernel = orth_few_kernel<BCols>;
+    if (int rc = allow_lds(kernel, kFewLds)) return rc;
+    const int64_t items = OrthTiles(p.Mp, p.Np, kFewEdge, p.symmetric).tiles() * p.batch;
+    kernel<<<static_cast<unsigned>(TileOrder::blocks(items)), kFewThreads, kFewLds, s>>>(p);
+    return SPO_OK;
+}
+template <typename TT, bool BCols>
+static int launch_tiles(const OrthProduct &p, hipStream_t s) {
+    return p.split ? launch_tiles<TT, BCols, true>(p, s) : launch_tiles<TT, BCols, false>(p, s);
+}
+// Which kernel forms a product?  About what a launch takes, in us (measured on single matrices of 64 to 4096 and stacks of
+// four of 1024 x 4096, both kinds of products; within a fifth of it but for launches of a few us):
+//   tiles shared by wavefronts: rounds of workgroups on the chip x (steps x time of a step + the tile's ends); a step slows
+//   down as the chip fills up.  Half of the time that the addend and the output take from and to memory comes on top.
+//   a share of the contraction per wavefront: half rounds of a tile per compute unit.
+// So 64 x 64 x 64 (k, L, steps) takes 5 us instead of 7, 1024 x 1024 x 16 8.8 instead of 14 (128), 48 steps 14 instead of 33;
+// 2048 x 2048 x 32 24 on tiles of 128 (64: 25, 192: 31), 4096 x 4096 x 64 symmetric 73 on 192 (253 tiles on 256 compute units;
+// 85 on 256, 99 on 128), otherwise 118 on 256.
+enum class Kind { few, small, middle, large };
+struct OrthTimes {
+    int64_t edge, slots;
+    double start, step, crowd, ends;  // crowd: what a step takes longer on a chip that is full
+};
+constexpr OrthTimes kSmallTimes{128, 512, 3.0, 0.57, 0.30, 4.0}, kMiddleTimes{192, 256, 3.0, 0.75, 0.25, 4.0},
+    kLargeTimes{256, 256, 3.0, 1.00, 0.40, 9.0};
+static double product_time(const OrthTimes &t, const OrthProduct &p, double steps) {
+    const int64_t tiles = OrthTiles(p.Mp, p.Np, t.edge, p.symmetric).tiles() * p.batch, full = tiles / t.slots, rest = tiles % t.slots;
+    // (two small tiles share a compute unit once half of the slots are taken)
+    const double fill = t.slots > kChipCUs ? std::max<int64_t>(0, rest - kChipCUs) / 256.0 : static_cast<double>(rest) / static_cast<double>(t.slots);
+    const double bytes = static_cast<double>(p.Mp) * static_cast<double>(p.Np) * static_cast<double>(p.batch) *
+                         ((p.d.base ? (p.d_lo ? 4 : 2) : 0) + (p.out_lo ? 4 : 2));
+    return t.start + static_cast<double>(full) * (steps * (t.step + t.crowd) + t.ends) +
+           (rest ? steps * (t.step + t.crowd * fill) + t.ends : 0.0) + 0.5 * bytes / 5.0e6;
+}
+static Kind product_kind(const OrthProduct &p, bool middle) {
+    const double steps = p.KT * (p.split ? 3 : 1);
+    const int64_t tiles = OrthTiles(p.Mp, p.Np, kFewEdge, p.symmetric).tiles() * p.batch;
+    const double halves = std::max(1.0, static_cast<double>(ceil_div(2 * tiles, kChipCUs)) * 0.5);
+    Kind best = Kind::few;
+    double least = 4.0 + halves * (steps * 0.2 + 1.7);
+    auto offer = [&](Kind k, const OrthTimes &t) {
+        const double time = product_time(t, p, steps);
+        if (time < least) {
+            least = time;
+            best = k;
+        }
+    };
+    offer(Kind::small, kSmallTimes);
+    if (middle) offer(Kind::middle, kMiddleTimes);
+    offer(Kind::large, kLargeTimes);
+    return best;
+}
+template <bool BCols>
 static int launch_product(const OrthProduct &p, hipStream_t s) {
-    const bool small = tiles_over(p.Mp, false) * tiles_over(p.Np, false) * p.batch < kChipCUs * 3 / 4;
-    if (small) return p.split ? launch_product<OS, ACols, BCols, true>(p, s) : launch_product<OS, ACols, BCols, false>(p, s);
-    return p.split ? launch_product<OL, ACols, BCols, true>(p, s) : launch_product<OL, ACols, BCols, false>(p, s);
+    const Kind kind = product_kind(p, !BCols);  // (tiles of 192 take rows along the contraction only)
+    if (kind == Kind::few) return launch_few<BCols>(p, s);
+    if (kind == Kind::small) return launch_tiles<OS, BCols>(p, s);
+    if constexpr (!BCols)
+        if (kind == Kind::middle) return launch_tiles<OM, BCols>(p, s);
+    return launch_tiles<OL, BCols>(p, s);
 }
 
 static int run_orth(const spo_orth_desc *d, const OrthInput &in, OrthOut last, void *ws, size_t ws_bytes, hipStream_t s) {
     const OrthPlan p = plan_orth(d, ws);
     if (ws_bytes < p.bytes) return SPO_EWORKSPACE;
-    const dim3 parts(static_cast<unsigned>(p.parts), static_cast<unsigned>(d->batch));
-    orth_norm_kernel<<<parts, 256, 0, s>>>(in, p.norm);
-    const int64_t vectors = p.rp * p.cp / 8;
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(1024, ceil_div(vectors, 256))), static_cast<unsigned>(d->batch));
-    orth_scale_kernel<<<grid, 256, 0, s>>>(in, p.norm, p.parts, p.x_scale, p.X[0], p.rp, d->steps ? OrthOut{} : last);
+    const bool tall = d->rows > d->cols;
+    const unsigned batch = static_cast<unsigned>(d->batch);
+    orth_norm_kernel<<<dim3(static_cast<unsigned>(p.parts), batch), 256, 0, s>>>(in, p.norm);
+    if (tall && d->steps) {
+        orth_scale_turned_kernel<<<dim3(static_cast<unsigned>(p.Lp / 64 * (p.kp / 64)), batch), 256, 0, s>>>(in, p.norm, p.parts, p.x_scale,
+                                                                                                           p.X[0], static_cast<unsigned>(p.Lp / 64));
+    } else {
+        const int64_t vectors = p.kp * p.Lp / 8;
+        const int64_t x_rows = d->steps ? p.kp : d->rows;
+        orth_scale_kernel<<<dim3(static_cast<unsigned>(std::min<int64_t>(1024, ceil_div(vectors, 256))), batch), 256, 0, s>>>(
+            in, p.norm, p.parts, p.x_scale, p.X[0], x_rows, d->steps ? OrthOut{} : last);
+    }
+    last.across = tall;
     // Where the smaller side is one step of the contraction, launches are all that counts, and so few roundings do not
     // average out (one of 1 x 1: 4e-3): always pairs.
-    const bool tall = d->rows > d->cols, split = d->products == SPO_PRODUCTS_SPLIT || p.k <= kBK;
+    const bool split = d->products == SPO_PRODUCTS_SPLIT || p.k <= kBK;
     for (int i = 0; i < d->steps; ++i) {
-        const Stack &X = p.X[i & 1], &Xn = p.X[(i + 1) & 1];
+        const Stack &X = p.X[i & 1];
         OrthProduct q{};
         q.batch = d->batch;
         q.split = split;
         q.d_lo = q.out_lo = split;
-        // A = X X^T (X^T X)
+        // A = X X^T
+        q.symmetric = 1;
         q.a = q.b = X;
         q.out = p.A;
         q.M = q.N = p.k;
         q.Mp = q.Np = p.kp;
-        q.KT = static_cast<int>((tall ? p.rp : p.cp) / kBK);
+        q.KT = static_cast<int>(p.Lp / kBK);
         q.alpha = kGramScale / (p.x_scale * p.x_scale);
-        if (int rc = tall ? launch_product<true, true>(q, s) : launch_product<false, false>(q, s)) return rc;
-        // B = b A + c A A; both are symmetric, so rows serve as columns
+        if (int rc = launch_product<false>(q, s)) return rc;
+        // B = b A + c A A; A is symmetric, so its rows serve as columns
         q.a = q.b = q.d = p.A;
         q.out = p.B;
         q.KT = static_cast<int>(p.kp / kBK);
         q.alpha = d->c / kGramScale;
         q.beta = d->b;
-        if (int rc = launch_product<false, false>(q, s)) return rc;
-        // X <- a X + B X (X B)
-        q.a = tall ? X : p.B;
-        q.b = tall ? p.B : X;
-        q.d = X;
+        if (int rc = launch_product<false>(q, s)) return rc;
+        // X <- a X + B X
+        q.symmetric = 0;
+        q.a = p.B;
+        q.b = q.d = X;
         q.d_lo = q.out_lo = 1;
-        q.out = Xn;
-        q.M = d->rows;
-        q.N = d->cols;
-        q.Mp = p.rp;
-        q.Np = p.cp;
+        q.out = p.X[(i + 1) & 1];
+        q.N = p.L;
+        q.Np = p.Lp;
         q.alpha = 1.0f / kGramScale;
         q.beta = d->a;
         if (i == d->steps - 1) {
@@ -406,7 +860,7 @@ static int run_orth(const spo_orth_desc *d, const OrthInput &in, OrthOut last, v
             q.beta /= p.x_scale;
             q.last = last;
         }
-        if (int rc = tall ? launch_product<false, false>(q, s) : launch_product<false, true>(q, s)) return rc;
+        if (int rc = launch_product<true>(q, s)) return rc;
     }
     return launch_status();
 }
@@ -451,7 +905,7 @@ extern "C" int spo_orthogonalize(const spo_orth_desc *d, const void *G, int g_dt
     in.rows = d->rows;
     in.cols = d->cols;
     in.eps = d->eps;
-    return run_orth(d, in, OrthOut{out, out_dtype, 0, d->cols, d->rows * d->cols, 0.0f, 0.0f}, ws, ws_bytes, as_stream(stream));
+    return run_orth(d, in, OrthOut{out, out_dtype, 0, 0, d->cols, d->rows * d->cols, 0.0f, 0.0f}, ws, ws_bytes, as_stream(stream));
 }
 
 extern "C" int spo_muon_update(const spo_orth_desc *d, void *W, int w_dtype, float *momentum, const void *grad, int g_dtype, float mu,
@@ -475,5 +929,5 @@ extern "C" int spo_muon_update(const spo_orth_desc *d, void *W, int w_dtype, flo
     in.cols = d->cols;
     in.eps = d->eps;
     const float keep = static_cast<float>(1.0 - static_cast<double>(lr) * weight_decay);
-    return run_orth(d, in, OrthOut{W, w_dtype, 1, d->cols, d->rows * d->cols, keep, lr * scale}, ws, ws_bytes, as_stream(stream));
+    return run_orth(d, in, OrthOut{W, w_dtype, 1, 0, d->cols, d->rows * d->cols, keep, lr * scale}, ws, ws_bytes, as_stream(stream));
 }
