@@ -514,6 +514,263 @@ score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, Sc
 }
 
 // ----------------------------------------------------------------------------
+// a few tokens from hidden states and the head
+// ----------------------------------------------------------------------------
+// Up to kFewTokens tokens (a server's step): bound by one read of the head, 1.24 GB at 4096 x 151936 in bf16.  The sweep's
+// tiles of 128 tokens take 231 us for that, 239 with their preparation and joining.
+//   One token, or two of more than 2048 hidden units: a wavefront forms one vocabulary entry's logits after the other as dot
+//   products, its row read by whole kilobytes, the hidden states in registers; rows go round the wavefronts of the chip, which
+//   so walks the head in order (181 us = 6.9 TB/s; two tokens 184).  The sums over lanes are what does not scale: four tokens
+//   take 228 us, of 1024 hidden units 106 (and 57 the other way).
+//   More: a wavefront forms the logits of 16 vocabulary entries by 16 tokens, the entries' rows straight from memory into the
+//   operands of the matrix instruction, kFewLoads loads of 16 bytes per lane at a time and as many on their way behind them;
+//   the hidden states wait in LDS; blocks of 16 entries go round the wavefronts (235 to 247 us; 16 rows of 64 bytes per load do
+//   not reach the rate of whole rows).
+constexpr int kFewTokens = 16, kFewWaves = 8, kFewLoads = 8, kFewGroups = 512;
+constexpr int kFewPad = 16;                // bytes behind a token's row in LDS: rows on different banks
+constexpr int64_t kFewLds = 144 * 1024;
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+// a wavefront's values of tokens 0 .. T-1 joined over the workgroup, into part[token][workgroup]
+template <int Waves>
+__device__ __forceinline__ void store_few(float (*joined)[kFewTokens][3], int T, float *part) {
+    __syncthreads();
+    if (threadIdx.x >= T) return;
+    const int t = threadIdx.x;
+    float m = joined[0][t][0], s = joined[0][t][1], u = joined[0][t][2];
+    for (int w = 1; w < Waves; ++w) score_join(m, s, u, joined[w][t][0], joined[w][t][1], joined[w][t][2]);
+    float *o = part + (static_cast<int64_t>(t) * gridDim.x + blockIdx.x) * 3;
+    o[0] = m;
+    o[1] = s;
+    o[2] = u;
+}
+
+typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
+constexpr int kDotSpan = 8 * kWave;  // elements of a row per load of a wavefront
+// Up to NT tokens of up to 512 * NC hidden units, R rows of the head at a time (short rows: as many loads on their way as
+// long ones have).
+template <int NT, int NC, int R>
+__global__ void __launch_bounds__(kFewWaves * kWave, 2)
+few_dots_kernel(const bf16_t *__restrict__ X, const bf16_t *__restrict__ W, int T, int H, int64_t V, const int32_t *__restrict__ target,
+                float *__restrict__ part, float *__restrict__ z_target) {
+    static_assert(kWave % R == 0, "a lane keeps whole rounds of rows");
+    __shared__ float joined[kFewWaves][kFewTokens][3];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kFewWaves * R, r0 = (static_cast<int64_t>(blockIdx.x) * kFewWaves + wave) * R;
+    const int chunks = (H + kDotSpan - 1) / kDotSpan;
+    // (past the end of a row its start is read, and counts as zeros; past the last row the last)
+    auto request = [&](uint4 (&v)[R][NC], int64_t r) {
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const bf16_t *row = W + (r + q < V ? r + q : V - 1) * H;
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+                if (j < chunks) {
+                    const int k = j * kDotSpan + lane * 8;
+                    const u32x4_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(row + (k < H ? k : 0)));
+                    v[q][j] = make_uint4(w.x, w.y, w.z, w.w);
+                }
+        }
+    };
+    uint4 now[R][NC], next[R][NC], x[NT][NC];
+    if (r0 < V) request(now, r0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            const int k = j * kDotSpan + lane * 8;
+            x[t][j] = t < T && k < H ? *reinterpret_cast<const uint4 *>(X + static_cast<int64_t>(t) * H + k) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    int64_t y[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) y[t] = target && t < T ? target[t] : -1;
+    float m[NT], s[NT], u[NT], z[NT];  // lane l: of the logits of the l-th, (l + 64)-th, ... row of this wavefront's
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m[t] = kLowestFloat;
+        s[t] = u[t] = 0.0f;
+        z[t] = -INFINITY;
+    }
+    auto take = [&] {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float mx = fmaxf(m[t], z[t]), d = fmaxf((m[t] - mx) * kLog2e, kLowest2), q = (z[t] - mx) * kLog2e;
+            const float f = __builtin_amdgcn_exp2f(d), e = __builtin_amdgcn_exp2f(q);  // (a NaN stays one)
+            u[t] = f * fmaf(d, s[t], u[t]) + e * fmaxf(q, kLowest2);
+            s[t] = f * s[t] + e;
+            m[t] = mx;
+            z[t] = -INFINITY;
+        }
+    };
+    int n = 0;  // place of the next row among the lanes
+    for (int64_t r = r0; r < V; r += stride) {
+        if (r + stride < V) request(next, r + stride);
+        float a[R][NT][2];
+#pragma unroll
+        for (int q = 0; q < R; ++q)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) a[q][t][0] = a[q][t][1] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+            if (j < chunks)
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                    uint32_t w[4] = {now[q][j].x, now[q][j].y, now[q][j].z, now[q][j].w};
+                    if ((j + 1) * kDotSpan > H)  // an infinite weight times a zero that is not there
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = j * kDotSpan + lane * 8 < H ? w[i] : 0u;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint32_t h[4] = {x[t][j].x, x[t][j].y, x[t][j].z, x[t][j].w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            a[q][t][i & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2v_t, w[i]),
+                                                                             __builtin_bit_cast(bf16x2v_t, h[i]), a[q][t][i & 1], false);
+                    }
+                }
+#pragma unroll
+        for (int q = 0; q < R; ++q)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float sum = wave_sum(a[q][t][0] + a[q][t][1]);
+                if (r + q < V) {
+                    z[t] = lane == n + q ? sum : z[t];
+                    if (r + q == y[t] && lane == 0) z_target[t] = sum;
+                }
+            }
+        n = (n + R) % kWave;
+        if (n == 0) take();
+#pragma unroll
+        for (int q = 0; q < R; ++q)
+#pragma unroll
+            for (int j = 0; j < NC; ++j) now[q][j] = next[q][j];
+    }
+    take();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        join_lanes(m[t], s[t], u[t]);
+        if (lane == 0) {
+            joined[wave][t][0] = m[t];
+            joined[wave][t][1] = s[t];
+            joined[wave][t][2] = u[t];
+        }
+    }
+    store_few<kFewWaves>(joined, T, part);
+}
+
+static bool few_tokens(const spo_logprob_desc *d) {
+    return d->dtype == SPO_BF16 && d->w_layout == SPO_W_VH && d->T <= kFewTokens && d->T * (d->H * 2 + kFewPad) <= kFewLds;
+}
+
+// part[token][workgroup] = (max, sum of 2^x, sum of x 2^x); z_target[token] where the target is in the vocabulary
+__global__ void __launch_bounds__(kFewWaves * kWave, 2)
+few_tokens_kernel(const bf16_t *__restrict__ X, const bf16_t *__restrict__ W, int T, int H, int64_t V, const int32_t *__restrict__ target,
+                  float *__restrict__ part, float *__restrict__ z_target) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float joined[kFewWaves][kFewTokens][3];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int col = lane & 15, grp = lane >> 4, pitch = H * 2 + kFewPad;
+    const int64_t blocks = ceil_div(V, 16), stride = static_cast<int64_t>(gridDim.x) * kFewWaves;
+    const int slices = H / 32, chunks = (slices + kFewLoads - 1) / kFewLoads;
+    // chunk c of block b: this lane's row of W (the last one past the vocabulary) from element 32 * kFewLoads * c + 8 * grp on
+    uint4 set[2][kFewLoads];
+    auto request = [&](uint4 (&v)[kFewLoads], int64_t b, int c) {
+        const int64_t r = b * 16 + col;
+        const bf16_t *row = W + (r < V ? r : V - 1) * H + 8 * grp;
+#pragma unroll
+        for (int i = 0; i < kFewLoads; ++i) {
+            const int sl = c * kFewLoads + i;
+            const u32x4_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(row + (sl < slices ? sl : slices - 1) * 32));
+            v[i] = make_uint4(w.x, w.y, w.z, w.w);
+        }
+    };
+    int64_t b = static_cast<int64_t>(blockIdx.x) * kFewWaves + wave;
+    if (b < blocks) request(set[0], b, 0);
+    for (int i = threadIdx.x; i < T * (H / 8); i += blockDim.x) {
+        const int t = i / (H / 8), k = i % (H / 8);
+        *reinterpret_cast<uint4 *>(lds + t * pitch + k * 16) = *reinterpret_cast<const uint4 *>(X + static_cast<int64_t>(t) * H + k * 8);
+    }
+    const int64_t y = target && col < T ? target[col] : -1;
+    __syncthreads();
+    const char *x = lds + (col < T ? col : 0) * pitch + grp * 16;  // (columns past the tokens: the first, not used)
+    float m = kLowestFloat, s = 0.0f, u = 0.0f;
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    int c = 0;
+    auto work = [&](uint4 (&now)[kFewLoads], uint4 (&next)[kFewLoads]) {
+        const bool last = c + 1 == chunks;
+        const int64_t nb = last ? b + stride : b;
+        if (nb < blocks) request(next, nb, last ? 0 : c + 1);
+#pragma unroll
+        for (int i = 0; i < kFewLoads; ++i) {
+            const int sl = c * kFewLoads + i;
+            if (sl < slices)
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, now[i]),
+                                                              *reinterpret_cast<const bf16x8_t *>(x + sl * 64), acc, 0, 0, 0);
+        }
+        if (last) {  // a lane holds entries 4 grp .. 4 grp + 3 of the block for token col
+            const int64_t v0 = b * 16 + 4 * grp;
+            float mx = m;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (v0 + r >= V) acc[r] = -INFINITY;
+                if (v0 + r == y) z_target[col] = acc[r];
+                mx = fmaxf(mx, acc[r]);
+            }
+            const float d = fmaxf((m - mx) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d);
+            u = f * fmaf(d, s, u);
+            s *= f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float q = (acc[r] - mx) * kLog2e, e = __builtin_amdgcn_exp2f(q);  // (a NaN stays one)
+                s += e;
+                u = fmaf(e, fmaxf(q, kLowest2), u);
+            }
+            m = mx;
+            acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        c = last ? 0 : c + 1;
+        b = nb;
+    };
+    while (b < blocks) {
+        work(set[0], set[1]);
+        if (b >= blocks) break;
+        work(set[1], set[0]);
+    }
+#pragma unroll
+    for (int o = 16; o < kWave; o <<= 1) {
+        // (the lower lane's values first, so that both lanes of a pair form the same sums)
+        const float om = __shfl_xor(m, o, kWave), os = __shfl_xor(s, o, kWave), ou = __shfl_xor(u, o, kWave);
+        float a = lane & o ? om : m, p = lane & o ? os : s, q = lane & o ? ou : u;
+        score_join(a, p, q, lane & o ? m : om, lane & o ? s : os, lane & o ? u : ou);
+        m = a; s = p; u = q;
+    }
+    if (grp == 0) {
+        joined[wave][col][0] = m;
+        joined[wave][col][1] = s;
+        joined[wave][col][2] = u;
+    }
+    store_few<kFewWaves>(joined, T, part);
+}
+
+// Scores of token blockIdx.x from the workgroups' shares.
+__global__ void __launch_bounds__(kWave)
+few_scores_kernel(const float *__restrict__ part, int groups, const float *__restrict__ z_target, ScoreRows rows, ScoreOut out) {
+    const int64_t t = blockIdx.x;
+    if (rows.mask && !rows.mask[t]) {
+        if (threadIdx.x == 0) store_left_out(out, t);
+        return;
+    }
+    float zt = 0.0f, m, s, u;
+    if (rows.target) {
+        const int64_t y = rows.target[t];
+        zt = y >= 0 && y < rows.V ? z_target[t] : __builtin_nanf("");
+    }
+    join_segments(part, groups, t, m, s, u);
+    if (threadIdx.x == 0) store_scores(out, t, zt, m, s, u);
+}
+
+// ----------------------------------------------------------------------------
 // host side
 // ----------------------------------------------------------------------------
 static ScoreRows score_rows(const spo_logprob_desc *d) {
@@ -577,6 +834,45 @@ static int logits_logprob_fwd(const spo_logprob_desc *d, const ScoreOut &o, void
     return launch_status();
 }
 
+struct FewPlan {
+    float *part, *z_target;
+    size_t bytes;
+};
+static FewPlan plan_few(void *ws) {
+    FewPlan p;
+    Arena a(ws);
+    p.part = a.take<float>(kFewTokens * kFewGroups * 3);
+    p.z_target = a.take<float>(kFewTokens);
+    p.bytes = a.used;
+    return p;
+}
+
+static int few_logprob_fwd(const spo_logprob_desc *d, const ScoreOut &o, void *ws, size_t ws_bytes, hipStream_t s) {
+    const FewPlan p = plan_few(ws);
+    if (ws_bytes < p.bytes) return SPO_EWORKSPACE;
+    if (d->T == 0) return SPO_OK;
+    const int64_t chunks = ceil_div(d->H, kDotSpan);
+    const bool dots = (d->T == 1 && chunks <= 16) || (d->T == 2 && chunks > 4 && chunks <= 8);
+    const int64_t rows = !dots ? 16 : chunks <= 2 ? 4 : chunks <= 4 ? 2 : 1;  // that a wavefront takes at a time
+    const int groups = static_cast<int>(std::min<int64_t>(dots ? kFewGroups : kFewGroups / 2, ceil_div(ceil_div(d->V, rows), kFewWaves)));
+    const int lds = dots ? 0 : static_cast<int>(d->T * (d->H * 2 + kFewPad));
+    auto *kernel = !dots        ? few_tokens_kernel
+                   : d->T == 2  ? few_dots_kernel<2, 8, 1>
+                   : chunks > 8 ? few_dots_kernel<1, 16, 1>
+                   : rows == 4  ? few_dots_kernel<1, 2, 4>
+                   : rows == 2  ? few_dots_kernel<1, 4, 2>
+                                : few_dots_kernel<1, 8, 1>;
+    if (!dots && hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+        return SPO_EHIP;
+    {
+        ScopedKernelTimer timer(kTimeFwdSweep, s);
+        kernel<<<groups, kFewWaves * kWave, lds, s>>>(static_cast<const bf16_t *>(d->hidden), static_cast<const bf16_t *>(d->W),
+                                                      static_cast<int>(d->T), static_cast<int>(d->H), d->V, d->target, p.part, p.z_target);
+    }
+    few_scores_kernel<<<static_cast<unsigned>(d->T), kWave, 0, s>>>(p.part, groups, p.z_target, score_rows(d), o);
+    return launch_status();
+}
+
 template <typename T>
 static void launch_score_grad(const spo_logprob_desc *d, const ScoreGrads &g, void *d_logits, hipStream_t s) {
     const RowGrid grid = row_grid(d->T, d->V, d->dtype, kScoreGradGroup, 1, kScoreGradNarrow);
@@ -616,9 +912,9 @@ static int validate(const spo_logprob_desc *d) {
 extern "C" size_t spo_logprob_fwd_workspace_bytes(const spo_logprob_desc *d) {
     if (validate(d) != SPO_OK) return 0;
     size_t b = 0;
-    if (d->logits) b = plan_scores(d, nullptr).bytes;
-    else head_logprob_fwd_workspace(d, &b);
-    return b;
+    if (d->logits) return plan_scores(d, nullptr).bytes;
+    head_logprob_fwd_workspace(d, &b);
+    return std::max(b, plan_few(nullptr).bytes);  // (of any number of tokens: it serves smaller batches)
 }
 
 extern "C" int spo_logprob_fwd(const spo_logprob_desc *d, float *logp, float *lse, float *entropy, int32_t *top_id, float *top_logp,
@@ -629,6 +925,7 @@ extern "C" int spo_logprob_fwd(const spo_logprob_desc *d, float *logp, float *ls
     if (!ws) return SPO_EWORKSPACE;
     if (reinterpret_cast<uintptr_t>(ws) % 256 != 0) return SPO_EINVAL;
     if (!d->target) logp = nullptr;
+    if (!d->logits && few_tokens(d)) return few_logprob_fwd(d, ScoreOut{logp, lse, entropy, nullptr, nullptr, 0}, ws, ws_bytes, as_stream(stream));
     if (!d->logits) return head_logprob_fwd(d, logp, lse, entropy, ws, ws_bytes, as_stream(stream));
     return logits_logprob_fwd(d, ScoreOut{logp, lse, entropy, top_id, top_logp, d->top_k}, ws, ws_bytes, as_stream(stream));
 }

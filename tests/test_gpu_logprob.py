@@ -274,6 +274,42 @@ def test_head_forward(hv, dtype, T, H, V):
     assert logp is None and entropy is None and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("T", [1, 2, 3, 7, 16])
+@pytest.mark.parametrize("H,V", [(64, 1), (64, 17), (448, 3000), (1024, 501), (1088, 20000), (2112, 300), (4096, 1111), (4160, 640), (8192, 95)])
+def test_a_few_tokens(T, H, V):
+    X, W = head_inputs(T, H, V, BF16, T + V + H)
+    target = sc.targets(T, V, T + H)
+    target[-1] = V - 1
+    mask = None
+    if T > 2:
+        mask = torch.ones(T, dtype=torch.uint8)
+        mask[1] = 0
+        target[0] = V           # outside the vocabulary
+    d = spo.make_logprob_desc(X.cuda(), W.cuda(), target.cuda(), cuda(mask))
+    logp, lse, entropy, _, _ = spo.spo_logprob_fwd(d)
+    want = sc.scores(X.double() @ W.double().t(), target, mask)
+    for x, k in ((logp, "logp"), (lse, "lse"), (entropy, "entropy")):
+        close(x, want[k], atol=2e-4)
+    again = spo.spo_logprob_fwd(d)
+    assert torch.equal(again[1], lse) and torch.equal(again[2], entropy)
+
+
+@pytest.mark.parametrize("T", [1, 2, 5, 20])
+def test_an_infinite_weight_does_not_reach_other_tokens(T):
+    H, V = 192, 700
+    X, W = head_inputs(T, H, V, BF16, T)
+    X[:, 5] = 0
+    X[0, 5] = 1
+    W[333, 5] = float("-inf")     # bans an entry for the first token; for the others 0 * inf
+    d = spo.make_logprob_desc(X.cuda(), W.cuda(), torch.zeros(T, dtype=torch.int32, device="cuda"))
+    logp, lse, entropy, _, _ = spo.spo_logprob_fwd(d)
+    z = X.double() @ W.double().t()
+    want = sc.scores(z[:1], torch.zeros(1, dtype=torch.int32))
+    for x, k in ((logp, "logp"), (lse, "lse"), (entropy, "entropy")):
+        close(x[:1], want[k], atol=2e-4)
+    assert T == 1 or torch.isnan(lse[1:]).all()
+
+
 @pytest.mark.parametrize("hv", [False, True])
 @pytest.mark.parametrize("T,H,V,chunk", [(1, 64, 10, 0), (5, 128, 1003, 0), (713, 256, 3000, 0), (600, 64, 500, 256), (300, 1024, 2111, 0)])
 @pytest.mark.parametrize("parts", ["logp", "entropy", "both"])
