@@ -537,6 +537,10 @@ def spo_logprob_fwd_workspace_bytes(desc) -> int:
 def spo_logprob_fwd(desc, workspace=None, want_entropy=True):
     """Returns (logp[T] or None, lse[T], entropy[T] or None, top_id[T, top_k] or None, top_logp[T, top_k] or None)."""
     d, keep = desc
+    if workspace is not None and want_entropy is True:
+        out = _plain_calls().logprob_fwd(C.addressof(d), keep[0] if keep[2] is None else keep[2], workspace)
+        if out is not None:
+            return out
     dev = keep[5]
     lse = _per_token(d.T, dev)
     logp = _per_token(d.T, dev) if keep[3] is not None else None
@@ -561,6 +565,10 @@ def spo_logprob_bwd(desc, lse, entropy=None, d_logp=None, d_entropy=None, top_id
     """Gradients of sum(d_logp * logp) + sum(d_entropy * entropy) + sum(d_top_logp * top_logp); each may be None.
     Head form: returns (d_hidden[T, H] or None, d_W in W's layout or None).  Logits-in form: returns d_logits[T, V]."""
     d, keep = desc
+    if keep[2] is not None and chunk_tokens == 0:
+        out = _plain_calls().logprob_bwd(C.addressof(d), keep[2], lse, entropy, d_logp, d_entropy, top_id, d_top_logp)
+        if out is not None:
+            return out
     dev = keep[5]
     for t, name, n in ((lse, "lse", d.T), (entropy, "entropy", d.T), (d_logp, "d_logp", d.T), (d_entropy, "d_entropy", d.T),
                        (d_top_logp, "d_top_logp", d.T * d.top_k)):

@@ -296,6 +296,63 @@ PyObject *pg_loss_fwd_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// The descriptor of a call of log-probs: its address, and a tensor of its device.  False: not plain.
+bool scored(PyObject *address, PyObject *of, const spo_logprob_desc *&d, const at::Tensor *&like) {
+    if (!PyLong_CheckExact(address)) return false;
+    d = static_cast<const spo_logprob_desc *>(PyLong_AsVoidPtr(address));
+    like = tensor(of);
+    return d && like && d->T > 0;
+}
+
+// (descriptor, hidden states or logits, workspace) -> (logp or None, lse, entropy, top_id or None, top_logp or None)
+PyObject *logprob_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const spo_logprob_desc *d;
+    const at::Tensor *like;
+    if (n != 3 || !plain_context() || !scored(a[0], a[1], d, like) || d->top_k < 0) return none();
+    const at::Tensor *ws = workspace(a[2], spo_logprob_fwd_workspace_bytes(d));
+    if (!ws) return none();
+    const at::Tensor lse = fresh({d->T}, at::kFloat, *like), entropy = fresh({d->T}, at::kFloat, *like);
+    at::Tensor logp, ids, top;
+    if (d->target) logp = fresh({d->T}, at::kFloat, *like);
+    if (d->top_k) {
+        ids = fresh({d->T, d->top_k}, at::kInt, *like);
+        top = fresh({d->T, d->top_k}, at::kFloat, *like);
+    }
+    const spo_stream_t s = stream();
+    const int rc = unlocked([&] {
+        return spo_logprob_fwd(d, logp.defined() ? ptr<float>(logp) : nullptr, ptr<float>(lse), ptr<float>(entropy),
+                               d->top_k ? ptr<int32_t>(ids) : nullptr, d->top_k ? ptr<float>(top) : nullptr, ws->data_ptr(), ws->numel(), s);
+    });
+    auto given = [](const at::Tensor &t) { return t.defined() ? wrap(t) : none(); };
+    return rc ? refused(rc, "spo_logprob_fwd") : pack(given(logp), wrap(lse), wrap(entropy), given(ids), given(top));
+    END_HANDLE_TH_ERRORS
+}
+
+// (descriptor, logits, lse, entropy, d_logp, d_entropy, top_id, d_top_logp) -> d_logits, of the logits-in form; all but the first
+// three may be None
+PyObject *logprob_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const spo_logprob_desc *d;
+    const at::Tensor *like;
+    if (n != 8 || !plain_context() || !scored(a[0], a[1], d, like) || !d->logits || d->top_k < 0) return none();
+    const at::Tensor *lse = dense(a[2], at::kFloat, d->T);
+    const at::Tensor *in[5];  // entropy, d_logp, d_entropy, top_id, d_top_logp
+    if (!lse) return none();
+    for (int i = 0; i < 5; ++i) {
+        in[i] = a[3 + i] == Py_None ? nullptr : dense(a[3 + i], i == 3 ? at::kInt : at::kFloat, i < 3 ? d->T : d->T * d->top_k);
+        if (!in[i] && a[3 + i] != Py_None) return none();
+    }
+    const at::Tensor dl = fresh({d->T, d->V}, type_of(d->dtype), *like);
+    const spo_stream_t s = stream();
+    const int rc = unlocked([&] {
+        return spo_logprob_bwd(d, ptr<float>(lse), ptr<float>(in[0]), ptr<float>(in[1]), ptr<float>(in[2]), ptr<int32_t>(in[3]), ptr<float>(in[4]),
+                               nullptr, 0, nullptr, 0, 0, dl.data_ptr(), 0, nullptr, 0, s);
+    });
+    return rc ? refused(rc, "spo_logprob_bwd") : wrap(dl);
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject *set_error(PyObject *, PyObject *type) {
     Py_INCREF(type);
     Py_XSETREF(g_error, type);
@@ -304,7 +361,7 @@ PyObject *set_error(PyObject *, PyObject *type) {
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(sample_prompts), FAST(advantages), FAST(advantage_diagnostics), FAST(tracker_update), FAST(pg_loss_fwd),
-                         FAST(pg_loss_bwd), FAST(pg_loss_fwd_bwd), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         FAST(pg_loss_bwd), FAST(pg_loss_fwd_bwd), FAST(logprob_fwd), FAST(logprob_bwd), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_spo_calls", "plain calls of the binding", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

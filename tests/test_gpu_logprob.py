@@ -375,6 +375,59 @@ def test_head_batches_without_tokens_or_factors():
     assert (dx == 0).all() and (dw == 0).all()
 
 
+# ------------------------------------------------------------------ plain calls of the binding
+@pytest.mark.parametrize("K", [0, 6])
+@pytest.mark.parametrize("given", [True, False])
+def test_plain_calls_give_the_same_bits(monkeypatch, K, given):
+    z = sc.logits(20, 3000, BF16, 1).cuda()
+    target = sc.targets(20, 3000, 1).cuda() if given else None
+    d = spo.make_logprob_desc(None, None, target, sc.mask_of(20, 3).cuda(), logits=z, top_k=K)
+    ws = torch.empty(spo.spo_logprob_fwd_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    a, e, b = sc.factors(20, 1).cuda() if given else None, sc.factors(20, 2).cuda(), sc.factors((20, K), 3).cuda() if K else None
+    X, W = head_inputs(20, 64, 300, BF16, 1)
+    h = spo.make_logprob_desc(X.cuda(), W.cuda(), target if target is None else target % 300)
+    wh = torch.empty(spo.spo_logprob_fwd_workspace_bytes(h), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        out = spo.spo_logprob_fwd(d, workspace=ws)
+        return (*out, spo.spo_logprob_bwd(d, out[1], out[2], a, e, out[3], b), *spo.spo_logprob_fwd(h, workspace=wh))
+
+    real, taken = spo._plain_calls(), []
+
+    class Watch:
+        def __getattr__(self, name):
+            def f(*args):
+                out = getattr(real, name)(*args)
+                taken.append((name, out is not None))
+                return out
+            return f
+
+    class Nothing:
+        def __getattr__(self, name):
+            return lambda *args: None
+
+    results = []
+    for way in (Watch(), Nothing()):
+        with monkeypatch.context() as m:
+            m.setattr(spo, "_calls", way)
+            results.append(calls())
+    assert taken == [("logprob_fwd", True), ("logprob_bwd", True), ("logprob_fwd", True)]
+    for x, y in zip(*results):
+        assert (x is None and y is None) or (x.dtype == y.dtype and x.shape == y.shape and torch.equal(x, y))
+    # what is not plain goes the general way: its errors, and calls that are right all the same
+    with pytest.raises(TypeError):
+        spo.spo_logprob_bwd(d, out_of(results)[1].double())
+    with pytest.raises(ValueError):
+        spo.spo_logprob_bwd(d, out_of(results)[1][:3])
+    bad = spo.make_logprob_desc(None, None, target, None, logits=z, top_k=65)
+    with pytest.raises(spo.SpoError):
+        spo.spo_logprob_fwd(bad, workspace=ws)
+
+
+def out_of(results):
+    return results[0]
+
+
 # ------------------------------------------------------------------ refusals
 def test_refusals():
     z = torch.zeros((4, 100), device="cuda")
