@@ -7,7 +7,10 @@
 // low-rank matrices: small singular values grow by a (3.44) per step, and with them whatever was rounded in X; the rounding
 // of A and B is not amplified.  So X is kept as a pair of halves (hi + lo / 2048, 22 bits), the term a X reads both, the
 // products read hi alone: 2e-4 to 1.7e-3 after five steps (X in 11 bits: up to 2e-2; all of it in bf16: up to 0.16) for
-// 4 bytes more per entry in the epilogue.  SPO_PRODUCTS_SPLIT keeps A and B as pairs too and forms
+// 4 bytes more per entry in the epilogue.  Most of what is left comes from the diagonals of A and B, which lie near the mean
+// of the squared singular values, s = |X|_F^2 / k, and near b s + c s^2.  So what is stored is A' = A - s I and
+// B' = c A' A' + (b + 2 c s) A', and X <- (a + b s + c s^2) X + B' X: the same polynomial, 2e-4 to 8e-4.
+// SPO_PRODUCTS_SPLIT keeps A and B as pairs too and forms
 // hi hi + (hi lo + lo hi) / 2048 in every product: 3e-7 to 5e-6, three times the matrix instructions.
 //
 // Every matrix in the workspace has its sides rounded up to a step of the contraction (64), zero beyond the true ones: the
@@ -80,10 +83,47 @@ struct OrthProduct {
     int64_t batch;
     int KT, split;        // split: products of pairs
     int symmetric;        // only tiles on and below the diagonal are formed, each stored on both sides
-    float alpha, beta;    // value = alpha * (A B) + beta * D
+    float alpha;          // value = alpha * (A B) + beta * D, beta = c[0] + s (c[1] + s c[2])
+    float c[3];
     int d_lo, out_lo;     // D has, the output gets, a lo plane
+    // Of each matrix the mean s of X's squared singular values: the product of X and its transpose forms it from the partial
+    // sums of X's squares (n_sq of them, times sq_scale), takes it off its diagonal and leaves it in shift; the others read it.
+    const float *sq;
+    int n_sq;
+    float sq_scale;
+    float *shift;
+    float *sq_out;        // [matrix][tile][wavefront] sums of squares of what is stored, NULL: not asked for
     OrthOut last;
 };
+
+// s of a matrix (see OrthProduct) in two parts: every wavefront's sum into scratch (NT / 64 floats), and, after a barrier, their
+// total for every thread.
+template <int NT>
+__device__ __forceinline__ float begin_shift(const OrthProduct &p, int64_t matrix, float *scratch) {
+    if (!p.n_sq) return p.shift[matrix];
+    float sum = 0.0f;
+    for (int i = threadIdx.x; i < p.n_sq; i += NT) sum += p.sq[matrix * p.n_sq + i];
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x / kWave] = sum;
+    return 0.0f;
+}
+template <int NT>
+__device__ __forceinline__ float end_shift(const OrthProduct &p, int64_t matrix, const float *scratch, float begun, bool first_tile) {
+    if (!p.n_sq) return begun;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NT / kWave; ++w) sum += scratch[w];
+    sum *= p.sq_scale;
+    if (first_tile && threadIdx.x == 0) p.shift[matrix] = sum;
+    return sum;
+}
+__device__ __forceinline__ float beta_of(const OrthProduct &p, float s) { return p.c[0] + s * (p.c[1] + s * p.c[2]); }
+// a wavefront's sum of squares (one by one: no barrier)
+template <int NT>
+__device__ __forceinline__ void store_squares(const OrthProduct &p, int64_t matrix, uint32_t tiles, uint32_t tile, float sum) {
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) p.sq_out[(matrix * tiles + tile) * (NT / kWave) + threadIdx.x / kWave] = sum;
+}
 
 typedef uint32_t u32x4a2_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4a4_t __attribute__((ext_vector_type(4), aligned(4)));
@@ -193,12 +233,10 @@ struct OrthTiles {
     }
 };
 
-// beta D added to eight values of row m from column n on
-__device__ __forceinline__ void add_addend(const OrthProduct &p, const half_t *d, int64_t m, int64_t n, Eight &e) {
-    if (!d) return;
-    const uint4 hi = *reinterpret_cast<const uint4 *>(d + m * p.d.ld + n);
-    const uint4 lo = p.d_lo ? *reinterpret_cast<const uint4 *>(d + p.d.plane + m * p.d.ld + n) : make_uint4(0u, 0u, 0u, 0u);
-    e.add(p.beta, hi, lo);
+// `shift` off the diagonal of a tile on it
+__device__ __forceinline__ void off_diagonal(float shift, int m, int n, Eight &e) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e.v[k] -= m == n + k ? shift : 0.0f;
 }
 __device__ __forceinline__ void clear_padding(const OrthProduct &p, int64_t m, int64_t n, Eight &e) {
     if (m < p.M && n + 8 <= p.N) return;
@@ -211,14 +249,18 @@ template <typename TT> constexpr int kTurnPitch = TT::BM + 8;  // halves
 template <typename TT> constexpr int kOrthLds = TT::LDS_BYTES > TT::BN * kTurnPitch<TT> * 2 ? TT::LDS_BYTES : TT::BN * kTurnPitch<TT> * 2;
 
 // A finished tile, straight from the accumulators; of a symmetric product also its mirror image, which is turned in LDS, a
-// plane at a time (Plane: 0 the hi parts and all that goes straight out, 1 the mirror image's lo parts).
+// plane at a time (Plane: 0 the hi parts and all that goes straight out, 1 the mirror image's lo parts).  Returns the sum of
+// squares of what this thread stored (not of symmetric products).
 template <typename TT, int Plane, bool Mirror>
-__device__ __forceinline__ void store_product(typename TT::Acc &acc, const OrthProduct &p, int64_t matrix, int64_t m0, int64_t n0, char *lds) {
+__device__ __forceinline__ float store_product(typename TT::Acc &acc, const OrthProduct &p, float shift, int64_t matrix, int64_t m0, int64_t n0,
+                                               char *lds) {
+    const float beta = beta_of(p, shift), diagonal = Mirror && p.n_sq && m0 == n0 ? shift * kGramScale : 0.0f;
+    float squares = 0.0f;
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));  // not to be traced: nothing derived from it is to live through the main loop
     const int grp = lane >> 4, col = lane & 15;
     const bool mirror = Mirror && p.symmetric && m0 != n0;
-    if (Plane == 1 && !mirror) return;
+    if (Plane == 1 && !mirror) return 0.0f;
     // places inside the tile: in 32 bits (rows are at most 65600 halves)
     const int d_ld = static_cast<int>(p.d.ld), out_ld = static_cast<int>(p.out.ld);
     const half_t *d = p.d.base ? p.d.of(matrix) + m0 * p.d.ld + n0 : nullptr, *d_lo_plane = d + p.d.plane;
@@ -258,10 +300,14 @@ __device__ __forceinline__ void store_product(typename TT::Acc &acc, const OrthP
                 e.v[4 + r] = __uint_as_float(y) * p.alpha;
             }
             const int m = row(i), n = column(j);
-            if (d) e.add(p.beta, d_hi[i & 1][j], d_lo[i & 1][j]);
+            if (d) e.add(beta, d_hi[i & 1][j], d_lo[i & 1][j]);
+            if (Mirror && diagonal != 0.0f) off_diagonal(diagonal, m, n, e);
             if (!inside)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) e.v[k] = m < rows && n + k < cols ? e.v[k] : 0.0f;
+            if (!Mirror)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) squares = fmaf(e.v[k], e.v[k], squares);
             uint4 hi, lo;
             e.split(hi, lo);
             if (inside || (m < rows_p && n < cols_p)) {
@@ -278,7 +324,7 @@ __device__ __forceinline__ void store_product(typename TT::Acc &acc, const OrthP
             }
         }
     }
-    if (!mirror) return;
+    if (!mirror) return squares;
     __syncthreads();
     half_t *image = p.out.of(matrix) + n0 * p.out.ld + m0 + Plane * p.out.plane;
     for (int i = threadIdx.x; i < TT::BN * TT::BM / 8; i += TT::NT) {
@@ -286,6 +332,7 @@ __device__ __forceinline__ void store_product(typename TT::Acc &acc, const OrthP
         if (r < cols_p && c < rows_p)
             *reinterpret_cast<uint4 *>(image + (r * out_ld + c)) = *reinterpret_cast<const uint4 *>(turn + r * kTurnPitch<TT> + c);
     }
+    return squares;
 }
 
 // A finished tile of the last product: a wavefront's part in LDS, 64 rows at a time, and from there in whole lines of the
@@ -293,7 +340,7 @@ __device__ __forceinline__ void store_product(typename TT::Acc &acc, const OrthP
 constexpr int kLastPitch = 64 + 4;  // floats
 template <typename TT> constexpr int kLastLds = TT::NWAVE * 64 * kLastPitch * 4;
 template <typename TT>
-__device__ __forceinline__ void store_last_product(const typename TT::Acc &acc, const OrthProduct &p, int64_t matrix, int64_t m0, int64_t n0,
+__device__ __forceinline__ void store_last_product(const typename TT::Acc &acc, const OrthProduct &p, float beta, int64_t matrix, int64_t m0, int64_t n0,
                                                    char *lds) {
     static_assert(TT::WN == 64 && TT::WM % 64 == 0, "parts of 64 x 64");
     int lane = threadIdx.x & 63;
@@ -332,7 +379,7 @@ __device__ __forceinline__ void store_last_product(const typename TT::Acc &acc, 
                     e.v[k] = x[k] * p.alpha;
                     e.v[4 + k] = y[k] * p.alpha;
                 }
-                e.add(p.beta, hi[i], lo[i]);
+                e.add(beta, hi[i], lo[i]);
                 if (p.last.across) {
                     q[0] = f32x4_t{e.v[0], e.v[1], e.v[2], e.v[3]};
                     q[1] = f32x4_t{e.v[4], e.v[5], e.v[6], e.v[7]};
@@ -372,6 +419,8 @@ orth_product_kernel(OrthProduct p) {
     int64_t tm, tn;
     ord.at(i % tiles, tm, tn);
     const int64_t m0 = tm * TT::BM, n0 = tn * TT::BN;
+    __shared__ float scratch[TT::NWAVE];
+    const float begun = begin_shift<TT::NT>(p, matrix, scratch);
     const half_t *a = p.a.of(matrix), *b = p.b.of(matrix);
     auto A = [&](int lo) { return typename TT::Operand{reinterpret_cast<const char *>(a + lo * p.a.plane), p.a.ld * 2, m0, p.Mp, 0}; };
     auto B = [&](int lo) { return typename TT::Operand{reinterpret_cast<const char *>(b + lo * p.b.plane), p.b.ld * 2, n0, p.Np, 0}; };
@@ -386,10 +435,14 @@ orth_product_kernel(OrthProduct p) {
             for (int y = 0; y < TT::FN; ++y) acc[x][y] *= 1.0f / kLoScale;
     }
     TT::template mainloop<false, BCols, true>(A(0), B(0), p.KT, lds, acc);
-    if constexpr (Last) return store_last_product<TT>(acc, p, matrix, m0, n0, lds);
+    // (the main loop has barriers)
+    const float shift = end_shift<TT::NT>(p, matrix, scratch, begun, m0 == 0 && n0 == 0);
+    if constexpr (Last) return store_last_product<TT>(acc, p, beta_of(p, shift), matrix, m0, n0, lds);
     // (symmetric products have both operands along k)
-    store_product<TT, 0, !BCols>(acc, p, matrix, m0, n0, lds);
-    if constexpr (Split && !BCols) store_product<TT, 1, true>(acc, p, matrix, m0, n0, lds);
+    const float squares = store_product<TT, 0, !BCols>(acc, p, shift, matrix, m0, n0, lds);
+    if constexpr (Split && !BCols) store_product<TT, 1, true>(acc, p, shift, matrix, m0, n0, lds);
+    if constexpr (BCols)
+        if (p.sq_out) store_squares<TT::NT>(p, matrix, tiles, i % tiles, squares);
 }
 
 // ----------------------------------------------------------------------------
@@ -455,6 +508,22 @@ orth_few_kernel(OrthProduct p) {
 #pragma unroll
         for (int y = 0; y < F; ++y) acc[x][y] = typename T::AccBlock{0.0f, 0.0f, 0.0f, 0.0f};
     if (total > 0) request(0);
+    __shared__ float scratch[kFewWaves];
+    // meanwhile: s, and the addend of the two runs of eight values that this thread will store
+    const float begun = begin_shift<kFewThreads>(p, matrix, scratch);
+    constexpr int U = E * E / 8 / kFewThreads;
+    const half_t *d = p.d.base ? p.d.of(matrix) : nullptr;
+    uint4 d_hi[U], d_lo[U];
+    // (values that go out across: neighbouring lanes on neighbouring rows)
+    auto run_row = [&](int i) { return p.last.across ? (i * kFewThreads + static_cast<int>(threadIdx.x)) % E : (i * kFewThreads + static_cast<int>(threadIdx.x)) / (E / 8); };
+    auto run_col = [&](int i) { return 8 * (p.last.across ? (i * kFewThreads + static_cast<int>(threadIdx.x)) / E : (i * kFewThreads + static_cast<int>(threadIdx.x)) % (E / 8)); };
+    if (d)
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const half_t *q = d + (m0 + run_row(i)) * p.d.ld + n0 + run_col(i);
+            d_hi[i] = *reinterpret_cast<const uint4 *>(q);
+            d_lo[i] = p.d_lo ? *reinterpret_cast<const uint4 *>(q + p.d.plane) : make_uint4(0u, 0u, 0u, 0u);
+        }
     for (int j = 0; j < total; ++j) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const char *stage = lds + wave * kFewStage;
@@ -501,17 +570,15 @@ orth_few_kernel(OrthProduct p) {
         for (int y = 0; y < F; ++y)
             *reinterpret_cast<f32x4_t *>(sums + (wave * E + x * 16 + (lane & 15)) * kFewPitch + y * 16 + 4 * (lane >> 4)) = acc[x][y];
     __syncthreads();
-    const half_t *d = p.d.base ? p.d.of(matrix) : nullptr;
+    const float shift = end_shift<kFewThreads>(p, matrix, scratch, begun, m0 == 0 && n0 == 0), beta = beta_of(p, shift);
     half_t *out = p.out.base ? p.out.of(matrix) : nullptr;
     const bool mirror = p.symmetric && m0 != n0;
-    constexpr int U = E * E / 8 / kFewThreads;  // runs of eight values per thread
     uint4 hi[U], lo[U];
     int row[U], at[U];
+    float squares = 0.0f;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const int u = i * kFewThreads + threadIdx.x;
-        // (values that go out across: neighbouring lanes on neighbouring rows)
-        const int r = row[i] = p.last.across ? u % E : u / (E / 8), c = at[i] = (p.last.across ? u / E : u % (E / 8)) * 8;
+        const int r = row[i] = run_row(i), c = at[i] = run_col(i);
         Eight e;
 #pragma unroll
         for (int k = 0; k < 8; ++k) e.v[k] = 0.0f;
@@ -528,16 +595,20 @@ orth_few_kernel(OrthProduct p) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) e.v[k] *= p.alpha;
         const int64_t m = m0 + r, n = n0 + c;
-        add_addend(p, d, m, n, e);
+        if (d) e.add(beta, d_hi[i], d_lo[i]);
         if (p.last.out) {
             if (m < p.M) store_last(p.last, matrix, m, n, p.N, e);
             continue;
         }
+        if (p.n_sq && m0 == n0) off_diagonal(shift * kGramScale, r, c, e);
         clear_padding(p, m, n, e);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) squares = fmaf(e.v[k], e.v[k], squares);
         e.split(hi[i], lo[i]);
         *reinterpret_cast<uint4 *>(out + m * p.out.ld + n) = hi[i];
         if (p.out_lo) *reinterpret_cast<uint4 *>(out + p.out.plane + m * p.out.ld + n) = lo[i];
     }
+    if (p.sq_out) return store_squares<kFewThreads>(p, matrix, tiles, item % tiles, squares);
     if (!mirror) return;
     // the mirror image, turned in LDS (a pitch of 33 words: the writes of a wavefront on 32 different banks)
     constexpr int P = E + 2;
@@ -617,35 +688,43 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(OrthInput in, double *__
 }
 
 // scale / (|U| + eps), and 0 for a matrix of zeros; by a whole workgroup
-__device__ __forceinline__ float scale_of(const OrthInput &in, const double *part, int parts, int64_t matrix, float scale, double *scratch) {
+// sq (NULL: not): the sum of X's squares.
+__device__ __forceinline__ float scale_of(const OrthInput &in, const double *part, int parts, int64_t matrix, float scale, double *scratch, float *sq) {
     double sum = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256) sum += part[matrix * parts + i];
     const double norm = sqrt(block_sum(sum, scratch));
     const double whole = norm + static_cast<double>(in.eps);
-    return whole > 0.0 ? static_cast<float>(scale / whole) : whole == 0.0 ? 0.0f : __builtin_nanf("");
+    const float f = whole > 0.0 ? static_cast<float>(scale / whole) : whole == 0.0 ? 0.0f : __builtin_nanf("");
+    if (sq && blockIdx.x == 0 && threadIdx.x == 0) sq[matrix] = static_cast<float>((norm * f) * (norm * f));
+    return f;
 }
 
 // X = scale * U / (|U| + eps) as pairs of halves, zero in the padding; with last.out: U / (|U| + eps) goes there (no steps)
 __global__ void __launch_bounds__(256) orth_scale_kernel(OrthInput in, const double *__restrict__ part, int parts, float scale, Stack X,
-                                                         int64_t rows_p, OrthOut last) {
+                                                         int64_t rows_p, OrthOut last, float *__restrict__ sq) {
     __shared__ double scratch[4];
     const int64_t matrix = blockIdx.y;
-    const float f = scale_of(in, part, parts, matrix, last.out ? 1.0f : scale, scratch);
-    const int64_t per_row = X.ld / 8, n = rows_p * per_row;
+    const int64_t per_row = X.ld / 8, n = rows_p * per_row, stride = static_cast<int64_t>(gridDim.x) * 256;
+    auto load = [&](int64_t i, float (&u)[8]) {
+        const int64_t r = i / per_row, c = i % per_row * 8;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[k] = 0.0f;
+        if (i < n && r < in.rows && c < in.cols) load_update<false>(in, matrix, r, c, u);
+    };
+    int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    float u[8];
+    load(i, u);  // on their way while the norm is formed
+    const float f = scale_of(in, part, parts, matrix, last.out ? 1.0f : scale, scratch, sq);
     half_t *x = X.of(matrix);
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    while (i < n) {
         const int64_t r = i / per_row, c = i % per_row * 8;
         Eight e;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) e.v[k] = 0.0f;
-        const bool inside = r < in.rows && c < in.cols;
-        if (inside) {
-            load_update<false>(in, matrix, r, c, e.v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) e.v[k] *= f;
-        }
+        for (int k = 0; k < 8; ++k) e.v[k] = u[k] * f;
+        i += stride;
+        load(i, u);
         if (last.out) {
-            if (inside) store_last(last, matrix, r, c, in.cols, e);
+            if (r < in.rows && c < in.cols) store_last(last, matrix, r, c, in.cols, e);
             continue;
         }
         uint4 hi, lo;
@@ -657,19 +736,23 @@ __global__ void __launch_bounds__(256) orth_scale_kernel(OrthInput in, const dou
 
 // The same for matrices with more rows than columns: X gets their transpose, 64 x 64 entries by a workgroup through LDS.
 __global__ void __launch_bounds__(256) orth_scale_turned_kernel(OrthInput in, const double *__restrict__ part, int parts, float scale, Stack X,
-                                                                unsigned across) {
+                                                                unsigned across, float *__restrict__ sq) {
     __shared__ double scratch[4];
     __shared__ float turn[64][65];
     const int64_t matrix = blockIdx.y;
-    const float f = scale_of(in, part, parts, matrix, scale, scratch);
     const int64_t r0 = blockIdx.x % across * 64, c0 = blockIdx.x / across * 64;  // of U; across: tiles along X's rows
+    float v[2][8] = {};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {  // on their way while the norm is formed
+        const int u = i * 256 + threadIdx.x, r = u / 8, c = u % 8 * 8;
+        if (r0 + r < in.rows && c0 + c < in.cols) load_update<false>(in, matrix, r0 + r, c0 + c, v[i]);
+    }
+    const float f = scale_of(in, part, parts, matrix, scale, scratch, sq);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int u = i * 256 + threadIdx.x, r = u / 8, c = u % 8 * 8;
-        float v[8] = {};
-        if (r0 + r < in.rows && c0 + c < in.cols) load_update<false>(in, matrix, r0 + r, c0 + c, v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) turn[r][c + k] = v[k] * f;
+        for (int k = 0; k < 8; ++k) turn[r][c + k] = v[i][k] * f;
     }
     __syncthreads();
     half_t *x = X.of(matrix);
@@ -695,6 +778,7 @@ struct OrthPlan {
     int64_t k, L, kp, Lp;  // the smaller and the larger side, and both padded: X is k x L
     int parts;
     double *norm;
+    float *sq, *shift;     // see OrthProduct
     Stack X[2], A, B;
     float x_scale;
     size_t bytes;
@@ -713,6 +797,8 @@ static OrthPlan plan_orth(const spo_orth_desc *d, void *ws) {
     p.parts = static_cast<int>(std::min<int64_t>(kNormParts, ceil_div(vectors, 256 * 2)));
     Arena a(ws);
     p.norm = a.take<double>(static_cast<size_t>(d->batch) * kNormParts);
+    p.sq = a.take<float>(static_cast<size_t>(d->batch) * (p.kp / kFewEdge) * (p.Lp / kFewEdge) * kFewWaves);  // (other tiles: fewer)
+    p.shift = a.take<float>(d->batch);
     auto stack = [&](int64_t rows, int64_t ld) {
         Stack s{nullptr, ld, rows * ld, 2 * rows * ld};
         s.base = a.take<half_t>(static_cast<size_t>(d->batch) * 2 * rows * ld);
@@ -781,7 +867,7 @@ static Kind product_kind(const OrthProduct &p, bool middle) {
     const int64_t tiles = OrthTiles(p.Mp, p.Np, kFewEdge, p.symmetric).tiles() * p.batch;
     const double halves = std::max(1.0, static_cast<double>(ceil_div(2 * tiles, kChipCUs)) * 0.5);
     Kind best = Kind::few;
-    double least = 4.0 + halves * (steps * 0.2 + 1.7);
+    double least = 4.0 + halves * (steps * 0.2 + 2.4);
     auto offer = [&](Kind k, const OrthTimes &t) {
         const double time = product_time(t, p, steps);
         if (time < least) {
@@ -794,12 +880,15 @@ static Kind product_kind(const OrthProduct &p, bool middle) {
     offer(Kind::large, kLargeTimes);
     return best;
 }
+static int64_t edge_of(Kind k) {
+    return k == Kind::few ? kFewEdge : k == Kind::small ? kSmallTimes.edge : k == Kind::middle ? kMiddleTimes.edge : kLargeTimes.edge;
+}
+static int waves_of(Kind k) { return k == Kind::few ? kFewWaves : k == Kind::small ? OS::NWAVE : k == Kind::middle ? OM::NWAVE : OL::NWAVE; }
 template <bool BCols>
-static int launch_product(const OrthProduct &p, hipStream_t s) {
-    const Kind kind = product_kind(p, !BCols);  // (tiles of 192 take rows along the contraction only)
+static int launch_product(const OrthProduct &p, Kind kind, hipStream_t s) {
     if (kind == Kind::few) return launch_few<BCols>(p, s);
     if (kind == Kind::small) return launch_tiles<OS, BCols>(p, s);
-    if constexpr (!BCols)
+    if constexpr (!BCols)  // (tiles of 192 take rows along the contraction only)
         if (kind == Kind::middle) return launch_tiles<OM, BCols>(p, s);
     return launch_tiles<OL, BCols>(p, s);
 }
@@ -812,55 +901,67 @@ static int run_orth(const spo_orth_desc *d, const OrthInput &in, OrthOut last, v
     orth_norm_kernel<<<dim3(static_cast<unsigned>(p.parts), batch), 256, 0, s>>>(in, p.norm);
     if (tall && d->steps) {
         orth_scale_turned_kernel<<<dim3(static_cast<unsigned>(p.Lp / 64 * (p.kp / 64)), batch), 256, 0, s>>>(in, p.norm, p.parts, p.x_scale,
-                                                                                                           p.X[0], static_cast<unsigned>(p.Lp / 64));
+                                                                                                           p.X[0], static_cast<unsigned>(p.Lp / 64), p.sq);
     } else {
         const int64_t vectors = p.kp * p.Lp / 8;
         const int64_t x_rows = d->steps ? p.kp : d->rows;
         orth_scale_kernel<<<dim3(static_cast<unsigned>(std::min<int64_t>(1024, ceil_div(vectors, 256))), batch), 256, 0, s>>>(
-            in, p.norm, p.parts, p.x_scale, p.X[0], x_rows, d->steps ? OrthOut{} : last);
+            in, p.norm, p.parts, p.x_scale, p.X[0], x_rows, d->steps ? OrthOut{} : last, p.sq);
     }
     last.across = tall;
     // Where the smaller side is one step of the contraction, launches are all that counts, and so few roundings do not
     // average out (one of 1 x 1: 4e-3): always pairs.
     const bool split = d->products == SPO_PRODUCTS_SPLIT || p.k <= kBK;
+    // A' = X X^T - s I
+    OrthProduct gram{};
+    gram.batch = d->batch;
+    gram.split = gram.d_lo = gram.out_lo = split;
+    gram.shift = p.shift;
+    gram.symmetric = 1;
+    gram.out = p.A;
+    gram.M = gram.N = p.k;
+    gram.Mp = gram.Np = p.kp;
+    gram.KT = static_cast<int>(p.Lp / kBK);
+    gram.alpha = kGramScale / (p.x_scale * p.x_scale);
+    gram.sq = p.sq;
+    gram.sq_scale = 1.0f / (p.x_scale * p.x_scale * static_cast<float>(p.k));
+    // B' = (b + 2 c s) A' + c A' A'; A' is symmetric, so its rows serve as columns
+    OrthProduct poly = gram;
+    poly.n_sq = 0;
+    poly.a = poly.b = poly.d = p.A;
+    poly.out = p.B;
+    poly.KT = static_cast<int>(p.kp / kBK);
+    poly.alpha = d->c / kGramScale;
+    poly.c[0] = d->b;
+    poly.c[1] = 2.0f * d->c;
+    // X <- (a + b s + c s^2) X + B' X
+    OrthProduct update = poly;
+    update.symmetric = 0;
+    update.a = p.B;
+    update.d_lo = update.out_lo = 1;
+    update.N = p.L;
+    update.Np = p.Lp;
+    update.alpha = 1.0f / kGramScale;
+    update.c[0] = d->a;
+    update.c[1] = d->b;
+    update.c[2] = d->c;
+    update.sq_out = p.sq;
+    const Kind gram_kind = product_kind(gram, true), poly_kind = product_kind(poly, true), update_kind = product_kind(update, false);
     for (int i = 0; i < d->steps; ++i) {
         const Stack &X = p.X[i & 1];
-        OrthProduct q{};
-        q.batch = d->batch;
-        q.split = split;
-        q.d_lo = q.out_lo = split;
-        // A = X X^T
-        q.symmetric = 1;
-        q.a = q.b = X;
-        q.out = p.A;
-        q.M = q.N = p.k;
-        q.Mp = q.Np = p.kp;
-        q.KT = static_cast<int>(p.Lp / kBK);
-        q.alpha = kGramScale / (p.x_scale * p.x_scale);
-        if (int rc = launch_product<false>(q, s)) return rc;
-        // B = b A + c A A; A is symmetric, so its rows serve as columns
-        q.a = q.b = q.d = p.A;
-        q.out = p.B;
-        q.KT = static_cast<int>(p.kp / kBK);
-        q.alpha = d->c / kGramScale;
-        q.beta = d->b;
-        if (int rc = launch_product<false>(q, s)) return rc;
-        // X <- a X + B X
-        q.symmetric = 0;
-        q.a = p.B;
-        q.b = q.d = X;
-        q.d_lo = q.out_lo = 1;
-        q.out = p.X[(i + 1) & 1];
-        q.N = p.L;
-        q.Np = p.Lp;
-        q.alpha = 1.0f / kGramScale;
-        q.beta = d->a;
+        gram.a = gram.b = X;
+        gram.n_sq = i == 0 ? 1 : static_cast<int>(OrthTiles(p.kp, p.Lp, edge_of(update_kind), false).tiles()) * waves_of(update_kind);
+        if (int rc = launch_product<false>(gram, gram_kind, s)) return rc;
+        if (int rc = launch_product<false>(poly, poly_kind, s)) return rc;
+        update.b = update.d = X;
+        update.out = p.X[(i + 1) & 1];
         if (i == d->steps - 1) {
-            q.alpha /= p.x_scale;
-            q.beta /= p.x_scale;
-            q.last = last;
+            update.alpha /= p.x_scale;
+            for (float &c : update.c) c /= p.x_scale;
+            update.sq_out = nullptr;
+            update.last = last;
         }
-        if (int rc = launch_product<true>(q, s)) return rc;
+        if (int rc = launch_product<true>(update, update_kind, s)) return rc;
     }
     return launch_status();
 }
