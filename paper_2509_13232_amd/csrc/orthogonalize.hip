@@ -452,14 +452,20 @@ orth_product_kernel(OrthProduct p) {
 // order at the end.  What bounds a small product is the way of its operands: a step of the main loop above cannot be
 // shorter than one round trip to the L2s (0.57 us), here each wavefront has a stage of its own, waits for nobody, and eight
 // steps are on their way per compute unit (two workgroups; with two stages per wavefront and one workgroup no product was
-// faster); a wavefront reads 16 KB of LDS per 32 matrix instructions (tiles shared between wavefronts: twice that).  The sides of all matrices are multiples of 64, so nothing here has an end to look after.
+// faster); a wavefront reads 16 KB of LDS per 32 matrix instructions (tiles shared between wavefronts: twice that).  The
+// sides of all matrices are multiples of 64, so nothing here has an end to look after.
 constexpr int kFewEdge = 64, kFewWaves = 4, kFewThreads = kFewWaves * kWave;
-constexpr int kFewStage = 2 * kFewEdge * kRowBytes;  // bytes: 64 rows of both operands
+constexpr int kFewPanel = kFewEdge * kRowBytes;  // bytes: 64 rows of an operand (of one plane)
 constexpr int kFewPitch = kFewEdge + 4;              // floats, of a wavefront's sums
-constexpr int kFewLds = kFewWaves * (kFewStage > kFewEdge * kFewPitch * 4 ? kFewStage : kFewEdge * kFewPitch * 4);
+constexpr int kFewSums = kFewEdge * kFewPitch * 4;
+constexpr int few_stage(bool pairs) { return (pairs ? 4 : 2) * kFewPanel; }
+constexpr int few_lds(bool pairs) { return kFewWaves * (few_stage(pairs) > kFewSums ? few_stage(pairs) : kFewSums); }
 
-template <bool BCols>
-__global__ void __launch_bounds__(kFewThreads, 2)
+// Pairs: a stage holds both planes of both operands, read once for the three products; one workgroup per compute unit then.
+// (Two workgroups, each product with a stage of its own: 704 x 704 x 47 steps 31 us instead of 25, 1024 x 1024 x 16 14.6
+// instead of 14.0, 1536 x 1536 x 24 symmetric 33 either way.)
+template <bool BCols, bool Pairs>
+__global__ void __launch_bounds__(kFewThreads, Pairs ? 1 : 2)
 orth_few_kernel(OrthProduct p) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef Tile<256, 256, 2, 4, _Float16> T;  // its transfers and instruction
@@ -481,7 +487,9 @@ orth_few_kernel(OrthProduct p) {
     const char *a = reinterpret_cast<const char *>(p.a.of(matrix)) + m0 * lda;
     const char *b = reinterpret_cast<const char *>(p.b.of(matrix)) + (BCols ? n0 * 2 : n0 * ldb);
     const int64_t step_a = ROWS, step_b = BCols ? E * ldb : ROWS;
-    const uint32_t ring = T::lds_address(lds) + wave * kFewStage;
+    constexpr int PLANES = Pairs ? 2 : 1;
+    const char *stage = lds + wave * few_stage(Pairs);  // panels: A (hi, lo), B (hi, lo)
+    const uint32_t ring = T::lds_address(stage);
     auto cols_swizzle = [](int r) { return (r & 3) << 1; };  // columns along k: pieces of four rows on distinct banks
     uint32_t off_a[2], off_b[2];  // of rows 0..7 and 8..15 of sixteen
 #pragma unroll
@@ -490,24 +498,28 @@ orth_few_kernel(OrthProduct p) {
         off_a[h] = static_cast<uint32_t>((lane >> 3) * lda) + static_cast<uint32_t>((c ^ swz(r)) * 16);
         off_b[h] = static_cast<uint32_t>((lane >> 3) * ldb) + static_cast<uint32_t>((c ^ (BCols ? cols_swizzle(r) : swz(r))) * 16);
     }
-    // step j of this wavefront: with pairs first all hi lo, then all lo hi, then all hi hi
-    const int mine = (p.KT - wave + kFewWaves - 1) / kFewWaves, terms = p.split ? 3 : 1, total = mine * terms;
+    const int mine = (p.KT - wave + kFewWaves - 1) / kFewWaves;  // steps of this wavefront
     auto request = [&](int j) {
-        const int term = p.split ? j / mine : 2, kt = wave + kFewWaves * (j - (p.split ? term * mine : 0));
-        const char *ga = T::uniform(a + (term == 1 ? p.a.plane * 2 : 0) + kt * step_a);
-        const char *gb = T::uniform(b + (term == 0 ? p.b.plane * 2 : 0) + kt * step_b);
+        const int kt = wave + kFewWaves * j;
         const uint32_t to = __builtin_amdgcn_readfirstlane(ring);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) T::dma(ga + i * 8 * lda, off_a[i & 1], to + i * 1024);
+        for (int plane = 0; plane < PLANES; ++plane) {
+            const char *ga = T::uniform(a + plane * p.a.plane * 2 + kt * step_a), *gb = T::uniform(b + plane * p.b.plane * 2 + kt * step_b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) T::dma(gb + i * 8 * ldb, off_b[i & 1], to + E * ROWS + i * 1024);
+            for (int i = 0; i < 8; ++i) T::dma(ga + i * 8 * lda, off_a[i & 1], to + plane * kFewPanel + i * 1024);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) T::dma(gb + i * 8 * ldb, off_b[i & 1], to + (PLANES + plane) * kFewPanel + i * 1024);
+        }
     };
-    typename T::AccBlock acc[F][F];
+    typename T::AccBlock acc[F][F], cross[Pairs ? F : 1][Pairs ? F : 1];  // cross: hi lo + lo hi
 #pragma unroll
     for (int x = 0; x < F; ++x)
 #pragma unroll
-        for (int y = 0; y < F; ++y) acc[x][y] = typename T::AccBlock{0.0f, 0.0f, 0.0f, 0.0f};
-    if (total > 0) request(0);
+        for (int y = 0; y < F; ++y) {
+            acc[x][y] = typename T::AccBlock{0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (Pairs) cross[x][y] = acc[x][y];
+        }
+    if (mine > 0) request(0);
     __shared__ float scratch[kFewWaves];
     // meanwhile: s, and the addend of the two runs of eight values that this thread will store
     const float begun = begin_shift<kFewThreads>(p, matrix, scratch);
@@ -524,43 +536,51 @@ orth_few_kernel(OrthProduct p) {
             d_hi[i] = *reinterpret_cast<const uint4 *>(q);
             d_lo[i] = p.d_lo ? *reinterpret_cast<const uint4 *>(q + p.d.plane) : make_uint4(0u, 0u, 0u, 0u);
         }
-    for (int j = 0; j < total; ++j) {
+    for (int j = 0; j < mine; ++j) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const char *stage = lds + wave * kFewStage;
-        bf16x8_t fa[2][F], fb[2][F];
+        bf16x8_t fa[PLANES][2][F], fb[PLANES][2][F];
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            const int chunk = ((4 * kk + (lane >> 4)) ^ swz(lane & 15)) * 16 + (lane & 15) * ROWS;
+        for (int plane = 0; plane < PLANES; ++plane)
 #pragma unroll
-            for (int f = 0; f < F; ++f) fa[kk][f] = *reinterpret_cast<const bf16x8_t *>(stage + f * 16 * ROWS + chunk);
+            for (int kk = 0; kk < 2; ++kk) {
+                const int chunk = ((4 * kk + (lane >> 4)) ^ swz(lane & 15)) * 16 + (lane & 15) * ROWS;
+                const char *pa = stage + plane * kFewPanel, *pb = stage + (PLANES + plane) * kFewPanel;
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                if constexpr (BCols) {  // see Tile::Side
-                    const int row = 32 * kk + 8 * (lane >> 4) + ((lane & 15) >> 2), col = f * 16 + 4 * (lane & 3);
-                    const uint32_t at = T::lds_address(stage) + E * ROWS + row * ROWS + (((col >> 3) ^ cols_swizzle(row)) << 4) + ((col >> 2) & 1) * 8;
-                    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(uintptr_t)at);
-                    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(uintptr_t)(at + 4 * ROWS));
-                    fb[kk][f] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                } else {
-                    fb[kk][f] = *reinterpret_cast<const bf16x8_t *>(stage + E * ROWS + f * 16 * ROWS + chunk);
+                for (int f = 0; f < F; ++f) fa[plane][kk][f] = *reinterpret_cast<const bf16x8_t *>(pa + f * 16 * ROWS + chunk);
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    if constexpr (BCols) {  // see Tile::Side
+                        const int row = 32 * kk + 8 * (lane >> 4) + ((lane & 15) >> 2), col = f * 16 + 4 * (lane & 3);
+                        const uint32_t at = T::lds_address(pb) + row * ROWS + (((col >> 3) ^ cols_swizzle(row)) << 4) + ((col >> 2) & 1) * 8;
+                        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(uintptr_t)at);
+                        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3))) *)(uintptr_t)(at + 4 * ROWS));
+                        fb[plane][kk][f] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    } else {
+                        fb[plane][kk][f] = *reinterpret_cast<const bf16x8_t *>(pb + f * 16 * ROWS + chunk);
+                    }
                 }
             }
-        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage is in registers: its place may be written
         __builtin_amdgcn_sched_barrier(0);
-        if (j + 1 < total) request(j + 1);
-        if (p.split && j == 2 * mine)
-#pragma unroll
-            for (int x = 0; x < F; ++x)
-#pragma unroll
-                for (int y = 0; y < F; ++y) acc[x][y] *= 1.0f / kLoScale;
+        if (j + 1 < mine) request(j + 1);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int x = 0; x < F; ++x)
 #pragma unroll
-                for (int y = 0; y < F; ++y) acc[x][y] = T::template mfma<true>(fa[kk][x], fb[kk][y], acc[x][y]);
+                for (int y = 0; y < F; ++y) {
+                    acc[x][y] = T::template mfma<true>(fa[0][kk][x], fb[0][kk][y], acc[x][y]);
+                    if constexpr (Pairs) {
+                        cross[x][y] = T::template mfma<true>(fa[0][kk][x], fb[1][kk][y], cross[x][y]);
+                        cross[x][y] = T::template mfma<true>(fa[1][kk][x], fb[0][kk][y], cross[x][y]);
+                    }
+                }
     }
+    if constexpr (Pairs)
+#pragma unroll
+        for (int x = 0; x < F; ++x)
+#pragma unroll
+            for (int y = 0; y < F; ++y) acc[x][y] += cross[x][y] * (1.0f / kLoScale);
     // the wavefronts' sums in LDS: lane l holds row l % 16 and columns 4 (l / 16) .. of a block
     __syncthreads();
     float *sums = reinterpret_cast<float *>(lds);
@@ -826,12 +846,12 @@ static int launch_tiles(const OrthProduct &p, hipStream_t s) {
     kernel<<<static_cast<unsigned>(TileOrder::blocks(items)), TT::NT, lds, s>>>(p);
     return SPO_OK;
 }
-template <bool BCols>
+template <bool BCols, bool Pairs>
 static int launch_few(const OrthProduct &p, hipStream_t s) {
-    auto *kernel = orth_few_kernel<BCols>;
-    if (int rc = allow_lds(kernel, kFewLds)) return rc;
+    auto *kernel = orth_few_kernel<BCols, Pairs>;
+    if (int rc = allow_lds(kernel, few_lds(Pairs))) return rc;
     const int64_t items = OrthTiles(p.Mp, p.Np, kFewEdge, p.symmetric).tiles() * p.batch;
-    kernel<<<static_cast<unsigned>(TileOrder::blocks(items)), kFewThreads, kFewLds, s>>>(p);
+    kernel<<<static_cast<unsigned>(TileOrder::blocks(items)), kFewThreads, few_lds(Pairs), s>>>(p);
     return SPO_OK;
 }
 template <typename TT, bool BCols>
@@ -842,7 +862,7 @@ static int launch_tiles(const OrthProduct &p, hipStream_t s) {
 // four of 1024 x 4096, both kinds of products; within a fifth of it but for launches of a few us):
 //   tiles shared by wavefronts: rounds of workgroups on the chip x (steps x time of a step + the tile's ends); a step slows
 //   down as the chip fills up.  Half of the time that the addend and the output take from and to memory comes on top.
-//   a share of the contraction per wavefront: half rounds of a tile per compute unit.
+//   a share of the contraction per wavefront: half rounds of a tile per compute unit, with pairs whole ones.
 // So 64 x 64 x 64 (k, L, steps) takes 5 us instead of 7, 1024 x 1024 x 16 8.8 instead of 14 (128), 48 steps 14 instead of 33;
 // 2048 x 2048 x 32 24 on tiles of 128 (64: 25, 192: 31), 4096 x 4096 x 64 symmetric 73 on 192 (253 tiles on 256 compute units;
 // 85 on 256, 99 on 128), otherwise 118 on 256.
@@ -867,7 +887,7 @@ static Kind product_kind(const OrthProduct &p, bool middle) {
     const int64_t tiles = OrthTiles(p.Mp, p.Np, kFewEdge, p.symmetric).tiles() * p.batch;
     const double halves = std::max(1.0, static_cast<double>(ceil_div(2 * tiles, kChipCUs)) * 0.5);
     Kind best = Kind::few;
-    double least = 4.0 + halves * (steps * 0.2 + 2.4);
+    double least = p.split ? 4.0 + static_cast<double>(ceil_div(tiles, kChipCUs)) * (p.KT * 0.475 + 2.4) : 4.0 + halves * (steps * 0.2 + 2.4);
     auto offer = [&](Kind k, const OrthTimes &t) {
         const double time = product_time(t, p, steps);
         if (time < least) {
@@ -886,7 +906,7 @@ static int64_t edge_of(Kind k) {
 static int waves_of(Kind k) { return k == Kind::few ? kFewWaves : k == Kind::small ? OS::NWAVE : k == Kind::middle ? OM::NWAVE : OL::NWAVE; }
 template <bool BCols>
 static int launch_product(const OrthProduct &p, Kind kind, hipStream_t s) {
-    if (kind == Kind::few) return launch_few<BCols>(p, s);
+    if (kind == Kind::few) return p.split ? launch_few<BCols, true>(p, s) : launch_few<BCols, false>(p, s);
     if (kind == Kind::small) return launch_tiles<OS, BCols>(p, s);
     if constexpr (!BCols)  // (tiles of 192 take rows along the contraction only)
         if (kind == Kind::middle) return launch_tiles<OM, BCols>(p, s);
