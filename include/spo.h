@@ -409,11 +409,14 @@ int spo_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *en
  * products in the way of the Muon optimiser).  For each of `batch` matrices U of rows x cols:
  *   X <- U / (|U|_F + eps);  `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X
  * (A = X^T X on the other side where rows > cols), which moves every singular value towards one
- * and keeps the singular vectors.  A zero matrix stays zero.
+ * and keeps the singular vectors.  A zero matrix stays zero; an infinity or a NaN in U makes its
+ * matrix NaN.
  * products  SPO_PRODUCTS_FP16: the operands of the products are rounded to 11 bits, X itself is
- *           kept in 22: results to about 1.5e-3 relative (in 2-norm over the matrix; matrices
+ *           kept in 22: results to 2e-4 to 8e-4 relative (in 2-norm over the matrix; matrices
  *           whose smaller side is at most 64 are worked on as with SPO_PRODUCTS_SPLIT);
  *           SPO_PRODUCTS_SPLIT: operands of 22 bits, three products for one: about 1e-6.
+ * A and the polynomial b A + c A A are held in fp16 parts scaled by 256: coefficients have to keep
+ * their entries below 255 (in common use those of A stay below 1.5, the polynomial's below 3).
  * Sums are in fp32 in a fixed order: results are bitwise reproducible.
  * ------------------------------------------------------------------------- */
 #define SPO_PRODUCTS_FP16 0

@@ -697,24 +697,25 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(OrthInput in, double *__
     double sum = 0.0;
 #pragma unroll 2
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
-        float u[8], s = 0.0f;
+        float u[8];
         load_update<true>(in, matrix, i / per_row, i % per_row * 8, u);
+        double s[2] = {0.0, 0.0};  // (in 64 bits: any fp32 entry's square is a number there)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s = fmaf(u[k], u[k], s);
-        sum += s;
+        for (int k = 0; k < 8; ++k) s[k & 1] = fma(static_cast<double>(u[k]), static_cast<double>(u[k]), s[k & 1]);
+        sum += s[0] + s[1];
     }
     sum = block_sum(sum, scratch);
     if (threadIdx.x == 0) part[matrix * gridDim.x + blockIdx.x] = sum;
 }
 
-// scale / (|U| + eps), and 0 for a matrix of zeros; by a whole workgroup
+// scale / (|U| + eps), 0 for a matrix of zeros, NaN for one with an infinity or a NaN; by a whole workgroup
 // sq (NULL: not): the sum of X's squares.
-__device__ __forceinline__ float scale_of(const OrthInput &in, const double *part, int parts, int64_t matrix, float scale, double *scratch, float *sq) {
+__device__ __forceinline__ double scale_of(const OrthInput &in, const double *part, int parts, int64_t matrix, float scale, double *scratch, float *sq) {
     double sum = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256) sum += part[matrix * parts + i];
     const double norm = sqrt(block_sum(sum, scratch));
     const double whole = norm + static_cast<double>(in.eps);
-    const float f = whole > 0.0 ? static_cast<float>(scale / whole) : whole == 0.0 ? 0.0f : __builtin_nanf("");
+    const double f = whole == 0.0 ? 0.0 : whole < __builtin_inf() ? scale / whole : __builtin_nan("");
     if (sq && blockIdx.x == 0 && threadIdx.x == 0) sq[matrix] = static_cast<float>((norm * f) * (norm * f));
     return f;
 }
@@ -734,13 +735,13 @@ __global__ void __launch_bounds__(256) orth_scale_kernel(OrthInput in, const dou
     int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     float u[8];
     load(i, u);  // on their way while the norm is formed
-    const float f = scale_of(in, part, parts, matrix, last.out ? 1.0f : scale, scratch, sq);
+    const double f = scale_of(in, part, parts, matrix, last.out ? 1.0f : scale, scratch, sq);
     half_t *x = X.of(matrix);
     while (i < n) {
         const int64_t r = i / per_row, c = i % per_row * 8;
         Eight e;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) e.v[k] = u[k] * f;
+        for (int k = 0; k < 8; ++k) e.v[k] = static_cast<float>(u[k] * f);
         i += stride;
         load(i, u);
         if (last.out) {
@@ -767,12 +768,12 @@ __global__ void __launch_bounds__(256) orth_scale_turned_kernel(OrthInput in, co
         const int u = i * 256 + threadIdx.x, r = u / 8, c = u % 8 * 8;
         if (r0 + r < in.rows && c0 + c < in.cols) load_update<false>(in, matrix, r0 + r, c0 + c, v[i]);
     }
-    const float f = scale_of(in, part, parts, matrix, scale, scratch, sq);
+    const double f = scale_of(in, part, parts, matrix, scale, scratch, sq);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int u = i * 256 + threadIdx.x, r = u / 8, c = u % 8 * 8;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) turn[r][c + k] = v[i][k] * f;
+        for (int k = 0; k < 8; ++k) turn[r][c + k] = static_cast<float>(v[i][k] * f);
     }
     __syncthreads();
     half_t *x = X.of(matrix);
