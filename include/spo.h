@@ -364,7 +364,7 @@ int spo_pg_loss_fwd_bwd(const spo_pg_desc *d, float grad_loss, float *loss, floa
  * top_id is -1, their gradients are zeros.  (The head form multiplies them along with the others in
  * the forward, not in the backward.)
  * A row whose logits are all -inf has lse = -inf, and logp, entropy, top_logp NaN; its top_id are
- * the lowest ids.  A row with a NaN has NaN in all of them, and some ids.
+ * the lowest ids.  A row with a NaN or +inf has NaN in all of them, and some ids.
  * ------------------------------------------------------------------------- */
 #define SPO_MAX_TOP_K 64
 typedef struct {
@@ -393,7 +393,7 @@ int spo_logprob_fwd(const spo_logprob_desc *d, float *logp, float *lse, float *e
 /* Backward.  lse, entropy, top_id: from the forward of the same desc; entropy is needed with
  * d_entropy, top_id with d_top_logp.  d_logp, d_entropy [T] and d_top_logp [T][top_k] fp32: each may
  * be NULL for zeros; d_logp needs a target.
- * Logits-in form: d_logits [T, V] in desc dtype, rows V apart; ws is not needed.
+ * Logits-in form: d_logits [T, V] in desc dtype, rows V apart, not on top of logits; ws is not needed.
  * Head form: d_hidden, d_W, accumulate_dW, chunk_tokens and the workspace are those of
  * spo_pg_loss_bwd; tokens whose factors are both zero are left out of all contractions.  Logit
  * gradients are rounded to bf16 between the contractions, so desc dtype has to be SPO_BF16
