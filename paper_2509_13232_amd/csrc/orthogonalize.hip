@@ -693,10 +693,11 @@ __device__ __forceinline__ void load_update(const OrthInput &in, int64_t matrix,
 // part[matrix][workgroup] = sum of squares of its share of U
 __global__ void __launch_bounds__(256) orth_norm_kernel(OrthInput in, double *__restrict__ part) {
     __shared__ double scratch[4];
-    const int64_t matrix = blockIdx.y, per_row = ceil_div(in.cols, 8), n = in.rows * per_row;
+    const int64_t matrix = blockIdx.y;
+    const uint32_t per_row = static_cast<uint32_t>(ceil_div(in.cols, 8)), n = static_cast<uint32_t>(in.rows) * per_row;  // (2^29 at most)
     double sum = 0.0;
 #pragma unroll 2
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
         float u[8];
         load_update<true>(in, matrix, i / per_row, i % per_row * 8, u);
         double s[2] = {0.0, 0.0};  // (in 64 bits: any fp32 entry's square is a number there)
@@ -725,14 +726,14 @@ __global__ void __launch_bounds__(256) orth_scale_kernel(OrthInput in, const dou
                                                          int64_t rows_p, OrthOut last, float *__restrict__ sq) {
     __shared__ double scratch[4];
     const int64_t matrix = blockIdx.y;
-    const int64_t per_row = X.ld / 8, n = rows_p * per_row, stride = static_cast<int64_t>(gridDim.x) * 256;
-    auto load = [&](int64_t i, float (&u)[8]) {
+    const uint32_t per_row = static_cast<uint32_t>(X.ld / 8), n = static_cast<uint32_t>(rows_p) * per_row, stride = gridDim.x * 256;
+    auto load = [&](uint32_t i, float (&u)[8]) {
         const int64_t r = i / per_row, c = i % per_row * 8;
 #pragma unroll
         for (int k = 0; k < 8; ++k) u[k] = 0.0f;
         if (i < n && r < in.rows && c < in.cols) load_update<false>(in, matrix, r, c, u);
     };
-    int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    uint32_t i = blockIdx.x * 256 + threadIdx.x;
     float u[8];
     load(i, u);  // on their way while the norm is formed
     const double f = scale_of(in, part, parts, matrix, last.out ? 1.0f : scale, scratch, sq);
