@@ -73,9 +73,8 @@ __device__ __forceinline__ int swz(int row) {
 // MI is the edge of the MFMA block: 16 for v_mfma_f32_16x16x32_bf16, the instruction the
 // main loop is written for.  (The same tile on v_mfma_f32_32x32x16_bf16, with two
 // phase-shifted groups of wavefronts, was 4-6 % slower on the same chip.)
-// Elt: __bf16, or _Float16 (v_mfma_f32_16x16x32_f16, of the same shape and rate): 16 bits each, so all but the
-// instruction is the same.
-template <int BM_, int BN_, int WGM_, int WGN_, typename Elt = __bf16, int MI_ = 16>
+// Half: fp16 instead of bf16 (v_mfma_f32_16x16x32_f16, of the same shape and rate): all but the instruction is the same.
+template <int BM_, int BN_, int WGM_, int WGN_, int MI_ = 16, bool Half = false>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, MI = MI_;
     static_assert(MI == 16, "the main loop issues 16x16x32 MFMAs");
@@ -339,7 +338,7 @@ struct Tile {
 
     template <bool Across>
     __device__ static __forceinline__ AccBlock mfma(const bf16x8_t &a, const bf16x8_t &b, const AccBlock &c) {
-        if constexpr (std::is_same_v<Elt, _Float16>) {
+        if constexpr (Half) {
             const f16x8_t x = __builtin_bit_cast(f16x8_t, a), y = __builtin_bit_cast(f16x8_t, b);
             return Across ? __builtin_amdgcn_mfma_f32_16x16x32_f16(y, x, c, 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
         }

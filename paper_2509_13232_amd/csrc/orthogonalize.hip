@@ -23,9 +23,9 @@
 namespace spo {
 
 // Tiles that the wavefronts of a workgroup share; symmetric products also take the middle ones.
-typedef Tile<256, 256, 2, 4, _Float16> OL;
-typedef Tile<192, 192, 4, 2, _Float16> OM;
-typedef Tile<128, 128, 2, 2, _Float16> OS;
+typedef Tile<256, 256, 2, 4, 16, true> OL;
+typedef Tile<192, 192, 4, 2, 16, true> OM;
+typedef Tile<128, 128, 2, 2, 16, true> OS;
 
 constexpr float kLoScale = 2048.0f;   // lo parts are held that much larger: as far above fp16's smallest numbers as hi parts
 constexpr float kGramScale = 256.0f;  // A and B: their entries stay below about 10
@@ -470,7 +470,7 @@ template <bool BCols, bool Pairs>
 __global__ void __launch_bounds__(kFewThreads, Pairs ? 1 : 2)
 orth_few_kernel(OrthProduct p) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    typedef Tile<256, 256, 2, 4, _Float16> T;  // its transfers and instruction
+    typedef Tile<256, 256, 2, 4, 16, true> T;  // its transfers and instruction
     typedef short v4s __attribute__((ext_vector_type(4)));
     typedef short v8s __attribute__((ext_vector_type(8)));
     constexpr int E = kFewEdge, F = E / 16, ROWS = kRowBytes;
