@@ -235,7 +235,8 @@ __device__ __forceinline__ void rank_candidates(uint64_t *cand, int n, int K, F 
 //   2. The groups of these shares whose maximum reaches the bound, somewhat more than K, are looked into: a thread per vector.
 //   3. What reaches the bound is ranked by counting.
 // Bound by latency, of loads and of instructions not yet in a cache (one row of 151936 in bf16 with 20 alternatives: 16.8 us;
-// with loads eight at a time, a second look at these shares instead of all groups and one atomic per vector 7.2).
+// with loads eight at a time, a second look at these shares instead of all groups and one atomic per vector 7.2, with the search
+// for the bound ended as soon as K shares reach it 6.3).
 // Rows with more ties at the bound than there is room, or with fewer groups than K, are walked step by step from the first
 // logit on, with the K best so far kept; later ones have to beat the last of these, so ties cost little after the first step.
 template <typename T, int TR>
@@ -285,17 +286,21 @@ score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, co
             row_log = logf(s);
         }
     } else if (tid < 2 * kWave) {
-        // The K-th largest by the second wavefront, bit by bit from the highest: the largest number that K of the 256 reach.
+        // The K-th largest by the second wavefront, bit by bit from the highest: the largest number that K of the 256 reach, or a
+        // shorter one that exactly K do (where its bits end in a NaN's, the row is walked step by step).
         // (Every thread counting the larger ones: 1024 wavefront operations per compute unit, 2 us.)
         uint32_t key[kPickThreads / kWave], kth = 0;
 #pragma unroll
         for (int i = 0; i < kPickThreads / kWave; ++i) key[i] = order_key(best[i * kWave + tid - kWave]);
-#pragma unroll 4
-        for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-            int reach = 0;
+        int reach = kPickThreads;
+        for (uint32_t bit = 0x80000000u; bit && reach != K; bit >>= 1) {
+            int n = 0;
 #pragma unroll
-            for (int i = 0; i < kPickThreads / kWave; ++i) reach += __popcll(__ballot(key[i] >= (kth | bit)));
-            if (reach >= K) kth |= bit;
+            for (int i = 0; i < kPickThreads / kWave; ++i) n += __popcll(__ballot(key[i] >= (kth | bit)));
+            if (n >= K) {
+                kth |= bit;
+                reach = n;
+            }
         }
         if (tid == kWave) bound = order_value(kth);
     }
