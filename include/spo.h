@@ -449,8 +449,8 @@ int spo_muon_update(const spo_orth_desc *d, void *W, int w_dtype, float *momentu
 
 /* ---------------------------------------------------------------------------
  * Per-kernel timing (measurement aid, not part of the method; with the static
- * buffer of spo_sample_prompts_static the only state the library keeps).  While enabled, the loss entry points bracket each launch
- * of their heavy kernels with a pair of HIP events on the launch stream.
+ * buffer of spo_sample_prompts_static the only state the library keeps).  While enabled, the loss and score entry points bracket
+ * each launch of their heavy kernels with a pair of HIP events on the launch stream.
  * spo_kernel_timing_read waits for the recorded events, writes the summed
  * milliseconds and the number of launches per kernel class, and forgets them.
  * Classes: 0 fused forward vocabulary sweep, 1 backward logits recompute,
