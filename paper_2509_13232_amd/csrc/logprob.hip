@@ -532,11 +532,11 @@ score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, Sc
 //   take 228 us, of 1024 hidden units 106 (and 57 the other way).
 //   More: a wavefront forms the logits of 16 vocabulary entries by 16 tokens, the entries' rows straight from memory into the
 //   operands of the matrix instruction, kFewLoads loads of 16 bytes per lane at a time and as many on their way behind them;
-//   the hidden states wait in LDS; blocks of 16 entries go round the wavefronts (235 to 247 us; 16 rows of 64 bytes per load do
-//   not reach the rate of whole rows).
+//   the hidden states wait in LDS; blocks of 16 entries go round the wavefronts or the workgroups (223 to 247 us; 16 rows of 64
+//   bytes per load do not reach the rate of whole rows).
 constexpr int kFewTokens = 16, kFewWaves = 8, kFewLoads = 8, kFewGroups = 512;
 constexpr int kFewPad = 16;                // bytes behind a token's row in LDS: rows on different banks
-constexpr int64_t kFewLds = 144 * 1024;
+constexpr int64_t kFewLds = 140 * 1024;
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
@@ -670,8 +670,20 @@ few_dots_kernel(const bf16_t *__restrict__ X, const bf16_t *__restrict__ W, int 
 static bool few_tokens(const spo_logprob_desc *d) {
     return d->dtype == SPO_BF16 && d->w_layout == SPO_W_VH && d->T <= kFewTokens && d->T * (d->H * 2 + kFewPad) <= kFewLds;
 }
+constexpr int kFewParts = 2 * kFewWaves * kWave * 16;  // bytes
+// Whether the wavefronts of a workgroup share a block of entries.  Blocks of their own leave wavefronts without one where blocks
+// are few (three tokens, 2496 x 6024: 22.9 us, shared 11.1; 4096 x 3000 32.0 and 9.7; 256 x 2000 5.6 and 4.3) or the last round of
+// them is (960 x 73158 37.2 and 29.0), and rows of 8 KB come faster shared (4096 x 151936 235 and 223).  Otherwise the barrier and
+// the joining of every block cost more (512 x 151936 30.3 and 38.8, 2048 x 151936 119 and 126, 512 x 32000 8.2 and 9.7).
+static bool shared_few(const spo_logprob_desc *d) {
+    const int64_t blocks = ceil_div(d->V, 16), places = kFewGroups / 2 * kFewWaves, taken = ceil_div(blocks, places) * places;
+    return d->H >= 4096 || blocks <= places / 2 || (d->H >= 768 && 4 * taken >= 5 * blocks);
+}
 
 // part[token][workgroup] = (max, sum of 2^x, sum of x 2^x); z_target[token] where the target is in the vocabulary
+// Shared: the wavefronts of a workgroup share the hidden units of a block of entries, and one of them in turn adds their parts
+// up in order; otherwise each has blocks of its own.
+template <bool Shared>
 __global__ void __launch_bounds__(kFewWaves * kWave, 2)
 few_tokens_kernel(const bf16_t *__restrict__ X, const bf16_t *__restrict__ W, int T, int H, int64_t V, const int32_t *__restrict__ target,
                   float *__restrict__ part, float *__restrict__ z_target) {
@@ -679,21 +691,24 @@ few_tokens_kernel(const bf16_t *__restrict__ X, const bf16_t *__restrict__ W, in
     __shared__ float joined[kFewWaves][kFewTokens][3];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, grp = lane >> 4, pitch = H * 2 + kFewPad;
-    const int64_t blocks = ceil_div(V, 16), stride = static_cast<int64_t>(gridDim.x) * kFewWaves;
-    const int slices = H / 32, chunks = (slices + kFewLoads - 1) / kFewLoads;
-    // chunk c of block b: this lane's row of W (the last one past the vocabulary) from element 32 * kFewLoads * c + 8 * grp on
+    const int64_t blocks = ceil_div(V, 16), stride = Shared ? gridDim.x : static_cast<int64_t>(gridDim.x) * kFewWaves;
+    const int share = Shared ? (H / 32 + kFewWaves - 1) / kFewWaves : H / 32;  // of 32 hidden units: this wavefront's first and number
+    const int first = Shared ? wave * share : 0, slices = H / 32 - first < share ? H / 32 - first : share;
+    const int chunks = (share + kFewLoads - 1) / kFewLoads;
+    // chunk c of block b: this lane's row of W (the last one past the vocabulary) from slice kFewLoads * c of its share on
     uint4 set[2][kFewLoads];
     auto request = [&](uint4 (&v)[kFewLoads], int64_t b, int c) {
         const int64_t r = b * 16 + col;
-        const bf16_t *row = W + (r < V ? r : V - 1) * H + 8 * grp;
+        const bf16_t *row = W + (r < V ? r : V - 1) * H + first * 32 + 8 * grp;
 #pragma unroll
         for (int i = 0; i < kFewLoads; ++i) {
             const int sl = c * kFewLoads + i;
-            const u32x4_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(row + (sl < slices ? sl : slices - 1) * 32));
+            if (Shared && sl >= slices) break;
+            const u32x4_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(row + (Shared || sl < slices ? sl : slices - 1) * 32));
             v[i] = make_uint4(w.x, w.y, w.z, w.w);
         }
     };
-    int64_t b = static_cast<int64_t>(blockIdx.x) * kFewWaves + wave;
+    int64_t b = Shared ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kFewWaves + wave;
     if (b < blocks) request(set[0], b, 0);
     for (int i = threadIdx.x; i < T * (H / 8); i += blockDim.x) {
         const int t = i / (H / 8), k = i % (H / 8);
@@ -701,7 +716,9 @@ few_tokens_kernel(const bf16_t *__restrict__ X, const bf16_t *__restrict__ W, in
     }
     const int64_t y = target && col < T ? target[col] : -1;
     __syncthreads();
-    const char *x = lds + (col < T ? col : 0) * pitch + grp * 16;  // (columns past the tokens: the first, not used)
+    const char *x = lds + (col < T ? col : 0) * pitch + grp * 16 + first * 64;  // (columns past the tokens: the first, not used)
+    f32x4_t *parts = reinterpret_cast<f32x4_t *>(lds + T * pitch);             // Shared: [parity of the block][wavefront][lane]
+    int turn = 0;                                                              // blocks so far
     float m = kLowestFloat, s = 0.0f, u = 0.0f;
     f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
     int c = 0;
@@ -716,7 +733,18 @@ few_tokens_kernel(const bf16_t *__restrict__ X, const bf16_t *__restrict__ W, in
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, now[i]),
                                                               *reinterpret_cast<const bf16x8_t *>(x + sl * 64), acc, 0, 0, 0);
         }
-        if (last) {  // a lane holds entries 4 grp .. 4 grp + 3 of the block for token col
+        bool mine = last;
+        if (Shared && last) {
+            // (one barrier: a block's parts are read before the reader comes to the next barrier, and written over after that)
+            parts[(turn % 2 * kFewWaves + wave) * kWave + lane] = acc;
+            acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            __syncthreads();
+            mine = turn % kFewWaves == wave;
+            if (mine)
+                for (int w = 0; w < kFewWaves; ++w) acc += parts[(turn % 2 * kFewWaves + w) * kWave + lane];
+            ++turn;
+        }
+        if (mine) {  // a lane holds entries 4 grp .. 4 grp + 3 of the block for token col
             const int64_t v0 = b * 16 + 4 * grp;
             float mx = m;
 #pragma unroll
@@ -862,9 +890,11 @@ static int few_logprob_fwd(const spo_logprob_desc *d, const ScoreOut &o, void *w
     const int64_t chunks = ceil_div(d->H, kDotSpan);
     const bool dots = (d->T == 1 && chunks <= 16) || (d->T == 2 && chunks > 4 && chunks <= 8);
     const int64_t rows = !dots ? 16 : chunks <= 2 ? 4 : chunks <= 4 ? 2 : 1;  // that a wavefront takes at a time
-    const int groups = static_cast<int>(std::min<int64_t>(dots ? kFewGroups : kFewGroups / 2, ceil_div(ceil_div(d->V, rows), kFewWaves)));
-    const int lds = dots ? 0 : static_cast<int>(d->T * (d->H * 2 + kFewPad));
-    auto *kernel = !dots        ? few_tokens_kernel
+    const bool shared = !dots && shared_few(d);
+    const int groups = static_cast<int>(std::min<int64_t>(dots || shared ? kFewGroups : kFewGroups / 2, ceil_div(d->V, shared ? rows : rows * kFewWaves)));
+    const int lds = dots ? 0 : static_cast<int>(d->T * (d->H * 2 + kFewPad)) + (shared ? kFewParts : 0);
+    auto *kernel = shared       ? few_tokens_kernel<true>
+                   : !dots      ? few_tokens_kernel<false>
                    : d->T == 2  ? few_dots_kernel<2, 8, 1>
                    : chunks > 8 ? few_dots_kernel<1, 16, 1>
                    : rows == 4  ? few_dots_kernel<1, 2, 4>
