@@ -312,19 +312,31 @@ score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, co
         if (mine >= tau) share[atomicAdd(&n_share, 1)] = tid;
         __syncthreads();
         const int ns = n_share, items = ns * ((G + kPickThreads - 1) / kPickThreads);
-        for (int i = tid; i < items; i += kPickThreads) {
-            const int g = i / ns * kPickThreads + share[i % ns];
-            if (g < G && gm[g] >= tau) {
-                const int at = atomicAdd(&n_group, 1);
-                if (at < kPickGroups) groups[at] = g;
+        constexpr int S = 4;  // on their way at a time
+        for (int i0 = tid; i0 < items; i0 += S * kPickThreads) {
+            float x[S];
+            int g[S];
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                const int i = i0 + j * kPickThreads;
+                g[j] = i < items ? i / ns * kPickThreads + share[i % ns] : G;
+                x[j] = gm[g[j] < G ? g[j] : 0];
             }
+#pragma unroll
+            for (int j = 0; j < S; ++j)
+                if (g[j] < G && x[j] >= tau) {
+                    const int at = atomicAdd(&n_group, 1);
+                    if (at < kPickGroups) groups[at] = g[j];
+                }
         }
         __syncthreads();
         const int ng = n_group;
         by_step = ng > kPickGroups;
         if (!by_step) {
-            for (int i = tid; i < ng * (VPG + 1); i += kPickThreads) {
-                const int g = groups[i / (VPG + 1)], v = i % (VPG + 1), th = g % TR;
+            const bool one_round = grid.seg_len <= TR * kScoreGroup * N;  // (groups of half as many vectors)
+            for (int i = tid; i < ng * (one_round ? kScoreGroup + 1 : VPG + 1); i += kPickThreads) {
+                const int at_g = one_round ? i / (kScoreGroup + 1) : i / (VPG + 1), j = i - at_g * (one_round ? kScoreGroup + 1 : VPG + 1);
+                const int g = groups[at_g], v = one_round && j == kScoreGroup ? VPG : j, th = g % TR;
                 const int64_t e0 = (g / TR) * grid.seg_len;
                 const Span sp(row + e0, static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len));
                 float x[N];
