@@ -112,8 +112,9 @@ score_rows_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, fl
         // for the maximum and one each for its value, exponent, sum and weighted sum.  The weighted sum goes without kLowest2:
         // a NaN in it says that there was a logit of -inf (or a NaN), and then it is formed again with it.  (8192 rows of
         // 151936: with kLowest2 for every logit 376 us, without 354.)
+        // What rounding -mx log2(e) took off all exponents alike goes back into the sums (rows about 1e4: 3e-4 of them).
         const float nm2 = -mx * kLog2e;
-        float a[U] = {}, w[U] = {};
+        float a[U] = {}, w[U] = {}, rest = 0.0f;
         auto add = [&](auto exponent, auto bound) {
 #pragma unroll
             for (int u = 0; u < U; ++u) a[u] = w[u] = 0.0f;
@@ -129,13 +130,19 @@ score_rows_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, fl
             }
         };
         const bool far = fabsf(mx) > kFarLogit;
-        if (!__any(i0 < sp.nvec && far)) add([&](float v) { return fmaf(v, kLog2e, nm2); }, [](float d) { return d; });
+        if (!__any(i0 < sp.nvec && far)) {
+            add([&](float v) { return fmaf(v, kLog2e, nm2); }, [](float d) { return d; });
+            rest = far ? 0.0f : fmaf(-mx, kLog2e, -nm2);  // (far: a thread without logits)
+        }
         const float sum = (w[0] + w[1]) + (w[2] + w[3]);
-        if (__any(i0 < sp.nvec && (far || sum != sum)))
+        if (__any(i0 < sp.nvec && (far || sum != sum))) {
             add([&](float v) { return (v - mx) * kLog2e; }, [](float d) { return fmaxf(d, kLowest2); });
-        const float d = fmaxf((m - mx) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d);
-        u2 = f * fmaf(d, s, u2) + ((w[0] + w[1]) + (w[2] + w[3]));
-        s = s * f + ((a[0] + a[1]) + (a[2] + a[3]));
+            rest = 0.0f;
+        }
+        const float d = fmaxf((m - mx) * kLog2e, kLowest2), f = __builtin_amdgcn_exp2f(d), g = __builtin_amdgcn_exp2f(rest);
+        const float sa = (a[0] + a[1]) + (a[2] + a[3]), sw = (w[0] + w[1]) + (w[2] + w[3]);
+        u2 = f * fmaf(d, s, u2) + g * fmaf(rest, sa, sw);
+        s = s * f + g * sa;
         m = mx;
     };
     // a segment is at most Rounds rounds: all of it is requested at once
@@ -229,6 +236,23 @@ __device__ __forceinline__ void rank_candidates(uint64_t *cand, int n, int K, F 
     }
 }
 
+// A lower bound on the K-th largest of a wavefront's keys that exactly K of them reach, or the K-th largest itself: bit by bit
+// from the highest.
+__device__ __forceinline__ uint32_t kth_largest(const uint32_t (&key)[kPickThreads / kWave], int K) {
+    uint32_t kth = 0;
+    int reach = kPickThreads;
+    for (uint32_t bit = 0x80000000u; bit && reach != K; bit >>= 1) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kPickThreads / kWave; ++i) n += __popcll(__ballot(key[i] >= (kth | bit)));
+        if (n >= K) {
+            kth |= bit;
+            reach = n;
+        }
+    }
+    return kth;
+}
+
 // One workgroup per row: joins its segments and finds its K largest logits.
 //   1. Every thread takes the maximum of its share of group_max; the K-th largest of these 256 maxima of disjoint sets bounds
 //      the K-th largest logit from below, and few shares (K, and those that tie) reach it.
@@ -250,6 +274,7 @@ score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, co
     __shared__ int groups[kPickGroups], share[kPickThreads];
     __shared__ int n_cand, n_group, n_share;
     __shared__ float bound, row_max, row_log;
+    __shared__ uint32_t second;
     const int64_t t = flat_block();
     if (t >= rows.T) return;
     const int tid = threadIdx.x, K = out.K, nseg = grid.nseg;
@@ -286,22 +311,12 @@ score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, co
             row_log = logf(s);
         }
     } else if (tid < 2 * kWave) {
-        // The K-th largest by the second wavefront, bit by bit from the highest: the largest number that K of the 256 reach, or a
-        // shorter one that exactly K do (where its bits end in a NaN's, the row is walked step by step).
+        // The K-th largest by the second wavefront (where the bound's bits end in a NaN's, the row is walked step by step).
         // (Every thread counting the larger ones: 1024 wavefront operations per compute unit, 2 us.)
-        uint32_t key[kPickThreads / kWave], kth = 0;
+        uint32_t key[kPickThreads / kWave];
 #pragma unroll
         for (int i = 0; i < kPickThreads / kWave; ++i) key[i] = order_key(best[i * kWave + tid - kWave]);
-        int reach = kPickThreads;
-        for (uint32_t bit = 0x80000000u; bit && reach != K; bit >>= 1) {
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < kPickThreads / kWave; ++i) n += __popcll(__ballot(key[i] >= (kth | bit)));
-            if (n >= K) {
-                kth |= bit;
-                reach = n;
-            }
-        }
+        const uint32_t kth = kth_largest(key, K);
         if (tid == kWave) bound = order_value(kth);
     }
     __syncthreads();
@@ -367,6 +382,32 @@ score_pick_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, co
             }
             __syncthreads();
             by_step = n_cand > kPickRoom || n_cand < K;  // (fewer than K: NaNs, which reach no bound)
+            if (!by_step && n_cand > kPickThreads) {
+                // few groups for so many alternatives: ranking all would take longer than a second bound, from the candidates
+                constexpr int U = (kPickRoom + kPickThreads - 1) / kPickThreads;
+                uint64_t c[U], top = 0;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    c[u] = tid + u * kPickThreads < n_cand ? cand[tid + u * kPickThreads] : 0;
+                    top = c[u] > top ? c[u] : top;
+                }
+                uint32_t *keys = reinterpret_cast<uint32_t *>(best);
+                keys[tid] = static_cast<uint32_t>(top >> 32);
+                __syncthreads();
+                if (tid == 0) n_cand = 0;
+                if (tid < kWave) {
+                    uint32_t key[kPickThreads / kWave];
+#pragma unroll
+                    for (int i = 0; i < kPickThreads / kWave; ++i) key[i] = keys[i * kWave + tid];
+                    const uint32_t kth = kth_largest(key, K);
+                    if (tid == 0) second = kth;
+                }
+                __syncthreads();
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c[u] && c[u] >> 32 >= second) cand[atomicAdd(&n_cand, 1)] = c[u];
+                __syncthreads();
+            }
         }
     }
     auto put = [&](int place, uint64_t c) {
@@ -486,7 +527,7 @@ score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, Sc
     }
     if (a == 0.0f && e == 0.0f && !some) return zeros();
     const int y = yl >= 0 && yl < len ? static_cast<int>(yl) : -1;
-    const float c = -(e != 0.0f ? fmaf(e, h, total) : total), c2 = -e * kLn2;  // dz = p (c + c2 log2 p) + ...
+    float c = -(e != 0.0f ? fmaf(e, h, total) : total), c2 = -e * kLn2;  // dz = p (c + c2 log2 p) + ...
     auto finish = [&](auto exponent) {
         auto grad = [&](float z) {
             const float d = exponent(z);
@@ -528,7 +569,10 @@ score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, Sc
         row_max_log<T, TR>(logits + t * rows.stride, rows.V, top, log_sum);
         finish([&](float z) { return ((z - top) - log_sum) * kLog2e; });
     } else {
-        const float nl = -lse * kLog2e;
+        // (what rounding -lse log2(e) takes off all exponents alike goes into the factors)
+        const float nl = -lse * kLog2e, rest = fmaf(-lse, kLog2e, -nl), g = __builtin_amdgcn_exp2f(rest);
+        c = g * fmaf(c2, rest, c);
+        c2 *= g;
         finish([&](float z) { return fmaf(z, kLog2e, nl); });
     }
 }
