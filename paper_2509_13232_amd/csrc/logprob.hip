@@ -63,7 +63,7 @@ __device__ __forceinline__ void join_lanes(float &m, float &s, float &u) {
 // (max, sum of 2^x, sum of x 2^x) of one segment of a row by TR threads, a workgroup or one wavefront of it, and with Top each
 // thread's own maximum, group_max[row][segment * TR + thread].  Rows of one segment (whole) are finished here unless
 // alternatives are asked for.  Bound by HBM in fp32 (535 of 713 rows of 100003, 214 MB in 38.8 us = 5.5 TB/s), in bf16 by
-// instructions as well (6554 of 8192 rows of 151936, 1.99 GB in 330 to 377 us = 5.3 to 6.0 TB/s); single rows by latency (4 us).
+// instructions as well (6554 of 8192 rows of 151936, 1.99 GB in 330 to 393 us = 5.1 to 6.0 TB/s); single rows by latency (4 us).
 template <typename T, int TR, int Rounds, bool Stream, bool Top>
 __global__ void __launch_bounds__(kRowThreads)
 score_rows_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, float *__restrict__ part, float *__restrict__ group_max,
