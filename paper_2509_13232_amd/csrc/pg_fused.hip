@@ -329,15 +329,17 @@ struct LossRecords {
     }
 };
 // Log-probs and entropies: (c, -lse * log2(e), target, c2) with the gradient's softmax part p (c + c2 log2 p),
-// c = -(a + e H), c2 = -e ln 2, and a itself beside it in hot[r].
+// c = -(a + e H), c2 = -e ln 2, and a itself beside it in hot[r].  An id outside [0, V) is no target, whatever its bits.
 struct ScoreRecords {
+    int64_t V;
     const int32_t *target;
     const float *lse, *entropy, *d_logp, *d_entropy;
     float *hot;
     __device__ __forceinline__ float4 operator()(int64_t r, bool live, int64_t src) const {
         const float a = live && d_logp ? d_logp[src] : 0.0f, e = live && d_entropy ? d_entropy[src] : 0.0f;
         hot[r] = a;
-        const uint32_t ts = live && d_logp ? static_cast<uint32_t>(target[src]) & 0x7fffffffu : 0x7fffffffu;
+        const int32_t y = live && d_logp ? target[src] : -1;
+        const uint32_t ts = y >= 0 && y < V ? static_cast<uint32_t>(y) : 0x7fffffffu;
         return make_float4(-fmaf(e, e != 0.0f ? entropy[src] : 0.0f, a), live ? -lse[src] * kLog2e : -INFINITY, __uint_as_float(ts), -e * kLn2);
     }
 };
@@ -2279,7 +2281,7 @@ int head_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *e
         const bool small = small_sweep(Tv, V, p.Kc);
         const int64_t edge = tile_edge(small), Tcp = round_up(Tv, edge);
         float *hot = p.g;  // of the chunk's rows
-        launch_gather(d->dtype, H, d->hidden, p.act_idx, p.n_act, t0, Tcp, ScoreRecords{d->target, lse, entropy, d_logp, d_entropy, hot}, p.Xc,
+        launch_gather(d->dtype, H, d->hidden, p.act_idx, p.n_act, t0, Tcp, ScoreRecords{d->V, d->target, lse, entropy, d_logp, d_entropy, hot}, p.Xc,
                       nullptr, p.tok, c == 0 ? d_hidden : nullptr, d_hidden_dtype, T, s);
         int rc;
         if ((rc = launch_recompute<true>(&pg, Wk, direct && hv, p.Xc, p.Kc, Tcp, small, p.tok, p.dZ, p.n_act, t0, hot, s))) return rc;
