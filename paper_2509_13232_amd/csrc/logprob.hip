@@ -956,7 +956,9 @@ static int few_logprob_fwd(const spo_logprob_desc *d, const ScoreOut &o, void *w
                    : rows == 4  ? few_dots_kernel<1, 2, 4>
                    : rows == 2  ? few_dots_kernel<1, 4, 2>
                                 : few_dots_kernel<1, 8, 1>;
-    if (!dots && hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+    // (the limit is the kernel's, not this call's: every call sets the same, so that no other thread's can lower it before the launch)
+    if (!dots && hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(kFewLds) + (shared ? kFewParts : 0)) != hipSuccess)
         return SPO_EHIP;
     {
         ScopedKernelTimer timer(kTimeFwdSweep, s);
