@@ -18,7 +18,7 @@
 #include <algorithm>
 
 #include "gemm_core.hpp"
-#include "tile_choice.hpp"
+#include "orth_choice.hpp"
 
 namespace spo {
 
@@ -219,10 +219,11 @@ __device__ __forceinline__ void store_last(const OrthOut &o, int64_t matrix, int
 // The tiles of a product in the order of their ids: those of TileOrder, or of a symmetric product (n x n tiles) the rows of the
 // lower triangle one after the other.
 struct OrthTiles {
-    int64_t nM, nN;
+    int64_t nM, nN, count;
     bool symmetric;
-    __host__ __device__ OrthTiles(int64_t M, int64_t N, int64_t edge, bool sym) : nM(ceil_div(M, edge)), nN(ceil_div(N, edge)), symmetric(sym) {}
-    __host__ __device__ int64_t tiles() const { return symmetric ? nM * (nM + 1) / 2 : nM * nN; }
+    __host__ __device__ OrthTiles(int64_t M, int64_t N, int64_t edge, bool sym)
+        : nM(ceil_div(M, edge)), nN(ceil_div(N, edge)), count(orth_tiles(M, N, edge, sym)), symmetric(sym) {}
+    __host__ __device__ int64_t tiles() const { return count; }
     __device__ __forceinline__ void at(uint32_t i, int64_t &tm, int64_t &tn) const {
         if (!symmetric) return TileOrder(nM, nN).at(i, tm, tn);
         uint32_t r = static_cast<uint32_t>((sqrtf(8.0f * static_cast<float>(i) + 1.0f) - 1.0f) * 0.5f);  // to one off
@@ -825,7 +826,7 @@ static OrthPlan plan_orth(const spo_orth_desc *d, void *ws) {
     p.parts = static_cast<int>(std::min<int64_t>(kNormParts, ceil_div(vectors, 256 * 2)));
     Arena a(ws);
     p.norm = a.take<double>(static_cast<size_t>(d->batch) * kNormParts);
-    p.sq = a.take<float>(static_cast<size_t>(d->batch) * (p.kp / kFewEdge) * (p.Lp / kFewEdge) * kFewWaves);  // (other tiles: fewer)
+    p.sq = a.take<float>(static_cast<size_t>(d->batch) * square_room(p.kp, p.Lp));
     p.shift = a.take<float>(d->batch);
     auto stack = [&](int64_t rows, int64_t ld) {
         Stack s{nullptr, ld, rows * ld, 2 * rows * ld};
@@ -866,52 +867,9 @@ template <typename TT, bool BCols>
 static int launch_tiles(const OrthProduct &p, hipStream_t s) {
     return p.split ? launch_tiles<TT, BCols, true>(p, s) : launch_tiles<TT, BCols, false>(p, s);
 }
-// Which kernel forms a product?  About what a launch takes, in us (measured on single matrices of 64 to 4096 and stacks of
-// four of 1024 x 4096, both kinds of products; within a fifth of it but for launches of a few us):
-//   tiles shared by wavefronts: rounds of workgroups on the chip x (steps x time of a step + the tile's ends); a step slows
-//   down as the chip fills up.  Half of the time that the addend and the output take from and to memory comes on top.
-//   a share of the contraction per wavefront: half rounds of a tile per compute unit, with pairs whole ones.
-// So 64 x 64 x 64 (k, L, steps) takes 5 us instead of 7, 1024 x 1024 x 16 8.8 instead of 14 (128), 48 steps 14 instead of 33;
-// 2048 x 2048 x 32 24 on tiles of 128 (64: 25, 192: 31), 4096 x 4096 x 64 symmetric 73 on 192 (253 tiles on 256 compute units;
-// 85 on 256, 99 on 128), otherwise 118 on 256.
-enum class Kind { few, small, middle, large };
-struct OrthTimes {
-    int64_t edge, slots;
-    double start, step, crowd, ends;  // crowd: what a step takes longer on a chip that is full
-};
-constexpr OrthTimes kSmallTimes{128, 512, 3.0, 0.57, 0.30, 4.0}, kMiddleTimes{192, 256, 3.0, 0.75, 0.25, 4.0},
-    kLargeTimes{256, 256, 3.0, 1.00, 0.40, 9.0};
-static double product_time(const OrthTimes &t, const OrthProduct &p, double steps) {
-    const int64_t tiles = OrthTiles(p.Mp, p.Np, t.edge, p.symmetric).tiles() * p.batch, full = tiles / t.slots, rest = tiles % t.slots;
-    // (two small tiles share a compute unit once half of the slots are taken)
-    const double fill = t.slots > kChipCUs ? std::max<int64_t>(0, rest - kChipCUs) / 256.0 : static_cast<double>(rest) / static_cast<double>(t.slots);
-    const double bytes = static_cast<double>(p.Mp) * static_cast<double>(p.Np) * static_cast<double>(p.batch) *
-                         ((p.d.base ? (p.d_lo ? 4 : 2) : 0) + (p.out_lo ? 4 : 2));
-    return t.start + static_cast<double>(full) * (steps * (t.step + t.crowd) + t.ends) +
-           (rest ? steps * (t.step + t.crowd * fill) + t.ends : 0.0) + 0.5 * bytes / 5.0e6;
-}
-static Kind product_kind(const OrthProduct &p, bool middle) {
-    const double steps = p.KT * (p.split ? 3 : 1);
-    const int64_t tiles = OrthTiles(p.Mp, p.Np, kFewEdge, p.symmetric).tiles() * p.batch;
-    const double halves = std::max(1.0, static_cast<double>(ceil_div(2 * tiles, kChipCUs)) * 0.5);
-    Kind best = Kind::few;
-    double least = p.split ? 4.0 + static_cast<double>(ceil_div(tiles, kChipCUs)) * (p.KT * 0.475 + 2.4) : 4.0 + halves * (steps * 0.2 + 2.4);
-    auto offer = [&](Kind k, const OrthTimes &t) {
-        const double time = product_time(t, p, steps);
-        if (time < least) {
-            least = time;
-            best = k;
-        }
-    };
-    offer(Kind::small, kSmallTimes);
-    if (middle) offer(Kind::middle, kMiddleTimes);
-    offer(Kind::large, kLargeTimes);
-    return best;
-}
-static int64_t edge_of(Kind k) {
-    return k == Kind::few ? kFewEdge : k == Kind::small ? kSmallTimes.edge : k == Kind::middle ? kMiddleTimes.edge : kLargeTimes.edge;
-}
-static int waves_of(Kind k) { return k == Kind::few ? kFewWaves : k == Kind::small ? OS::NWAVE : k == Kind::middle ? OM::NWAVE : OL::NWAVE; }
+static_assert(OS::BM == kOrthEdge[1] && OS::NWAVE == kOrthWaves[1] && OM::BM == kOrthEdge[2] && OM::NWAVE == kOrthWaves[2] &&
+                  OL::BM == kOrthEdge[3] && OL::NWAVE == kOrthWaves[3] && kFewEdge == kOrthEdge[0] && kFewWaves == kOrthWaves[0],
+              "orth_choice.hpp knows the kernels' tiles");
 template <bool BCols>
 static int launch_product(const OrthProduct &p, Kind kind, hipStream_t s) {
     if (kind == Kind::few) return p.split ? launch_few<BCols, true>(p, s) : launch_few<BCols, false>(p, s);
@@ -974,13 +932,13 @@ static int run_orth(const spo_orth_desc *d, const OrthInput &in, OrthOut last, v
     update.c[1] = d->b;
     update.c[2] = d->c;
     update.sq_out = p.sq;
-    const Kind gram_kind = product_kind(gram, true), poly_kind = product_kind(poly, true), update_kind = product_kind(update, false);
+    const OrthKinds kinds = orth_kinds(p.kp, p.Lp, d->batch, split);
     for (int i = 0; i < d->steps; ++i) {
         const Stack &X = p.X[i & 1];
         gram.a = gram.b = X;
-        gram.n_sq = i == 0 ? 1 : static_cast<int>(OrthTiles(p.kp, p.Lp, edge_of(update_kind), false).tiles()) * waves_of(update_kind);
-        if (int rc = launch_product<false>(gram, gram_kind, s)) return rc;
-        if (int rc = launch_product<false>(poly, poly_kind, s)) return rc;
+        gram.n_sq = i == 0 ? 1 : static_cast<int>(square_sums(p.kp, p.Lp, kinds.update));
+        if (int rc = launch_product<false>(gram, kinds.gram, s)) return rc;
+        if (int rc = launch_product<false>(poly, kinds.poly, s)) return rc;
         update.b = update.d = X;
         update.out = p.X[(i + 1) & 1];
         if (i == d->steps - 1) {
@@ -989,7 +947,7 @@ static int run_orth(const spo_orth_desc *d, const OrthInput &in, OrthOut last, v
             update.sq_out = nullptr;
             update.last = last;
         }
-        if (int rc = launch_product<true>(update, update_kind, s)) return rc;
+        if (int rc = launch_product<true>(update, kinds.update, s)) return rc;
     }
     return launch_status();
 }
