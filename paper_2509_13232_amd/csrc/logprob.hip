@@ -450,28 +450,59 @@ struct ScoreGrads {
     int K;
 };
 
-// (max, log of the sum of exp(x - max)) of a whole row by a group of TR threads.
+// The gradient takes log p = z - lse, and what rounding lse to fp32 took off is an error that all of a row's probabilities share: half
+// of its last place, 2^-18 up to 128 and 2^-14 up to 2048.  Beyond that it is no longer small (in fp32 beside the other roundings, in
+// bf16 beside the output's 2^-8), and the row's own maximum and sum are formed again.
+template <typename T> constexpr float kFarLse = sizeof(T) == 4 ? 128.0f : 2048.0f;
+template <typename T> constexpr int kFarLoads = 16 / Vec<T>::N;  // on their way per thread
+constexpr uint32_t kFarUnits = 512;  // see score_grad_kernel
+
+// (max, log of the sum of exp(x - max)) of a whole row by a group of TR threads, in one pass.
 template <typename T, int TR>
 __device__ __forceinline__ void row_max_log(const T *row, int64_t V, float &m, float &l) {
-    __shared__ float wm[kRowThreads / kWave], wu[kRowThreads / kWave];
-    const int tid = threadIdx.x % TR, wave = threadIdx.x >> 6;
-    m = kLowestFloat;
-    for (int64_t i = tid; i < V; i += TR) m = fmaxf(m, Vec<T>::get(row + i));
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
-    if constexpr (TR > kWave) {
-        wm[wave] = m;
-        __syncthreads();
-        for (int w = 0; w < TR / kWave; ++w) m = fmaxf(m, wm[w]);
-    }
+    constexpr int N = Vec<T>::N, U = kFarLoads<T>;
+    const int tid = threadIdx.x % TR, nvec = static_cast<int>(V / N);
     float s = 0.0f;
-    for (int64_t i = tid; i < V; i += TR) s += __builtin_amdgcn_exp2f((Vec<T>::get(row + i) - m) * kLog2e);
-    s = wave_sum(s);
+    m = kLowestFloat;
+    for (int i0 = tid; i0 < nvec; i0 += U * TR) {
+        uint4 v[U];
+        float x[N], mx = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = load16<false>(row + static_cast<int64_t>(i0 + u * TR < nvec ? i0 + u * TR : i0) * N);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            Vec<T>::unpack(v[u], x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) mx = fmaxf(mx, x[i]);
+        }
+        s *= __builtin_amdgcn_exp2f((m - mx) * kLog2e);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * TR >= nvec) break;
+            Vec<T>::unpack(v[u], x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((x[i] - mx) * kLog2e);
+        }
+        m = mx;
+    }
+    if (tid < static_cast<int>(V - static_cast<int64_t>(nvec) * N)) {
+        const float x = Vec<T>::get(row + static_cast<int64_t>(nvec) * N + tid), mx = fmaxf(m, x);
+        s = s * __builtin_amdgcn_exp2f((m - mx) * kLog2e) + __builtin_amdgcn_exp2f((x - mx) * kLog2e);
+        m = mx;
+    }
+    float top = m;
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    s = wave_sum(s * __builtin_amdgcn_exp2f((m - top) * kLog2e));
+    m = top;
     if constexpr (TR > kWave) {
-        wu[wave] = s;
+        __shared__ float wm[TR / kWave], ws[TR / kWave];
+        if ((threadIdx.x & 63) == 0) { wm[threadIdx.x >> 6] = m; ws[threadIdx.x >> 6] = s; }
         __syncthreads();
+        m = wm[0];
+        for (int w = 1; w < TR / kWave; ++w) m = fmaxf(m, wm[w]);
         s = 0.0f;
-        for (int w = 0; w < TR / kWave; ++w) s += wu[w];
+        for (int w = 0; w < TR / kWave; ++w) s += ws[w] * __builtin_amdgcn_exp2f((wm[w] - m) * kLog2e);
     }
     l = logf(s);
 }
@@ -479,56 +510,73 @@ __device__ __forceinline__ void row_max_log(const T *row, int64_t V, float &m, f
 // One segment of a row of d_logits (at most kScoreGradGroup vectors per thread).  Rows that the mask leaves out are not read;
 // they and rows whose factors are all zero are written as zeros.  Vectors are aligned on the output side.  Bound by HBM: 8192 rows
 // of 151936 in bf16, a fifth left out, 4.48 GB in 770 us = 5.8 TB/s; 512 rows of 1000 in fp32 4.6 us.
+// Rows far from zero (kFarLse) are read once more for their own maximum and sum, by each of the groups that then write the row, some
+// kFarUnits for all rows together (rows of 151936 in fp32: one 18 us, 27 36, 512 239; by one group per row 63, 74, 252, by one per
+// segment 18, 64, 1026; other rows 5, 6, 95).
 template <typename T, int TR, bool Stream>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 8)
 score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, ScoreGrads gr, T *__restrict__ d_logits) {
     constexpr int N = Vec<T>::N, U = kScoreGradGroup;
     const int64_t unit = group_unit<TR>();
     const int tid = threadIdx.x % TR, lane = threadIdx.x & 63;
     if (unit >= grid.units()) return;
     const uint32_t nseg = static_cast<uint32_t>(grid.nseg);
-    const int64_t t = static_cast<uint32_t>(unit) / nseg, e0 = (static_cast<uint32_t>(unit) % nseg) * grid.seg_len;
-    const T *p = logits + t * rows.stride + e0;
-    T *out = d_logits + t * rows.V + e0;
-    const int len = static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len);
-    const Span sp(out, len);
-    uint4 *dst = reinterpret_cast<uint4 *>(out + sp.head);
-    const bool edge = tid < sp.head + sp.tail;
-    const int at_edge = tid < sp.head ? tid : tid + sp.nvec * N;
+    const int64_t t = static_cast<uint32_t>(unit) / nseg;
+    uint32_t seg = static_cast<uint32_t>(unit) % nseg;
+    const T *row = logits + t * rows.stride;
+    T *out_row = d_logits + t * rows.V;
+    // a segment: its start and length, its vectors and this thread's element outside of them
+    int64_t e0;
+    int len;
+    Span sp(out_row, 0);
+    auto start = [&] {
+        e0 = seg * grid.seg_len;
+        len = static_cast<int>(rows.V - e0 < grid.seg_len ? rows.V - e0 : grid.seg_len);
+        sp = Span(out_row + e0, len);
+    };
+    auto edge = [&] { return tid < sp.head + sp.tail; };
+    auto at_edge = [&] { return tid < sp.head ? tid : tid + sp.nvec * N; };
+    auto vectors = [&] { return reinterpret_cast<uint4 *>(out_row + e0 + sp.head); };
+    start();
     auto zeros = [&] {
-        if (edge) Vec<T>::put(out + at_edge, 0.0f);
-        for (int i = tid; i < sp.nvec; i += TR) store16<Stream>(dst + i, make_uint4(0u, 0u, 0u, 0u));
+        if (edge()) Vec<T>::put(out_row + e0 + at_edge(), 0.0f);
+        for (int i = tid; i < sp.nvec; i += TR) store16<Stream>(vectors() + i, make_uint4(0u, 0u, 0u, 0u));
     };
     if (rows.mask && !rows.mask[t]) return zeros();
     // everything is requested before any of it is looked at
-    const T *body = p + sp.head;
     uint4 v[U];
+    T x_edge;
+    auto request = [&] {
+        const T *body = row + e0 + sp.head;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (tid + u * TR < sp.nvec) v[u] = load16<Stream>(body + (tid + u * TR) * N);
-    const T x_edge = edge ? p[at_edge] : T(0);  // (as it is: a conversion would wait for it here)
+        for (int u = 0; u < U; ++u)
+            if (tid + u * TR < sp.nvec) v[u] = load16<Stream>(body + (tid + u * TR) * N);
+        x_edge = edge() ? row[e0 + at_edge()] : T(0);  // (as it is: a conversion would wait for it here)
+    };
+    request();
     const float lse = gr.lse[t], a = gr.d_logp ? gr.d_logp[t] : 0.0f, e = gr.d_entropy ? gr.d_entropy[t] : 0.0f;
     const float h = gr.d_entropy ? gr.entropy[t] : 0.0f;
-    const int64_t yl = gr.d_logp ? static_cast<int64_t>(rows.target[t]) - e0 : -1;
+    const int64_t target = gr.d_logp ? static_cast<int64_t>(rows.target[t]) : -1;
     float total = a;
-    int id = -1;  // lane k: the k-th alternative's place in the segment, and its factor
+    int64_t top_id = -1;  // lane k: the k-th alternative, and its factor
     float b = 0.0f;
-    uint64_t hot = 0;
     bool some = false;
     if (gr.d_top) {
         if (lane < gr.K) {
             b = gr.d_top[t * gr.K + lane];
-            const int64_t at = static_cast<int64_t>(gr.top_id[t * gr.K + lane]) - e0;
-            id = at >= 0 && at < len ? static_cast<int>(at) : -1;
+            top_id = gr.top_id[t * gr.K + lane];
         }
-        hot = __ballot(id >= 0 && b != 0.0f);
         some = __any(b != 0.0f);  // (factors of both signs may add up to zero)
         total += wave_sum(b);
     }
     if (a == 0.0f && e == 0.0f && !some) return zeros();
-    const int y = yl >= 0 && yl < len ? static_cast<int>(yl) : -1;
     float c = -(e != 0.0f ? fmaf(e, h, total) : total), c2 = -e * kLn2;  // dz = p (c + c2 log2 p) + ...
     auto finish = [&](auto exponent) {
+        // places in the segment
+        const int64_t yl = target - e0, il = top_id - e0;
+        const int y = target >= 0 && yl >= 0 && yl < len ? static_cast<int>(yl) : -1;
+        const int id = top_id >= 0 && il >= 0 && il < len ? static_cast<int>(il) : -1;
+        const uint64_t hot = some ? __ballot(id >= 0 && b != 0.0f) : 0;
         auto grad = [&](float z) {
             const float d = exponent(z);
             return __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, kLowest2), c2, c);
@@ -540,10 +588,10 @@ score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, Sc
                 add(__builtin_amdgcn_readlane(id, l), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b), l)));
             }
         };
-        if (edge) {
+        if (edge()) {
             float g = grad(Vec<T>::get(&x_edge));
-            of_hot([&](int place, float w) { g += place == at_edge ? w : 0.0f; });
-            Vec<T>::put(out + at_edge, g);
+            of_hot([&](int place, float w) { g += place == at_edge() ? w : 0.0f; });
+            Vec<T>::put(out_row + e0 + at_edge(), g);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -559,21 +607,26 @@ score_grad_kernel(const T *__restrict__ logits, ScoreRows rows, RowGrid grid, Sc
 #pragma unroll
                     for (int i = 0; i < N; ++i) x[i] += at == i ? w : 0.0f;
             });
-            store16<Stream>(dst + iv, Vec<T>::pack(x));
+            store16<Stream>(vectors() + iv, Vec<T>::pack(x));
         }
     };
-    // Beside a large log-sum-exp its rounding is no longer small (a row of 1e30: the logarithm of the sum is gone): such a
-    // row's own maximum and sum are formed again, by every segment.
-    if (fabsf(lse) > kFarLogit) {
-        float top, log_sum;
-        row_max_log<T, TR>(logits + t * rows.stride, rows.V, top, log_sum);
-        finish([&](float z) { return ((z - top) - log_sum) * kLog2e; });
-    } else {
+    if (fabsf(lse) <= kFarLse<T> || lse != lse) {
         // (what rounding -lse log2(e) takes off all exponents alike goes into the factors)
         const float nl = -lse * kLog2e, rest = fmaf(-lse, kLog2e, -nl), g = __builtin_amdgcn_exp2f(rest);
         c = g * fmaf(c2, rest, c);
         c2 *= g;
-        finish([&](float z) { return fmaf(z, kLog2e, nl); });
+        return finish([&](float z) { return fmaf(z, kLog2e, nl); });
+    }
+    const uint32_t share = kFarUnits / static_cast<uint32_t>(rows.T), groups = share < 1 ? 1 : share;  // of a row
+    if (seg >= groups) return;
+    float top, log_sum;
+    row_max_log<T, TR>(row, rows.V, top, log_sum);
+    for (;;) {
+        finish([&](float z) { return ((z - top) - log_sum) * kLog2e; });
+        seg += groups;
+        if (seg >= nseg) return;
+        start();
+        request();
     }
 }
 
