@@ -10,6 +10,10 @@ namespace spo {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegBig = -1.0e30f;  // finite stand-in for -inf in running maxima
+// Largest magnitude of a maximum at which the exponents are formed in one multiply-add.  What is lost with the
+// maximum's product is half of its last place: a factor common to all, as small as the log-sum-exp's own rounding up to
+// here, but past the range of exponents in rows that are masked with -1e30 throughout.
+constexpr float kFarLogit = 65536.0f;
 
 struct Surrogate {
     float ratio, obj;

@@ -838,8 +838,11 @@ fwd_sweep_kernel(const char *__restrict__ W, int64_t ldw_bytes, int64_t V, const
                 }
             }
             if (Emit == kEmitEntropy) {
+                // what rounding c took off all exponents alike goes back into the sums (logits about 1e4: 3e-4 of them)
+                const float rest = fabsf(nm) <= kFarLogit ? fmaf(-nm, kLog2e, -c) : 0.0f, g = __builtin_amdgcn_exp2f(rest);
                 const float d = fmaxf((m_run[fn] - nm) * kLog2e, kLowest2);
-                ref[fn] = __builtin_amdgcn_exp2f(d) * fmaf(d, s_run[fn], ref[fn]) + w;
+                ref[fn] = __builtin_amdgcn_exp2f(d) * fmaf(d, s_run[fn], ref[fn]) + g * fmaf(rest, s, w);
+                s *= g;
             }
             s_run[fn] = s_run[fn] * __builtin_amdgcn_exp2f((m_run[fn] - nm) * kLog2e) + s;
             m_run[fn] = nm;
@@ -2164,9 +2167,9 @@ head_scores_kernel(const float *__restrict__ part_max, const float *__restrict__
     if (way != 0 || t >= T) return;
     if (live)
         for (int w = 1; w < ways; ++w) score_join(m, s, u, sm[w][lane], ss[w][lane], su[w][lane]);
-    const float lse = live ? m + logf(s) : 0.0f;
-    lse_out[t] = lse;
-    if (logp) logp[t] = live ? z_target[t] - lse : 0.0f;
+    const float l = logf(s);
+    lse_out[t] = live ? m + l : 0.0f;
+    if (logp) logp[t] = live ? (z_target[t] - m) - l : 0.0f;  // (beside a logit of 1e4 the sum m + l has lost some of l)
     if (entropy) entropy[t] = live ? score_entropy(s, u) : 0.0f;
 }
 

@@ -8,10 +8,6 @@ namespace spo {
 
 constexpr int kRowThreads = 256;
 constexpr int64_t kStreamBytes = int64_t(256) << 20;  // the Infinity Cache: larger arrays take the non-temporal hint
-// Largest magnitude of a maximum at which the exponents are formed in one multiply-add.  What is lost with the
-// maximum's product is half of its last place: a factor common to all, as small as the log-sum-exp's own rounding up to
-// here, but past the range of exponents in rows that are masked with -1e30 throughout.
-constexpr float kFarLogit = 65536.0f;
 constexpr int kFewSegments = 8;                        // see row_grid
 
 // 16 bytes of a row as floats and back
