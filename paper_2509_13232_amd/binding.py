@@ -613,6 +613,13 @@ def _stack_shape(t, name):
     return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
 
 
+def _want_stack(t, dtype, name, shape):
+    """A contiguous array of a stack of matrices (a flat one, too): not of as many elements that lie in another order."""
+    _want(t, dtype, name, shape[0] * shape[1] * shape[2])
+    if t.dim() != 1 and _stack_shape(t, name) != shape:
+        raise ValueError(f"{name}: expected {shape[0]} x {shape[1]} x {shape[2]}, got {tuple(t.shape)}")
+
+
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
 
 
@@ -633,7 +640,7 @@ def spo_orthogonalize(G, out=None, out_dtype=None, steps=5, coeffs=NEWTON_SCHULZ
     if out is None:
         out = torch.empty(G.shape, dtype=out_dtype or G.dtype, device=G.device)
     else:
-        _want(out, out.dtype, "out", batch * rows * cols)
+        _want_stack(out, out.dtype, "out", (batch, rows, cols))
     d = _orth_desc(batch, rows, cols, steps, coeffs, eps, products)
     ws = _workspace(lib().spo_orthogonalize_workspace_bytes(C.byref(d)), G.device, workspace)
     _check(lib().spo_orthogonalize(C.byref(d), _ptr(G), _dt(G.dtype), stride, step, _ptr(out), _dt(out.dtype), _ptr(ws), ws.numel(),
@@ -646,10 +653,9 @@ def spo_muon_update(W, momentum, grad, lr, mu=0.95, nesterov=True, weight_decay=
     """The momentum step, IN PLACE on W and momentum ([rows, cols] or [batch, rows, cols], contiguous).  scale: factor of
     the orthogonalised update beside lr; None: sqrt(max(1, rows / cols))."""
     batch, rows, cols = _stack_shape(W, "W")
-    n = batch * rows * cols
     _want(W, W.dtype, "W")
-    _want(momentum, torch.float32, "momentum", n)
-    _want(grad, grad.dtype, "grad", n)
+    _want_stack(momentum, torch.float32, "momentum", (batch, rows, cols))
+    _want_stack(grad, grad.dtype, "grad", (batch, rows, cols))
     for t, name in ((W, "W"), (grad, "grad")):
         if t.dtype not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16")
