@@ -74,6 +74,12 @@ static inline Kind product_kind(const ProductSize &p) {
     return best;
 }
 
+// Sides are rounded up to steps of the contraction.
+static inline int64_t padded(int64_t n) { return (n + kStep - 1) / kStep * kStep; }
+// Where the smaller side is one step of the contraction, launches are all that counts, and so few roundings do not
+// average out (one of 1 x 1: 4e-3): always pairs.
+static inline bool as_pairs(int64_t k, bool asked) { return asked || k <= kStep; }
+
 // The products of a step on X of k x L (padded): A = X X^T, B = c A A + ..., X <- B X + ...
 struct OrthKinds {
     Kind gram, poly, update;

@@ -801,7 +801,7 @@ __global__ void __launch_bounds__(256) orth_scale_turned_kernel(OrthInput in, co
 // ----------------------------------------------------------------------------
 // host side
 // ----------------------------------------------------------------------------
-static int64_t padded(int64_t n) { return ceil_div(n, kBK) * kBK; }
+static_assert(kStep == kBK, "steps of the main loop");
 
 struct OrthPlan {
     int64_t k, L, kp, Lp;  // the smaller and the larger side, and both padded: X is k x L
@@ -895,9 +895,7 @@ static int run_orth(const spo_orth_desc *d, const OrthInput &in, OrthOut last, v
             in, p.norm, p.parts, p.x_scale, p.X[0], x_rows, d->steps ? OrthOut{} : last, p.sq);
     }
     last.across = tall;
-    // Where the smaller side is one step of the contraction, launches are all that counts, and so few roundings do not
-    // average out (one of 1 x 1: 4e-3): always pairs.
-    const bool split = d->products == SPO_PRODUCTS_SPLIT || p.k <= kBK;
+    const bool split = as_pairs(p.k, d->products == SPO_PRODUCTS_SPLIT);
     // A' = X X^T - s I
     OrthProduct gram{};
     gram.batch = d->batch;

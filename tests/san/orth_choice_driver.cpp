@@ -1,4 +1,5 @@
-// Products of orthogonalised updates (csrc/orth_choice.hpp): room for the sums of squares that any kind of tiles leaves.
+// Products of orthogonalised updates (csrc/orth_choice.hpp): room for the sums of squares that any kind of tiles leaves, or, with
+// batch, rows, cols and products as arguments, the kinds that are chosen.
 #define __host__
 #define __device__
 #define __forceinline__ inline
@@ -6,10 +7,19 @@
 #include "orth_choice.hpp"
 
 #include <cstdio>
+#include <cstdlib>
 
 using namespace spo;
 
-int main() {
+int main(int argc, char **argv) {
+    if (argc == 5) {
+        const int64_t batch = std::atoll(argv[1]), rows = std::atoll(argv[2]), cols = std::atoll(argv[3]);
+        const OrthKinds q = orth_kinds(padded(std::min(rows, cols)), padded(std::max(rows, cols)), batch,
+                                       as_pairs(std::min(rows, cols), std::atoi(argv[4]) != 0));
+        const char *name[] = {"few", "small", "middle", "large"};
+        std::printf("%s %s %s\n", name[static_cast<int>(q.gram)], name[static_cast<int>(q.poly)], name[static_cast<int>(q.update)]);
+        return 0;
+    }
     int bad = 0;
     for (int64_t k = 64; k <= 65536; k += k < 2048 ? 64 : 4032)
         for (int64_t L = k; L <= 65536; L += L < 2048 ? 64 : 4032)

@@ -5,6 +5,7 @@ import subprocess
 
 import pytest
 
+import update_kinds
 from paper_2509_13232_amd import binding as spo
 from paper_2509_13232_amd import build
 
@@ -25,10 +26,28 @@ def test_a_kernels_limit_of_lds_is_the_same_for_all_calls(tmp_path):
     assert "limits are the kernels' own" in r.stdout
 
 
-def test_sums_of_squares_have_room_whatever_tiles_leave_them(tmp_path):
-    exe = str(tmp_path / "orth_choice")
+@pytest.fixture(scope="module")
+def orth_choice(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("orth") / "orth_choice")
     subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-Wall", "-Wextra",
                     "-I" + build.CSRC, os.path.join(ROOT, "tests", "san", "orth_choice_driver.cpp"), "-o", exe], check=True)
-    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
-    assert r.returncode == 0, r.stderr[-3000:]
-    assert "sums of squares have room" in r.stdout
+
+    def run(*args):
+        r = subprocess.run([exe, *map(str, args)], capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stderr[-3000:]
+        return r.stdout
+    return run
+
+
+def test_sums_of_squares_have_room_whatever_tiles_leave_them(orth_choice):
+    assert "sums of squares have room" in orth_choice()
+
+
+def test_the_stacks_of_the_gpu_tests_reach_every_kind_of_tiles(orth_choice):
+    # (the product that updates X has no tiles of 192)
+    reached = set()
+    for batch, rows, cols, products, *kinds in update_kinds.STACKS:
+        assert orth_choice(batch, rows, cols, products).split() == kinds, (batch, rows, cols, products)
+        assert orth_choice(batch, cols, rows, products).split() == kinds
+        reached |= {(products, which, kind) for which, kind in enumerate(kinds)}
+    assert len(reached) == 2 * (4 + 4 + 3)
