@@ -394,10 +394,13 @@ int spo_logprob_fwd(const spo_logprob_desc *d, float *logp, float *lse, float *e
  * d_entropy, top_id with d_top_logp.  d_logp, d_entropy [T] and d_top_logp [T][top_k] fp32: each may
  * be NULL for zeros; d_logp needs a target.
  * Logits-in form: d_logits [T, V] in desc dtype, rows V apart, not on top of logits; ws is not needed.
+ * Rows whose |lse| is beyond 128 (SPO_BF16: 2048) are read once more for sums of their own: lse rounded
+ * to fp32 is no longer exact enough there.
  * Head form: d_hidden, d_W, accumulate_dW, chunk_tokens and the workspace are those of
  * spo_pg_loss_bwd; tokens whose factors are both zero are left out of all contractions.  Logit
  * gradients are rounded to bf16 between the contractions, so desc dtype has to be SPO_BF16
- * (SPO_FP32 -> SPO_EUNSUPPORTED: form the logits and use the logits-in form). */
+ * (SPO_FP32 -> SPO_EUNSUPPORTED: form the logits and use the logits-in form).  The softmax part takes
+ * lse as it is, rounded to fp32: up to 1e-3 of that part at 1e4. */
 size_t spo_logprob_bwd_workspace_bytes(const spo_logprob_desc *d, int64_t chunk_tokens);
 int spo_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *entropy, const float *d_logp,
                     const float *d_entropy, const int32_t *top_id, const float *d_top_logp, void *d_hidden,
@@ -412,9 +415,11 @@ int spo_logprob_bwd(const spo_logprob_desc *d, const float *lse, const float *en
  * and keeps the singular vectors.  A zero matrix stays zero; an infinity or a NaN in U makes its
  * matrix NaN.
  * products  SPO_PRODUCTS_FP16: the operands of the products are rounded to 11 bits, X itself is
- *           kept in 22: results to 2e-4 to 8e-4 relative (in 2-norm over the matrix; matrices
- *           whose smaller side is at most 64 are worked on as with SPO_PRODUCTS_SPLIT);
- *           SPO_PRODUCTS_SPLIT: operands of 22 bits, three products for one: about 1e-6.
+ *           kept in 22: results to 1e-3 relative or better (in 2-norm over the matrix, five steps;
+ *           9e-4 where the smaller side is 66, 7e-4 and less from 128 on; matrices whose smaller side is
+ *           at most 64 are worked on as with SPO_PRODUCTS_SPLIT);
+ *           SPO_PRODUCTS_SPLIT: operands of 22 bits, three products for one: 3e-7 to 6e-7, of nearly
+ *           low rank 3e-6.
  * A and the polynomial b A + c A A are held in fp16 parts scaled by 256: coefficients have to keep
  * their entries below 255 (in common use those of A stay below 1.5, the polynomial's below 3).
  * Sums are in fp32 in a fixed order: results are bitwise reproducible.

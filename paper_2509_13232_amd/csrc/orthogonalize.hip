@@ -9,9 +9,10 @@
 // products read hi alone: 2e-4 to 1.7e-3 after five steps (X in 11 bits: up to 2e-2; all of it in bf16: up to 0.16) for
 // 4 bytes more per entry in the epilogue.  Most of what is left comes from the diagonals of A and B, which lie near the mean
 // of the squared singular values, s = |X|_F^2 / k, and near b s + c s^2.  So what is stored is A' = A - s I and
-// B' = c A' A' + (b + 2 c s) A', and X <- (a + b s + c s^2) X + B' X: the same polynomial, 2e-4 to 8e-4.
+// B' = c A' A' + (b + 2 c s) A', and X <- (a + b s + c s^2) X + B' X: the same polynomial, 7e-5 to 7.2e-4
+// from sides of 128 on, 9.4e-4 at 66 x 66.
 // SPO_PRODUCTS_SPLIT keeps A and B as pairs too and forms
-// hi hi + (hi lo + lo hi) / 2048 in every product: 3e-7 to 5e-6, three times the matrix instructions.
+// hi hi + (hi lo + lo hi) / 2048 in every product: 3e-7 to 3.4e-6, three times the matrix instructions.
 //
 // Every matrix in the workspace has its sides rounded up to a step of the contraction (64), zero beyond the true ones: the
 // main loop of gemm_core.hpp then has no ends to look after.
