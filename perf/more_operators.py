@@ -1,0 +1,425 @@
+"""What stands around the head in a training step, as cases that can be timed and compared.
+
+Two kinds of work:
+
+  norm   the normalisation that makes the head's hidden states: its outputs alone ("forward"), or with the gradients of its
+         input, weight and bias ("train");
+  adamw  one AdamW step over many tensors, with its state in 32 or in 8 bits, clipped by the norm of all gradients or not.
+
+Where `own` is false, `run` computes the plain form in 32 bits with elementary torch operations; where it is true,
+it makes the calls of `paper_2509_13232_amd.binding`.
+
+The tensors of a step are views of flat buffers, as programs that reduce gradients in buckets keep them; each begins at a
+multiple of 64 elements, and what lies between them is zero.  A state in 8 bits is held in blocks of 64: for each a power of
+two, for each element of the first moment a sign, 4 bits of exponent and 3 of mantissa, and of the second moment's root 4 and
+4.  A value between two codes goes to the upper one if its place between them is past a threshold, which moves on with the step.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda"
+HIDDEN, VOCAB = 4096, 151936                   # the large LM head of this repository's configurations
+EPS_NORM = 1e-6
+LR, BETA1, BETA2, EPS, WEIGHT_DECAY = 1e-4, 0.9, 0.999, 1e-8, 0.01
+BLOCK = 64                                     # elements of a state in 8 bits that share a scale
+STEPS_BEFORE = 20                              # steps that the states in hand have behind them
+
+
+def _norm(name, path, kind, x, y, w, T, N, pad=0, bias=True):
+    """x, y, w: types of input and its gradient, of output and its gradient, of weight and bias; pad: elements between rows of x."""
+    return dict(name=name, kind="norm", path=path, norm=kind, x=x, y=y, w=w, T=T, N=N, pad=pad, bias=bias)
+
+
+def _adamw(name, bits, param, grad, count, lo, hi, clip=0.0, copy=False):
+    """count tensors of lo to hi elements; clip: the norm that gradients are clipped to (0: they are not); copy: weights in fp32
+    are also left in bf16."""
+    return dict(name=name, kind="adamw", bits=bits, param=param, grad=grad, count=count, lo=lo, hi=hi, clip=clip, copy=copy)
+
+
+def listed():
+    return [
+        # one generated token before it is scored
+        _norm("norm_token", "forward", "rms", "bf16", "bf16", "bf16", 1, HIDDEN, bias=False),
+        # the smallest training run's step
+        _norm("norm_tiny_fp32", "train", "layer", "fp32", "fp32", "fp32", 512, 128),
+        # an odd batch out of a wider buffer, of a model whose width is no power of two
+        _norm("norm_odd", "train", "layer", "bf16", "bf16", "fp32", 713, 1001, pad=23),
+        # a mini-batch that is scored, from a residual stream in fp32
+        _norm("norm_score", "forward", "layer", "fp32", "bf16", "fp32", 17043, HIDDEN),
+        # the small model's step: 64 responses of 128 tokens
+        _norm("norm_small_model", "train", "layer", "bf16", "bf16", "bf16", 8192, 1024),
+        # the whole batch of the headline benchmark
+        _norm("norm_full_batch", "train", "rms", "bf16", "bf16", "fp32", 284780, HIDDEN, bias=False),
+        # the smallest run's weights: head, projection, normalisation
+        _adamw("adamw_tiny", 32, "fp32", "fp32", 6, 128, 128000, clip=1.0),
+        # a model's matrices, biases and weights of normalisations, of any size, with the bf16 weights that the products read
+        _adamw("adamw_tensors", 32, "fp32", "bf16", 150, 257, 1 << 22, clip=1.0, copy=True),
+        # the small model's head
+        _adamw("adamw_head", 32, "bf16", "bf16", 1, 1024 * VOCAB, 1024 * VOCAB),
+        # one weight of a normalisation, state in 8 bits: launches and latency
+        _adamw("adamw8_one", 8, "fp32", "bf16", 1, HIDDEN, HIDDEN),
+        # odd tensors, state in 8 bits
+        _adamw("adamw8_tensors", 8, "fp32", "bf16", 40, 1000, 1 << 22, clip=1.0),
+        # the large head, state in 8 bits: the tensor whose state takes the most memory
+        _adamw("adamw8_head", 8, "bf16", "bf16", 1, HIDDEN * VOCAB, HIDDEN * VOCAB),
+    ]
+
+
+# ------------------------------------------------------------------ drawn cases
+def _log_uniform(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _draw_norm(rng):
+    N = HIDDEN if rng.random() < 0.3 else _log_uniform(rng, 16, 16384)
+    T = _log_uniform(rng, 1, max(1, min(300000, (1 << 29) // N)))
+    x = rng.choice(["bf16", "bf16", "fp32"])
+    kind = rng.choice(["layer", "rms"])
+    return _norm("", rng.choice(["forward", "train", "train"]), kind, x, rng.choice([x, "bf16"]), rng.choice(["fp32", "bf16"]), T, N,
+                 pad=rng.choice([0, 0, 0, 64, 23]), bias=kind == "layer" and rng.random() < 0.7)
+
+
+def _draw_adamw(rng):
+    bits, param = rng.choice([32, 8]), rng.choice(["fp32", "bf16"])
+    count = _log_uniform(rng, 1, 200)
+    hi = _log_uniform(rng, 1000, 1 << 28) // count + 64
+    return _adamw("", bits, param, rng.choice([param, "bf16"]), count, max(1, hi // _log_uniform(rng, 1, 1000)), hi,
+                  clip=rng.choice([0.0, 1.0]), copy=param == "fp32" and rng.random() < 0.5)
+
+
+def draw(rng):
+    case = rng.choice([_draw_norm, _draw_adamw])(rng)
+    del case["name"]
+    return case
+
+
+# ------------------------------------------------------------------ inputs
+def _dtype(name):
+    return {"fp32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def _generator(seed, stream):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed) * 64 + stream)
+    return g
+
+
+def _prepare_norm(case, seed):
+    T, N = case["T"], case["N"]
+    g = _generator(seed, 1)
+    s = dict(case)
+    # a residual stream: a few channels are far larger than the others, tokens differ in scale
+    channel = torch.exp(0.3 * torch.randn(N, generator=g, device=DEV))
+    channel[torch.randint(0, N, (max(1, N // 500),), generator=g, device=DEV)] *= 20.0
+    token = torch.exp(0.5 * torch.randn((T, 1), generator=g, device=DEV))
+    rows = torch.randn((T, N + case["pad"]), generator=g, device=DEV)
+    rows.mul_(token)
+    rows[:, :N].mul_(channel).add_(0.1 * channel)
+    s["x"] = rows.to(_dtype(case["x"]))[:, :N]
+    s["weight"] = (1.0 + 0.1 * torch.randn(N, generator=g, device=DEV)).to(_dtype(case["w"]))
+    s["bias"] = (0.1 * torch.randn(N, generator=g, device=DEV)).to(_dtype(case["w"])) if case["bias"] else None
+    if case["path"] == "train":
+        s["dy"] = torch.randn((T, N), generator=g, device=DEV).mul_(1.0 / T).to(_dtype(case["y"]))
+    return s
+
+
+def _sizes(case):
+    """The tensors' sizes: of the case alone, any from lo to hi."""
+    r = random.Random(case["count"] * 1000003 + case["hi"])
+    return [_log_uniform(r, case["lo"], case["hi"]) for _ in range(case["count"])]
+
+
+def _offsets(sizes):
+    """Where each tensor begins in the flat buffers, and their length."""
+    at, starts = 0, []
+    for n in sizes:
+        starts.append(at)
+        at += (n + BLOCK - 1) // BLOCK * BLOCK
+    return starts, at
+
+
+def _prepare_adamw(case, seed):
+    g = _generator(seed, 2)
+    sizes = _sizes(case)
+    starts, total = _offsets(sizes)
+    blocks = total // BLOCK
+    # gradients whose size differs from row to row, and the moments of steps like these
+    scale = 1e-3 * torch.exp(torch.randn((blocks, 1), generator=g, device=DEV))
+    normal = lambda: torch.randn((blocks, BLOCK), generator=g, device=DEV)   # noqa: E731
+    grad = normal().mul_(scale).to(_dtype(case["grad"]))
+    m = normal().mul_(0.25 * scale)
+    root = normal().mul_(0.3).exp_().mul_(scale)
+    param = normal().mul_(0.02).to(_dtype(case["param"]))
+    for n, at in zip(sizes, starts):
+        for t in (grad, m, root, param):
+            t.view(-1)[at + n:(at + n + BLOCK - 1) // BLOCK * BLOCK] = 0
+    s = dict(case, sizes=sizes, starts=starts, step=STEPS_BEFORE, grad=grad.view(-1), param=param.view(-1))
+    if case["copy"]:
+        s["bf16"] = param.view(-1).to(torch.bfloat16)
+    if case["bits"] == 32:
+        s["m"], s["v"] = m.view(-1), (root * root).view(-1)
+    else:
+        s["m"], s["m_scale"] = _encode(m, 3, STEPS_BEFORE, FIRST)
+        del m
+        s["v"], s["v_scale"] = _encode(root, 4, STEPS_BEFORE, SECOND)
+    return s
+
+
+def prepare(case, seed):
+    return (_prepare_norm if case["kind"] == "norm" else _prepare_adamw)(case, seed)
+
+
+# ------------------------------------------------------------------ one pass, plain
+def _plain_norm(s):
+    x, w = s["x"].float(), s["weight"].float()
+    if s["norm"] == "layer":
+        mean = x.mean(dim=1, keepdim=True)
+        x = x - mean
+    rstd = 1.0 / torch.sqrt((x * x).mean(dim=1, keepdim=True) + EPS_NORM)
+    h = x * rstd
+    y = h * w
+    if s["bias"] is not None:
+        y = y + s["bias"].float()
+    out = dict(y=y.to(_dtype(s["y"])), rstd=rstd[:, 0])
+    if s["norm"] == "layer":
+        out["mean"] = mean[:, 0]
+    if s["path"] == "train":
+        dy = s["dy"].float()
+        out["d_weight"] = (dy * h).sum(dim=0)
+        if s["bias"] is not None:
+            out["d_bias"] = dy.sum(dim=0)
+        g = dy * w
+        dx = g - h * (g * h).mean(dim=1, keepdim=True)
+        if s["norm"] == "layer":
+            dx = dx - g.mean(dim=1, keepdim=True)
+        out["dx"] = (rstd * dx).to(s["x"].dtype)
+    return out
+
+
+# A block's scale is the exponent that its largest value takes once that is no larger than the largest code; codes are the
+# upper bits of values brought to where the exponent field runs from 0 to 15.
+FIRST, SECOND = 0, 1 << 31                      # where the thresholds of the two moments begin
+PER_STEP, PER_PLACE = 0x9E3779B9, 0xC13FA9A9    # the golden ratio's and a like number's fractions of 2^32
+
+
+def _threshold(step, start, bits):
+    """[BLOCK] thresholds of `bits` bits."""
+    place = torch.arange(BLOCK, device=DEV)
+    return ((((step * PER_STEP + start) & 0xFFFFFFFF) + place * PER_PLACE) & 0xFFFFFFFF) >> (32 - bits)
+
+
+def _encode(x, mantissa, step, start):
+    """(codes, scales) of x [blocks, BLOCK] in fp32; the sign is kept where the mantissa leaves a bit for it."""
+    drop = 23 - mantissa
+    magnitude = x.abs()
+    top = magnitude.view(torch.int32).amax(dim=1, keepdim=True).long()
+    scale = ((top + (1 << drop) - 1) >> 23).clamp(15, 255)
+    bits = (magnitude.double() * torch.exp2((15 - scale).double())).float().view(torch.int32)
+    code = (bits + _threshold(step, start, drop).int()) >> drop
+    if mantissa == 4:
+        code = torch.maximum(code, (bits > 0).int())     # a root that is not zero stays above it
+    else:
+        code = code | (x < 0).int() << 7
+    return code.to(torch.uint8).view(-1), scale.to(torch.uint8).view(-1)
+
+
+def _decode(code, scale, mantissa):
+    c = code.view(-1, BLOCK).int()
+    value = ((c & (0xFF >> (4 - mantissa))) << (23 - mantissa)).view(torch.float32).double()
+    value = (value * torch.exp2(scale.view(-1, 1).double() - 15)).float()
+    return torch.where(c >= 128, -value, value) if mantissa == 3 else value
+
+
+def _plain_adamw(s):
+    s["step"] += 1
+    step = s["step"]
+    p, g = s["param"].view(-1, BLOCK), s["grad"].float().view(-1, BLOCK)
+    out = dict(param=s["param"])
+    if s["clip"]:
+        norm = torch.sqrt((s["grad"].double() ** 2).sum()).float()
+        g = g * torch.where(norm > s["clip"], s["clip"] / norm, torch.ones_like(norm))
+        out["norm"] = norm.view(1)
+    if s["bits"] == 32:
+        m, v = s["m"].view(-1, BLOCK), s["v"].view(-1, BLOCK)
+        m.copy_(m * BETA1 + g * (1.0 - BETA1))
+        v.copy_(v * BETA2 + g * g * (1.0 - BETA2))
+        root = torch.sqrt(v)
+        out.update(m=s["m"], v=s["v"])
+    else:
+        m = _decode(s["m"], s["m_scale"], 3) * BETA1 + g * (1.0 - BETA1)
+        root = _decode(s["v"], s["v_scale"], 4)
+        root = torch.sqrt(root * root * BETA2 + g * g * (1.0 - BETA2))
+        for name, value, mantissa, start in (("m", m, 3, FIRST), ("v", root, 4, SECOND)):
+            code, scale = _encode(value, mantissa, step, start)
+            s[name].copy_(code)
+            s[name + "_scale"].copy_(scale)
+        out.update(m=_decode(s["m"], s["m_scale"], 3).to(torch.bfloat16).view(-1), root=_decode(s["v"], s["v_scale"], 4).to(torch.bfloat16).view(-1))
+    change = m / (root * (1.0 / math.sqrt(1.0 - BETA2 ** step)) + EPS) * (LR / (1.0 - BETA1 ** step))
+    new = p.float()
+    new = new - (change + new * (LR * WEIGHT_DECAY))
+    p.copy_(new)
+    if s["copy"]:
+        s["bf16"].copy_(new.view(-1))
+        out["bf16"] = s["bf16"]
+    return out
+
+
+# ------------------------------------------------------------------ one pass, through the framework
+def _kept(s, name, make):
+    """What a program makes once for its buffers and keeps: the descriptor and the workspaces."""
+    if name not in s:
+        s[name] = make()
+    return s[name]
+
+
+def _space(nbytes):
+    return torch.empty(max(256, int(nbytes)), dtype=torch.uint8, device=DEV)
+
+
+def _own_norm(s):
+    from paper_2509_13232_amd import binding as spo
+    kind = spo.SPO_NORM_LAYER if s["norm"] == "layer" else spo.SPO_NORM_RMS
+    d = _kept(s, "desc", lambda: spo.make_norm_desc(s["x"], s["weight"], s["bias"], eps=EPS_NORM, kind=kind, y_dtype=_dtype(s["y"])))
+    y, mean, rstd = spo.spo_norm_fwd(d)
+    out = dict(y=y, rstd=rstd)
+    if s["norm"] == "layer":
+        out["mean"] = mean
+    if s["path"] == "train":
+        ws = _kept(s, "ws", lambda: _space(spo.spo_norm_bwd_workspace_bytes(d)))
+        out["dx"], out["d_weight"], d_bias = spo.spo_norm_bwd(d, mean, rstd, s["dy"], workspace=ws)
+        if s["bias"] is not None:
+            out["d_bias"] = d_bias
+    return out
+
+
+def _tensors(s, spo):
+    """The step's tensors out of the flat buffers."""
+    view = lambda t: [t[at:at + n] for n, at in zip(s["sizes"], s["starts"])]   # noqa: E731
+    if s["bits"] == 32:
+        states = [spo.AdamwState(m, v) for m, v in zip(view(s["m"]), view(s["v"]))]
+    else:
+        scales = lambda t: [t[at // BLOCK:(at + n + BLOCK - 1) // BLOCK] for n, at in zip(s["sizes"], s["starts"])]   # noqa: E731
+        states = [spo.AdamwState(*x) for x in zip(view(s["m"]), view(s["v"]), scales(s["m_scale"]), scales(s["v_scale"]))]
+    return spo.make_adamw_desc(view(s["param"]), view(s["grad"]), states, weight_decay=WEIGHT_DECAY, copies=view(s["bf16"]) if s["copy"] else None)
+
+
+def _own_adamw(s):
+    from paper_2509_13232_amd import binding as spo
+    s["step"] += 1
+    d = _kept(s, "desc", lambda: _tensors(s, spo))
+    out = dict(param=s["param"])
+    if s["clip"]:
+        ws = _kept(s, "ws", lambda: _space(spo.spo_grad_norm_workspace_bytes(d)))
+        out["norm"] = spo.spo_grad_norm(d, workspace=ws)
+    spo.spo_adamw_update(d, lr=LR, step=s["step"], beta1=BETA1, beta2=BETA2, eps=EPS, grad_norm=out.get("norm"), max_norm=s["clip"])
+    if s["bits"] == 32:
+        out.update(m=s["m"], v=s["v"])
+    else:
+        out["m"], out["root"] = spo.spo_adamw_state_values(spo.AdamwState(s["m"], s["v"], s["m_scale"], s["v_scale"]), dtype=torch.bfloat16)
+    if s["copy"]:
+        out["bf16"] = s["bf16"]
+    return out
+
+
+def run(state):
+    if own:
+        return _own_norm(state) if state["kind"] == "norm" else _own_adamw(state)
+    return _plain_norm(state) if state["kind"] == "norm" else _plain_adamw(state)
+
+
+# ------------------------------------------------------------------ what a pass cannot do without
+def work(case):
+    elt = {"fp32": 4, "bf16": 2}
+    if case["kind"] == "norm":
+        T, N = case["T"], case["N"]
+        ways = 2 if case["path"] == "train" else 1       # x, y; and dy, dx
+        return {"bytes": ways * T * N * (elt[case["x"]] + elt[case["y"]]) + N * (elt[case["w"]] + 4 * (ways - 1)) * (1 + case["bias"]), "flops": 0}
+    total = sum(_sizes(case))
+    state = 16 if case["bits"] == 32 else 4.0 + 4.0 / BLOCK + 4
+    # weights read and written, gradients read, state read and written (8 bits: and its values)
+    return {"bytes": total * (2 * elt[case["param"]] + elt[case["grad"]] + state + 2 * case["copy"]), "flops": 0}
+
+
+# ------------------------------------------------------------------ from the definition, in 64 bits
+def _exact_norm(case, s):
+    x = s["x"].double().requires_grad_()
+    w = s["weight"].double().requires_grad_()
+    b = s["bias"].double().requires_grad_() if case["bias"] else None
+    N = (case["N"],)
+    y = torch.nn.functional.layer_norm(x, N, w, b, EPS_NORM) if case["norm"] == "layer" else torch.nn.functional.rms_norm(x, N, w, EPS_NORM)
+    out = dict(y=y.detach())
+    with torch.no_grad():
+        spread = x.var(dim=1, correction=0) if case["norm"] == "layer" else torch.linalg.vector_norm(x, dim=1) ** 2 / case["N"]
+        out["rstd"] = (spread + EPS_NORM) ** -0.5
+        if case["norm"] == "layer":
+            out["mean"] = x.sum(dim=1) / case["N"]
+    if case["path"] == "train":
+        of = [x, w] + ([b] if case["bias"] else [])
+        got = torch.autograd.grad(y, of, s["dy"].double())
+        out["dx"], out["d_weight"] = got[0], got[1]
+        if case["bias"]:
+            out["d_bias"] = got[2]
+    return out
+
+
+def _exact_codes(x, mantissa, step, start):
+    """x [blocks, BLOCK] in 64 bits, each at the code that it is held as."""
+    size = x.abs()
+    part, power = torch.frexp(size.amax(dim=1, keepdim=True))
+    power = power + (part > 1.0 - 2.0 ** -(mantissa + 1)).int() - 1          # of the block's largest binade
+    power = power.clamp(min=15 - 127).double()
+    # codes of a binade are 2^-mantissa of it apart, and those of the lowest one go on down to zero
+    _, binade = torch.frexp(size)
+    gap = torch.exp2(torch.maximum(binade.double() - 1, power - 14) - mantissa)
+    place = torch.arange(BLOCK, device=x.device, dtype=torch.int64)
+    turn = (step * 2654435769 + place * 3242174889 + start) % 2 ** 32
+    fraction = torch.floor(turn.double() / 2.0 ** (9 + mantissa)) / 2.0 ** (23 - mantissa)
+    held = torch.floor(size / gap + fraction) * gap
+    if mantissa == 4:
+        held = torch.where(size > 0, torch.maximum(held, torch.exp2(power - 18).expand_as(held)), held)
+    return torch.copysign(held, x)
+
+
+def _exact_adamw(case, s):
+    step = s["step"] + 1
+    g = s["grad"].double().view(-1, BLOCK)
+    out = {}
+    if case["clip"]:
+        norm = torch.linalg.vector_norm(g)
+        out["norm"] = norm.view(1)
+        g = g * min(1.0, case["clip"] / float(norm))
+    if case["bits"] == 32:
+        m, v = s["m"].double().view(-1, BLOCK), s["v"].double().view(-1, BLOCK)
+    else:
+        scale = lambda t: torch.exp2(t.double() - 15).view(-1, 1)   # noqa: E731
+        tiny = lambda c, bits: torch.ldexp(torch.where(c >> bits == 0, c, (c & (1 << bits) - 1) + (1 << bits)).double() * 2.0 ** -(126 + bits),  # noqa: E731
+                                           ((c >> bits) - 1).clamp(min=0).double())
+        c = s["m"].view(-1, BLOCK).long()
+        m = tiny(c & 127, 3) * scale(s["m_scale"]) * (1 - 2 * (c >> 7)).double()
+        v = (tiny(s["v"].view(-1, BLOCK).long(), 4) * scale(s["v_scale"])) ** 2
+        del c
+    m = torch.lerp(g, m, BETA1)
+    v = torch.lerp(g * g, v, BETA2)
+    p = s["param"].double().view(-1, BLOCK)
+    new = p * (1.0 - LR * WEIGHT_DECAY) - LR * (m / (1.0 - BETA1 ** step)) / (torch.sqrt(v / (1.0 - BETA2 ** step)) + EPS)
+    out["param"] = new.view(-1)
+    if case["copy"]:
+        out["bf16"] = out["param"]
+    if case["bits"] == 32:
+        out.update(m=m.view(-1), v=v.view(-1))
+    else:
+        out["m"] = _exact_codes(m, 3, step, 0).view(-1)
+        out["root"] = _exact_codes(torch.sqrt(v), 4, step, 2 ** 31).view(-1)
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    with torch.enable_grad():
+        return _exact_norm(case, s) if case["kind"] == "norm" else _exact_adamw(case, s)
