@@ -223,7 +223,7 @@ def _encode(x, mantissa, step, start):
     bits = (magnitude.double() * torch.exp2((15 - scale).double())).float().view(torch.int32)
     code = (bits + _threshold(step, start, drop).int()) >> drop
     if mantissa == 4:
-        code = torch.maximum(code, (bits > 0).int())     # a root that is not zero stays above it
+        code = torch.maximum(code, (x > 0).int())        # a root that is not zero stays above it
     else:
         code = code | (x < 0).int() << 7
     return code.to(torch.uint8).view(-1), scale.to(torch.uint8).view(-1)
