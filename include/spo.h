@@ -453,6 +453,106 @@ int spo_muon_update(const spo_orth_desc *d, void *W, int w_dtype, float *momentu
                     spo_stream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Normalisation of rows: what makes the hidden states that a head reads, and the way of their gradient back through it.
+ * For a row x of `cols` elements, with a weight w and a bias b (each may be NULL: ones, zeros):
+ *   SPO_NORM_LAYER  mean = sum x / cols;  rstd = (sum (x - mean)^2 / cols + eps)^-1/2;  h = (x - mean) rstd
+ *   SPO_NORM_RMS    rstd = (sum x^2 / cols + eps)^-1/2;                                 h = x rstd
+ *   y = h w + b
+ * and, with g = dy w:
+ *   dx = rstd (g - sum g / cols - h sum (g h) / cols), SPO_NORM_RMS without the second term;
+ *   d_weight = sum over rows of dy h;  d_bias = sum over rows of dy.
+ * Sums in fp32 in a fixed order (results are bitwise reproducible), in 64 bits where squares leave fp32's range.  A mean far
+ * from zero costs no digits: what rounding it takes off is found again from the row, in the backward too.  A row that holds
+ * a NaN, or with SPO_NORM_LAYER an infinity, gives NaN throughout (with SPO_NORM_RMS an infinity gives NaN there and zeros
+ * elsewhere); its dx is NaN, and so is d_weight where its h is.  A row of equal elements with eps = 0 gives NaN.
+ * ------------------------------------------------------------------------- */
+#define SPO_NORM_LAYER 0
+#define SPO_NORM_RMS 1
+typedef struct {
+    size_t struct_size;          /* sizeof(spo_norm_desc), checked                            */
+    int kind;                    /* SPO_NORM_LAYER or SPO_NORM_RMS                            */
+    int x_dtype, y_dtype;        /* SPO_BF16 or SPO_FP32                                      */
+    int w_dtype;                 /* of weight and bias                                        */
+    int64_t rows, cols;          /* rows >= 0; 1 <= cols <= 65536                             */
+    const void *x;               /* rows of cols elements, aligned to the element             */
+    int64_t x_stride;            /* elements from one row of x to the next; 0: cols           */
+    const void *weight, *bias;   /* [cols] or NULL                                            */
+    float eps;                   /* >= 0                                                      */
+} spo_norm_desc;
+
+/* Forward.  y in y_dtype, rows y_stride elements apart (0: cols); it may be x if type and stride are the same.
+ * mean (SPO_NORM_LAYER), rstd [rows] fp32, inputs of the backward: each may be NULL. */
+int spo_norm_fwd(const spo_norm_desc *d, void *y, int64_t y_stride, float *mean, float *rstd, spo_stream_t stream);
+
+/* Backward.  mean (SPO_NORM_LAYER), rstd from the forward of the same desc; dy in dy_dtype, rows dy_stride apart (0: cols).
+ * dx [rows][cols] contiguous in dx_dtype, d_weight, d_bias [cols] in d_w_dtype: each may be NULL; dx may be dy, or x, if
+ * that is contiguous and of its type.  accumulate = 1: d_weight and d_bias are added to (needs d_w_dtype = SPO_FP32).
+ * No rows: d_weight and d_bias are zeros.  The workspace size never shrinks with rows or cols. */
+size_t spo_norm_bwd_workspace_bytes(const spo_norm_desc *d);
+int spo_norm_bwd(const spo_norm_desc *d, const float *mean, const float *rstd, const void *dy, int dy_dtype, int64_t dy_stride,
+                 void *dx, int dx_dtype, void *d_weight, void *d_bias, int d_w_dtype, int accumulate, void *ws, size_t ws_bytes,
+                 spo_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * AdamW over many tensors at once, for what the orthogonalised step is not for: heads and embeddings, weights of
+ * normalisations, biases, or all of a model.  In the t-th step, for every element of every tensor:
+ *   g <- grad * min(1, max_norm / norm)                           (without grad_norm: g = grad)
+ *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2
+ *   param <- param - (lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps) + lr weight_decay param)
+ * in fp32, param rounded once.  copy receives the new param in bf16, from its fp32 value.
+ * State: state_bits = 32: m, v fp32 [n].  state_bits = 8: m, v uint8 [n], one code per element, and m_scale, v_scale uint8
+ * [ceil(n / 64)], one power of two per 64 elements; v holds the root of the second moment.  m has 4 significant bits over a
+ * range of 2^14 below its block's largest, the root 5 over 2^14 (2^28 of the second moment), with subnormals below; a root
+ * that is not zero stays above it.  Codes are rounded by thresholds that move with the step, so that changes smaller than a
+ * code add up over steps; a step's codes depend on its number and on an element's place modulo 64 alone.  Zeros in all arrays
+ * are the state before the first step.  A value that is not finite makes the 64 of its block NaN, one of 3.29e38 or more too.
+ * Arrays that are written must not overlap each other or what is read.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    void *param;                 /* [n] in param_dtype                                        */
+    const void *grad;            /* [n] in grad_dtype                                         */
+    void *m, *v;                 /* [n] fp32 or uint8                                         */
+    uint8_t *m_scale, *v_scale;  /* state_bits = 8                                            */
+    void *copy;                  /* [n] bf16 or NULL; needs param_dtype = SPO_FP32            */
+    int64_t n;                   /* elements, 0 <= n <= 2^36; 0: nothing else is looked at    */
+    double weight_decay;         /* >= 0                                                      */
+    int32_t param_dtype, grad_dtype;
+} spo_adamw_tensor;
+typedef struct {
+    size_t struct_size;          /* sizeof(spo_adamw_desc), checked                           */
+    int state_bits;              /* 32 or 8                                                   */
+    int64_t count;               /* tensors, >= 0                                             */
+    const spo_adamw_tensor *tensors;  /* HOST array [count], read during the call             */
+} spo_adamw_desc;
+
+/* norm[0] = sqrt(sum of squares of all gradients), fp32: the sum is formed in 64 bits in a fixed order.  Of the tensors only
+ * grad, grad_dtype and n are looked at.  The workspace size depends on count alone and never shrinks with it. */
+size_t spo_grad_norm_workspace_bytes(const spo_adamw_desc *d);
+int spo_grad_norm(const spo_adamw_desc *d, float *norm, void *ws, size_t ws_bytes, spo_stream_t stream);
+
+/* The step, in place.
+ * step          number of this step, 1 for the first.  step_device, a device int64[1], holds the number of steps taken instead
+ *               and is counted up by the call; lr_device, a device fp32[1], takes lr's place.  With either a captured graph's
+ *               replays move on by themselves; a small launch more, and ws, spo_adamw_update_workspace_bytes() bytes,
+ *               256-byte aligned, is needed (otherwise it may be NULL).
+ * grad_norm     device fp32[1] as spo_grad_norm leaves it, or NULL.  If it is not finite nothing is written, and
+ *               step_device is not counted up.
+ * rounding      of params in bf16: SPO_ROUND_NEAREST, or SPO_ROUND_THRESHOLD, by thresholds that move with the step, as the
+ *               states are: without a copy in fp32, changes below half a place add up over steps instead of being lost.
+ * A step of up to 60 tensors (48 in 8 bits) is one launch. */
+#define SPO_ROUND_NEAREST 0
+#define SPO_ROUND_THRESHOLD 1
+size_t spo_adamw_update_workspace_bytes(void);
+int spo_adamw_update(const spo_adamw_desc *d, double lr, const float *lr_device, double beta1, double beta2, double eps, int64_t step,
+                     int64_t *step_device, const float *grad_norm, double max_norm, int rounding, void *ws, size_t ws_bytes,
+                     spo_stream_t stream);
+
+/* The values that an 8-bit state stands for, of one tensor: the first moment and the root of the second, [n] in dtype (bf16
+ * holds them exactly).  Either output may be NULL, and its codes with it. */
+int spo_adamw_state_values(const uint8_t *m, const uint8_t *v, const uint8_t *m_scale, const uint8_t *v_scale, int64_t n, void *m_out,
+                           void *root_out, int dtype, spo_stream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Per-kernel timing (measurement aid, not part of the method; with the static
  * buffer of spo_sample_prompts_static the only state the library keeps).  While enabled, the loss and score entry points bracket
  * each launch of their heavy kernels with a pair of HIP events on the launch stream.

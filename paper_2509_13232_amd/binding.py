@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from collections import namedtuple
 
 import torch
 
@@ -19,6 +20,9 @@ SPO_W_VH, SPO_W_HV = 0, 1
 SPO_SAMPLE_STATIC_MAX_N = 1 << 20
 SPO_MAX_TOP_K = 64
 SPO_PRODUCTS_FP16, SPO_PRODUCTS_SPLIT = 0, 1
+SPO_NORM_LAYER, SPO_NORM_RMS = 0, 1
+SPO_ROUND_NEAREST, SPO_ROUND_THRESHOLD = 0, 1
+SPO_STATE_BLOCK = 64
 
 EXPORTS = (
     "spo_status_string", "spo_sample_prompts_workspace_bytes", "spo_sample_prompts",
@@ -32,6 +36,8 @@ EXPORTS = (
     "spo_logprob_fwd_workspace_bytes", "spo_logprob_fwd",
     "spo_logprob_bwd_workspace_bytes", "spo_logprob_bwd",
     "spo_orthogonalize_workspace_bytes", "spo_orthogonalize", "spo_muon_update",
+    "spo_norm_fwd", "spo_norm_bwd_workspace_bytes", "spo_norm_bwd",
+    "spo_grad_norm_workspace_bytes", "spo_grad_norm", "spo_adamw_update_workspace_bytes", "spo_adamw_update", "spo_adamw_state_values",
     "spo_kernel_timing_enable", "spo_kernel_timing_read",
 )
 TIMING_CLASSES = ("fwd_sweep", "bwd_recompute", "bwd_dhidden", "bwd_dw", "logits_fwd", "logits_bwd", "logits_to_dz")
@@ -68,6 +74,28 @@ class OrthDesc(C.Structure):
         ("struct_size", C.c_size_t), ("batch", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64),
         ("steps", C.c_int32), ("products", C.c_int),
         ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float),
+    ]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_size_t), ("kind", C.c_int), ("x_dtype", C.c_int), ("y_dtype", C.c_int), ("w_dtype", C.c_int),
+        ("rows", C.c_int64), ("cols", C.c_int64), ("x", C.c_void_p), ("x_stride", C.c_int64),
+        ("weight", C.c_void_p), ("bias", C.c_void_p), ("eps", C.c_float),
+    ]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [
+        ("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+        ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64),
+        ("weight_decay", C.c_double), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32),
+    ]
+
+
+class AdamwDesc(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_size_t), ("state_bits", C.c_int), ("count", C.c_int64), ("tensors", C.POINTER(AdamwTensor)),
     ]
 
 
@@ -136,6 +164,22 @@ def lib():
         L.spo_orthogonalize.argtypes = [C.POINTER(OrthDesc), vp, C.c_int, i64, i64, vp, C.c_int, vp, sz, vp]
         L.spo_muon_update.restype = C.c_int
         L.spo_muon_update.argtypes = [C.POINTER(OrthDesc), vp, C.c_int, vp, vp, C.c_int, f32, C.c_int, f32, f32, f32, vp, sz, vp]
+        L.spo_norm_fwd.restype = C.c_int
+        L.spo_norm_fwd.argtypes = [C.POINTER(NormDesc), vp, i64, vp, vp, vp]
+        L.spo_norm_bwd_workspace_bytes.restype = sz
+        L.spo_norm_bwd_workspace_bytes.argtypes = [C.POINTER(NormDesc)]
+        L.spo_norm_bwd.restype = C.c_int
+        L.spo_norm_bwd.argtypes = [C.POINTER(NormDesc), vp, vp, vp, C.c_int, i64, vp, C.c_int, vp, vp, C.c_int, C.c_int, vp, sz, vp]
+        L.spo_grad_norm_workspace_bytes.restype = sz
+        L.spo_grad_norm_workspace_bytes.argtypes = [C.POINTER(AdamwDesc)]
+        L.spo_grad_norm.restype = C.c_int
+        L.spo_grad_norm.argtypes = [C.POINTER(AdamwDesc), vp, vp, sz, vp]
+        L.spo_adamw_update_workspace_bytes.restype = sz
+        L.spo_adamw_update_workspace_bytes.argtypes = []
+        L.spo_adamw_update.restype = C.c_int
+        L.spo_adamw_update.argtypes = [C.POINTER(AdamwDesc), f64, vp, f64, f64, f64, i64, vp, vp, f64, C.c_int, vp, sz, vp]
+        L.spo_adamw_state_values.restype = C.c_int
+        L.spo_adamw_state_values.argtypes = [vp, vp, vp, vp, i64, vp, vp, C.c_int, vp]
         L.spo_kernel_timing_enable.restype = C.c_int
         L.spo_kernel_timing_enable.argtypes = [C.c_int]
         L.spo_kernel_timing_read.restype = C.c_int
@@ -666,3 +710,239 @@ def spo_muon_update(W, momentum, grad, lr, mu=0.95, nesterov=True, weight_decay=
     _check(lib().spo_muon_update(C.byref(d), _ptr(W), _dt(W.dtype), _ptr(momentum), _ptr(grad), _dt(grad.dtype), float(mu),
                                  int(bool(nesterov)), float(lr), float(weight_decay), float(scale), _ptr(ws), ws.numel(), _stream()),
            "spo_muon_update")
+
+
+# ------------------------------------------------------------ normalisation
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+def _here(t, name):
+    """Kernels run on the current device's stream: a tensor of another device is refused."""
+    if t is not None and t.device.index is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: is on {t.device}, and the current device is {torch.cuda.current_device()}")
+
+
+def _want_float(t, name, n=None):
+    if t is not None:
+        _want(t, t.dtype if t.dtype in _FLOATS else torch.float32, name, n)
+        _here(t, name)
+
+
+def _row_stride(t, name, shape=None):
+    """Elements from row to row of a CUDA tensor [rows, cols] whose rows are consecutive and do not overlap."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected {'[rows, cols]' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
+    rows, cols = t.shape
+    apart = t.stride(0) if rows > 1 else cols
+    if not t.is_cuda or t.dtype not in _FLOATS or (cols > 1 and t.stride(1) != 1) or apart < cols:
+        raise TypeError(f"{name}: expected a CUDA tensor [rows, cols] of torch.float32 or torch.bfloat16 with consecutive rows")
+    _here(t, name)
+    return apart
+
+
+def make_norm_desc(x, weight=None, bias=None, eps=1e-6, kind=SPO_NORM_LAYER, y_dtype=None):
+    """Builds the C descriptor; returns (desc, keepalive tuple).  x: [rows, cols], rows of consecutive elements, any distance of at
+    least cols apart.  weight, bias: [cols] of one type, or None for ones and zeros.  y_dtype: of the outputs (x's)."""
+    d = NormDesc()
+    d.struct_size = C.sizeof(NormDesc)
+    apart = _row_stride(x, "x")
+    rows, cols = x.shape
+    _want_float(weight, "weight", cols)
+    _want_float(bias, "bias", cols)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("weight and bias: expected tensors of one type")
+    given = weight if weight is not None else bias
+    d.kind, d.x_dtype, d.y_dtype, d.w_dtype = int(kind), _dt(x.dtype), _dt(y_dtype or x.dtype), SPO_FP32 if given is None else _dt(given.dtype)
+    d.rows, d.cols, d.x_stride, d.eps = rows, cols, apart, float(eps)
+    d.x, d.weight, d.bias = _ptr(x), _ptr(weight), _ptr(bias)
+    return d, (x, weight, bias, y_dtype or x.dtype)
+
+
+def spo_norm_fwd(desc, out=None, want_stats=True):
+    """Returns (y[rows, cols], mean[rows] or None, rstd[rows] or None), y in out if that is given (it may be x)."""
+    d, keep = desc
+    x = keep[0]
+    if out is None:
+        out, apart = torch.empty((d.rows, d.cols), dtype=keep[3], device=x.device), d.cols
+    else:
+        apart = _row_stride(out, "out", (d.rows, d.cols))
+        if out.dtype != keep[3]:
+            raise TypeError(f"out: expected {keep[3]}")
+    rstd = _per_token(d.rows, x.device) if want_stats else None
+    mean = _per_token(d.rows, x.device) if want_stats and d.kind == SPO_NORM_LAYER else None
+    _check(lib().spo_norm_fwd(C.byref(d), _ptr(out), apart, _ptr(mean), _ptr(rstd), _stream()), "spo_norm_fwd")
+    return out, mean, rstd
+
+
+def spo_norm_bwd_workspace_bytes(desc) -> int:
+    return int(lib().spo_norm_bwd_workspace_bytes(C.byref(desc[0])))
+
+
+def spo_norm_bwd(desc, mean, rstd, dy, dx=None, dx_dtype=None, d_weight=None, d_bias=None, d_w_dtype=torch.float32, accumulate=False,
+                 want_dx=True, want_dw=True, workspace=None):
+    """Returns (dx[rows, cols] or None, d_weight[cols] or None, d_bias[cols] or None): those of the descriptor's weight and bias,
+    and only if want_dw.  mean is None for SPO_NORM_RMS.  dx, d_weight, d_bias: where to write (dx may be dy, or x if contiguous)."""
+    d, keep = desc
+    x, weight, bias, _ = keep
+    dev = x.device
+    apart = _row_stride(dy, "dy", (d.rows, d.cols))
+    if d.kind == SPO_NORM_LAYER and mean is None:
+        raise TypeError("mean: expected the forward's")
+    _want(rstd, torch.float32, "rstd", d.rows)
+    _want(mean, torch.float32, "mean", d.rows)
+    if not want_dx:
+        dx = None
+    elif dx is None:
+        dx = torch.empty((d.rows, d.cols), dtype=dx_dtype or x.dtype, device=dev)
+    else:
+        _want_float(dx, "dx", d.rows * d.cols)
+        if tuple(dx.shape) != (d.rows, d.cols):
+            raise ValueError(f"dx: expected {(d.rows, d.cols)}, got {tuple(dx.shape)}")
+    grads = []
+    for name, of, given in (("d_weight", weight, d_weight), ("d_bias", bias, d_bias)):
+        if of is None or not want_dw:
+            given = None
+        elif given is not None:
+            _want_float(given, name, d.cols)
+        elif accumulate:
+            raise ValueError(f"accumulate needs an existing {name}")
+        else:
+            given = torch.empty(d.cols, dtype=d_w_dtype, device=dev)
+        grads.append(given)
+    types = {g.dtype for g in grads if g is not None}
+    if len(types) > 1:
+        raise TypeError("d_weight and d_bias: expected tensors of one type")
+    ws = _workspace(lib().spo_norm_bwd_workspace_bytes(C.byref(d)), dev, workspace)
+    _check(lib().spo_norm_bwd(C.byref(d), _ptr(mean), _ptr(rstd), _ptr(dy), _dt(dy.dtype), apart, _ptr(dx), _dt(dx.dtype) if dx is not None else 0,
+                              _ptr(grads[0]), _ptr(grads[1]), _dt(types.pop()) if types else 0, int(bool(accumulate)), _ptr(ws), ws.numel(),
+                              _stream()), "spo_norm_bwd")
+    return dx, grads[0], grads[1]
+
+
+# -------------------------------------------------------------------- AdamW
+# A tensor's moments: fp32 of its shape; or codes (uint8, of its shape) and scales (uint8, one per 64 elements), where v holds the
+# root of the second moment.
+AdamwState = namedtuple("AdamwState", ["m", "v", "m_scale", "v_scale"], defaults=[None, None])
+
+
+def adamw_state(param, bits=32):
+    """The state of a tensor before its first step."""
+    if bits not in (8, 32):
+        raise ValueError("bits: expected 8 or 32")
+    make = lambda n, dtype: torch.zeros(n, dtype=dtype, device=param.device)   # noqa: E731
+    if bits == 32:
+        return AdamwState(make(param.shape, torch.float32), make(param.shape, torch.float32))
+    blocks = -(-param.numel() // SPO_STATE_BLOCK)
+    return AdamwState(*(make(n, torch.uint8) for n in (param.shape, param.shape, blocks, blocks)))
+
+
+def _disjoint(written, read):
+    """No array that is written shares memory with another one: (address, bytes, name) of each."""
+    spans = sorted((a, a + n, name, w) for w, of in ((True, written), (False, read)) for a, n, name in of if n)
+    reach = reach_written = (0, "")    # how far what came before goes, and what of it is written
+    for a, end, name, w in spans:
+        if a < (reach if w else reach_written)[0]:
+            raise ValueError(f"{name}: overlaps {(reach if w else reach_written)[1]}")
+        reach = max(reach, (end, name))
+        if w:
+            reach_written = max(reach_written, (end, name))
+
+
+def make_adamw_desc(params, grads, states, weight_decay=0.0, copies=None):
+    """Builds the C descriptor of a step over many tensors; returns (desc, keepalive tuple).  All contiguous; params, grads fp32 or
+    bf16; states as adamw_state makes them, all of one kind; weight_decay: one number, or one per tensor; copies: bf16
+    tensors that take the new values of fp32 params, or None in the place of any."""
+    params, grads, states = list(params), list(grads), list(states)
+    n = len(params)
+    decay = [float(w) for w in weight_decay] if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * n
+    copies = [None] * n if copies is None else list(copies)
+    for name, of in (("grads", grads), ("states", states), ("weight_decay", decay), ("copies", copies)):
+        if len(of) != n:
+            raise ValueError(f"{name}: expected {n}, one per tensor, got {len(of)}")
+    eight = n > 0 and states[0].m.dtype == torch.uint8
+    kind = torch.uint8 if eight else torch.float32
+    table = (AdamwTensor * n)()
+    written, read = [], []
+    for i, (p, g, s, copy) in enumerate(zip(params, grads, states, copies)):
+        size = p.numel()
+        _want_float(p, f"params[{i}]")
+        _want_float(g, f"grads[{i}]", size)
+        for name in ("m", "v"):
+            t = getattr(s, name)
+            if t is None:
+                raise TypeError(f"states[{i}].{name}: expected a tensor")
+            _want(t, kind, f"states[{i}].{name}", size)
+        for name in ("m_scale", "v_scale"):
+            if (getattr(s, name) is not None) != eight:
+                raise TypeError(f"states[{i}].{name}: expected {'a tensor' if eight else 'None'}")
+            _want(getattr(s, name), torch.uint8, f"states[{i}].{name}", -(-size // SPO_STATE_BLOCK))
+        if copy is not None:
+            _want(copy, torch.bfloat16, f"copies[{i}]", size)
+            if p.dtype != torch.float32:
+                raise TypeError(f"copies[{i}]: the tensor itself is not of torch.float32")
+        t = table[i]
+        t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy = (_ptr(x) for x in (p, g, *s, copy))
+        t.n, t.weight_decay, t.param_dtype, t.grad_dtype = size, decay[i], _dt(p.dtype), _dt(g.dtype)
+        span = lambda x, name: (x.data_ptr(), x.numel() * x.element_size(), f"{name}[{i}]")   # noqa: E731
+        written += [span(x, name) for x, name in ((p, "params"), (s.m, "states"), (s.v, "states"), (s.m_scale, "states"), (s.v_scale, "states"),
+                                                  (copy, "copies")) if x is not None]
+        read.append(span(g, "grads"))
+    _disjoint(written, read)
+    d = AdamwDesc()
+    d.struct_size, d.state_bits, d.count = C.sizeof(AdamwDesc), 8 if eight else 32, n
+    d.tensors = C.cast(table, C.POINTER(AdamwTensor))
+    return d, (table, params, grads, states, copies)
+
+
+def _step_device(desc):
+    of = desc[1][1]
+    return of[0].device if of else torch.device("cuda", torch.cuda.current_device())
+
+
+def spo_grad_norm_workspace_bytes(desc) -> int:
+    return int(lib().spo_grad_norm_workspace_bytes(C.byref(desc[0])))
+
+
+def spo_grad_norm(desc, workspace=None):
+    """The norm of all gradients of the descriptor's tensors together: fp32[1]."""
+    d = desc[0]
+    dev = _step_device(desc)
+    norm = torch.empty(1, dtype=torch.float32, device=dev)
+    ws = _workspace(lib().spo_grad_norm_workspace_bytes(C.byref(d)), dev, workspace)
+    _check(lib().spo_grad_norm(C.byref(d), _ptr(norm), _ptr(ws), ws.numel(), _stream()), "spo_grad_norm")
+    return norm
+
+
+def spo_adamw_update_workspace_bytes() -> int:
+    return int(lib().spo_adamw_update_workspace_bytes())
+
+
+def spo_adamw_update(desc, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_norm=None, max_norm=0.0, rounding=SPO_ROUND_NEAREST, workspace=None):
+    """One step, IN PLACE on the descriptor's params, states and copies.  step: the number of this step, 1 for the first, or a CUDA
+    int64[1] that holds the steps taken and is counted up; lr: a number or a CUDA fp32[1].  grad_norm: fp32[1] as spo_grad_norm
+    leaves it, gradients are then scaled down to max_norm; None: they are taken as they are."""
+    lr_t, step_t = (x if isinstance(x, torch.Tensor) else None for x in (lr, step))
+    _want(lr_t, torch.float32, "lr", 1)
+    _want(step_t, torch.int64, "step", 1)
+    _want(grad_norm, torch.float32, "grad_norm", 1)
+    ws = workspace
+    if ws is not None or lr_t is not None or step_t is not None:
+        ws = _workspace(lib().spo_adamw_update_workspace_bytes(), _step_device(desc), workspace)
+    _check(lib().spo_adamw_update(C.byref(desc[0]), 0.0 if lr_t is not None else float(lr), _ptr(lr_t), float(beta1), float(beta2), float(eps),
+                                  0 if step_t is not None else int(step), _ptr(step_t), _ptr(grad_norm), float(max_norm), int(rounding), _ptr(ws),
+                                  0 if ws is None else ws.numel(), _stream()), "spo_adamw_update")
+
+
+def spo_adamw_state_values(state, dtype=torch.bfloat16):
+    """What an 8-bit state stands for: (first moment, root of the second), flat, in bf16 (exact) or fp32."""
+    n = state.m.numel()
+    for t, name, size in ((state.m, "m", n), (state.v, "v", n), (state.m_scale, "m_scale", -(-n // SPO_STATE_BLOCK)),
+                          (state.v_scale, "v_scale", -(-n // SPO_STATE_BLOCK))):
+        if t is None:
+            raise TypeError(f"{name}: expected a state in 8 bits")
+        _want(t, torch.uint8, name, size)
+    _here(state.m, "state")
+    m, root = (torch.empty(n, dtype=dtype, device=state.m.device) for _ in range(2))
+    _check(lib().spo_adamw_state_values(_ptr(state.m), _ptr(state.v), _ptr(state.m_scale), _ptr(state.v_scale), n, _ptr(m), _ptr(root), _dt(dtype),
+                                        _stream()), "spo_adamw_state_values")
+    return m, root
