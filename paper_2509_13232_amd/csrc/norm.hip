@@ -7,13 +7,15 @@
 // The mean is rounded to fp32; rows far from zero lose digits of x - mu to that, all elements alike, so the sum of what is left
 // (x - rounded mu) is taken as well and put right, in the backward from the row itself.
 #include <algorithm>
+#include <type_traits>
 
 #include "vec8.hpp"
 
 namespace spo {
 
 constexpr int kMostCols = 65536;
-constexpr int kParts = 256;  // workgroups of the backward: each leaves one row of partial sums
+constexpr int kParts = 512;        // most workgroups of the backward: each leaves one row of partial sums
+constexpr int kColumnParts = 256;   // ... and of the one that takes rows by columns
 
 struct NormArgs {
     const void *x;
@@ -23,47 +25,76 @@ struct NormArgs {
     float eps;
 };
 
-// Sums over the TR threads that share a row, in a fixed order; every thread receives them.  TR > 64: all threads of the workgroup
-// call this together; scratch holds M floats per wavefront and is free again after the next such call with the other scratch.
-template <int TR, int M, typename T>
-__device__ __forceinline__ void row_sums(T (&v)[M], T *scratch) {
+// Sums over a wavefront by moves between lanes: within rows of 16, then from row to row; the last lane's are everybody's.
+template <int M>
+__device__ __forceinline__ void wave_sums(float (&v)[M]) {
+    const auto step = [&](auto control, auto rows) {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+            v[m] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v[m]), decltype(control)::value, decltype(rows)::value, 0xf, false));
+    };
+    typedef std::integral_constant<int, 0xf> All;
+    step(std::integral_constant<int, 0x111>{}, All{});  // from one lane below
+    step(std::integral_constant<int, 0x112>{}, All{});
+    step(std::integral_constant<int, 0x114>{}, All{});
+    step(std::integral_constant<int, 0x118>{}, All{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // a row's last lane to the next row
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // the second row's last lane to the upper half
+#pragma unroll
+    for (int m = 0; m < M; ++m) v[m] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v[m]), kWave - 1));
+}
+template <int M>
+__device__ __forceinline__ void wave_sums(double (&v)[M]) {
 #pragma unroll
     for (int m = 0; m < M; ++m) v[m] = wave_sum(v[m]);
+}
+// Sums over the TR threads that share a row, in a fixed order; every thread receives them.  TR > 64: all threads of the workgroup
+// call this together; scratch holds M numbers per wavefront and is free again after the next such call with another scratch.
+template <int TR, int M, typename T>
+__device__ __forceinline__ void row_sums(T (&v)[M], T *scratch) {
+    wave_sums(v);
     if constexpr (TR > kWave) {
         const int wave = threadIdx.x / kWave;
         if ((threadIdx.x & (kWave - 1)) == 0)
 #pragma unroll
             for (int m = 0; m < M; ++m) scratch[wave * M + m] = v[m];
         __syncthreads();
-        const T *of = scratch + (threadIdx.x / TR) * (TR / kWave) * M;
 #pragma unroll
-        for (int m = 0; m < M; ++m) {
-            v[m] = T(0);
-            for (int i = 0; i < TR / kWave; ++i) v[m] += of[i * M + m];
-        }
+        for (int m = 0; m < M; ++m) v[m] = T(0);
+        for (int i = 0; i < TR / kWave; ++i)
+#pragma unroll
+            for (int m = 0; m < M; ++m) v[m] += scratch[i * M + m];
     }
 }
 
-constexpr int threads_of(int TR) { return TR < 256 ? 256 : TR; }
+constexpr int kFwdThreads = 256;  // of a workgroup, where a wavefront has a row to itself
+constexpr int threads_of(int TR) { return TR < kFwdThreads ? kFwdThreads : TR; }
 constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e38f;  // a variance below, sums of squares above: formed again in 64 bits
+// Elements of a vector: 16 bytes of bf16; four where fp32 is among the arrays, so that a wavefront's loads are whole lines
+// (17043 rows of 4096 from fp32 to bf16: 81 us with eight neighbours per thread).
+template <typename TX, typename TY>
+constexpr int kVector = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
 
-// NV vectors of eight elements per thread: the thread's k-th begins at column (k * TR + thread) * 8.
-template <typename TX, typename TY, int TR, int NV>
-__global__ void __launch_bounds__(threads_of(TR)) norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean,
-                                                                  float *__restrict__ rstd) {
+// Eights: eight elements per thread times this; the thread's k-th vector begins at column (k * TR + thread) * E.
+template <typename TX, typename TY, int TR, int Eights, bool Stream>
+__global__ void __launch_bounds__(threads_of(TR)) norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd) {
+    constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E;
     constexpr int kWaves = threads_of(TR) / kWave;
     __shared__ double scratch[3][kWaves * 2];
     const int t = threadIdx.x % TR;
     const int64_t row = flat_block() * (threads_of(TR) / TR) + threadIdx.x / TR;
     if (row >= a.rows) return;  // (TR > 64: the workgroup's one row)
     const TX *x = static_cast<const TX *>(a.x) + row * a.x_stride;
-    float v[NV][8];
+    float v[NV][E];
+    {
+        RawE<E, TX> r[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int c = (k * TR + t) * 8;
-        Raw8<TX> r;
-        load_some(r, x + c, within(c, a.cols));
-        raw_floats(r, v[k]);
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TR + t) * E;
+            fetch<E, Stream>(r[k], x + c, within_e<E>(c, a.cols));
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) floats(r[k], v[k]);
     }
     const float n = static_cast<float>(a.cols);
     float mu = 0.0f;
@@ -72,7 +103,7 @@ __global__ void __launch_bounds__(threads_of(TR)) norm_fwd_kernel(NormArgs a, TY
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += v[k][i];
+            for (int i = 0; i < E; ++i) s[0] += v[k][i];
         row_sums<TR, 1, float>(s, reinterpret_cast<float *>(scratch[0]));
         mu = s[0] / n;
         if (!(fabsf(s[0]) <= 3e38f)) {  // the sum left fp32's range (or something in the row is not finite)
@@ -80,22 +111,22 @@ __global__ void __launch_bounds__(threads_of(TR)) norm_fwd_kernel(NormArgs a, TY
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[0] += v[k][i];
+                for (int i = 0; i < E; ++i) d[0] += v[k][i];
             row_sums<TR, 1, double>(d, scratch[2]);
             mu = static_cast<float>(d[0] / a.cols);
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int some = within((k * TR + t) * 8, a.cols);
+            const int some = within_e<E>((k * TR + t) * E, a.cols);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] = i < some ? v[k][i] - mu : 0.0f;
+            for (int i = 0; i < E; ++i) v[k][i] = i < some ? v[k][i] - mu : 0.0f;
         }
     }
     float s[2] = {0.0f, 0.0f};  // of what is left, and its squares
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < E; ++i) {
             s[0] += v[k][i];
             s[1] += v[k][i] * v[k][i];
         }
@@ -109,7 +140,7 @@ __global__ void __launch_bounds__(threads_of(TR)) norm_fwd_kernel(NormArgs a, TY
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[0] += static_cast<double>(v[k][i]) * static_cast<double>(v[k][i]);
+            for (int i = 0; i < E; ++i) d[0] += static_cast<double>(v[k][i]) * static_cast<double>(v[k][i]);
         row_sums<TR, 1, double>(d, scratch[2]);
         rs = static_cast<float>(1.0 / sqrt(d[0] / a.cols - static_cast<double>(off) * off + a.eps));
     }
@@ -119,22 +150,22 @@ __global__ void __launch_bounds__(threads_of(TR)) norm_fwd_kernel(NormArgs a, TY
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int c = (k * TR + t) * 8, some = within(c, a.cols);
+        const int c = (k * TR + t) * E, some = within_e<E>(c, a.cols);
         if (some == 0) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = (v[k][i] - off) * rs;
-        float p[8];
+        for (int i = 0; i < E; ++i) v[k][i] = (v[k][i] - off) * rs;
+        float p[E];
         if (a.w) {
-            load_typed(p, a.w, a.w_dtype, c, some);
+            load_weights(p, a.w, a.w_dtype, c, some);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] *= p[i];
+            for (int i = 0; i < E; ++i) v[k][i] *= p[i];
         }
         if (a.b) {
-            load_typed(p, a.b, a.w_dtype, c, some);
+            load_weights(p, a.b, a.w_dtype, c, some);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] += p[i];
+            for (int i = 0; i < E; ++i) v[k][i] += p[i];
         }
-        store_some(y + row * y_stride + c, v[k], some);
+        store_e<Stream>(y + row * y_stride + c, v[k], some);
     }
 }
 
@@ -144,109 +175,130 @@ struct NormGrads {
     int64_t dy_stride;
     void *dx;
     int dx_dtype;
-    float *dw_parts, *db_parts;  // [kParts][cols], or NULL
+    float *dw_parts, *db_parts;  // a row of partial sums per workgroup, or NULL
+    int64_t part_stride;
 };
 
-// Rows g, g + G, ... of the grid's groups of TR threads; a thread keeps its columns' sums of dy h and dy over all its rows, the
-// groups of a workgroup add theirs in order at the end.
-template <typename TX, typename TY, int TR, int NV>
-__global__ void __launch_bounds__(1024) norm_bwd_kernel(NormArgs a, NormGrads g) {
-    constexpr int kGroups = 1024 / TR;
-    __shared__ float scratch[2][3 * 1024 / kWave];
-    extern __shared__ float joined[];  // [2][cols], where a workgroup has several groups
+// A group of TR threads takes every so-manieth row; it asks for the next one before it works on the one that it holds.  A thread
+// keeps its columns' sums of dy h and dy over all of its rows; wavefronts that have rows to themselves add theirs in order at the end.
+constexpr int groups_of(int TR) { return TR == kWave ? 4 : 1; }
+template <typename TX, typename TY, int TR, int Eights, bool Bias, bool Stream>
+__global__ void __launch_bounds__(TR * groups_of(TR)) norm_bwd_kernel(NormArgs a, NormGrads g) {
+    constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E, kGroups = groups_of(TR);
+    __shared__ float scratch[2][3 * TR * kGroups / kWave];
+    extern __shared__ float joined[];  // [kGroups][2][cols], where a workgroup has several groups
     const int t = threadIdx.x % TR, group = threadIdx.x / TR;
-    float w[NV][8], dw[NV][8], db[NV][8];
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+    RawE<E, TX> rx[NV], next_x[NV];
+    RawE<E, TY> ry[NV], next_y[NV];
+    float mu = 0.0f, rs = 0.0f, next_mu = 0.0f, next_rs = 0.0f;
+    const auto get = [&](int64_t at, RawE<E, TX> (&x)[NV], RawE<E, TY> (&y)[NV], float &m, float &r) {
+        if (at >= a.rows) return;
+        const TX *px = static_cast<const TX *>(a.x) + at * a.x_stride;
+        const TY *py = static_cast<const TY *>(g.dy) + at * g.dy_stride;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TR + t) * E, some = within_e<E>(c, a.cols);
+            fetch<E, Stream>(x[k], px + c, some);
+            fetch<E, Stream>(y[k], py + c, some);
+        }
+        if (a.layer) m = g.mean[at];
+        r = g.rstd[at];
+    };
+    get(row, rx, ry, mu, rs);
+    float w[NV][E], dw[NV][E], db[NV][E];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int c = (k * TR + t) * 8;
-        if (a.w) load_typed(w[k], a.w, a.w_dtype, c, within(c, a.cols));
+        const int c = (k * TR + t) * E;
+        if (a.w) load_weights(w[k], a.w, a.w_dtype, c, within_e<E>(c, a.cols));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < E; ++i) {
             if (!a.w) w[k][i] = 1.0f;
             dw[k][i] = db[k][i] = 0.0f;
         }
     }
     const float inv_n = 1.0f / static_cast<float>(a.cols);
     int turn = 0;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kGroups) {
-        const int64_t row = first + group;
-        const bool live = row < a.rows;
-        float h[NV][8], d[NV][8];
-        float rs = 0.0f;
-        float s[3] = {0.0f, 0.0f, 0.0f};  // of h, g, g h
-        if (live) {
-            const float mu = a.layer ? g.mean[row] : 0.0f;
-            rs = g.rstd[row];
-            const TX *x = static_cast<const TX *>(a.x) + row * a.x_stride;
-            const TY *dy = static_cast<const TY *>(g.dy) + row * g.dy_stride;
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int c = (k * TR + t) * 8, some = within(c, a.cols);
-                Raw8<TX> rx;
-                Raw8<TY> ry;
-                load_some(rx, x + c, some);
-                load_some(ry, dy + c, some);
-                raw_floats(rx, h[k]);
-                raw_floats(ry, d[k]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    h[k][i] = i < some ? (h[k][i] - mu) * rs : 0.0f;
-                    const float gi = d[k][i] * w[k][i];
-                    s[0] += h[k][i];
-                    s[1] += gi;
-                    s[2] += gi * h[k][i];
-                }
-            }
-        }
-        row_sums<TR, 3, float>(s, scratch[turn]);
-        turn ^= 1;
-        if (!live) continue;
-        const float off = a.layer ? s[0] * inv_n : 0.0f;
-        const float mean_g = a.layer ? s[1] * inv_n : 0.0f;
-        const float mean_gh = s[2] * inv_n - off * mean_g;
+    for (; row < a.rows; row += stride) {  // (TR > 64: the same rows for all of the workgroup)
+        get(row + stride, next_x, next_y, next_mu, next_rs);
+        float s[3] = {0.0f, 0.0f, 0.0f};  // of g h, g, h
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (k * TR + t) * 8, some = within(c, a.cols);
-            if (some == 0) continue;
-            float dx[8];
+            const int some = within_e<E>((k * TR + t) * E, a.cols);
+            float h[E], d[E];
+            floats(rx[k], h);
+            floats(ry[k], d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float hi = h[k][i] - off;
-                dx[i] = rs * (d[k][i] * w[k][i] - mean_g - hi * mean_gh);
-                dw[k][i] += d[k][i] * hi;
-                db[k][i] += d[k][i];
+            for (int i = 0; i < E; ++i) {
+                const float hi = i < some ? (h[i] - mu) * rs : 0.0f, gi = d[i] * w[k][i];
+                s[0] += gi * hi;
+                s[1] += gi;
+                s[2] += hi;
             }
-            if (g.dx) store_typed(g.dx, g.dx_dtype, row * a.cols + c, dx, some);
         }
+        float off = 0.0f, mean_g = 0.0f, mean_gh;
+        if (a.layer) {
+            row_sums<TR, 3, float>(s, scratch[turn]);
+            off = s[2] * inv_n;
+            mean_g = s[1] * inv_n;
+            mean_gh = s[0] * inv_n - off * mean_g;
+        } else {
+            float one[1] = {s[0]};
+            row_sums<TR, 1, float>(one, scratch[turn]);
+            mean_gh = one[0] * inv_n;
+        }
+        turn ^= 1;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TR + t) * E, some = within_e<E>(c, a.cols);
+            float h[E], d[E], dx[E];
+            floats(rx[k], h);
+            floats(ry[k], d);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float hi = (h[i] - mu) * rs - off;
+                dx[i] = rs * (d[i] * w[k][i] - mean_g - hi * mean_gh);
+                dw[k][i] += d[i] * hi;
+                if (Bias) db[k][i] += d[i];
+            }
+            if (some && g.dx) {
+                const int64_t at = row * a.cols + c;
+                if (g.dx_dtype == SPO_FP32) store_e<Stream && E == 4>(static_cast<float *>(g.dx) + at, dx, some);
+                else store_e<Stream>(static_cast<bf16_t *>(g.dx) + at, dx, some);
+            }
+            rx[k] = next_x[k];
+            ry[k] = next_y[k];
+        }
+        mu = next_mu;
+        rs = next_rs;
     }
     if (!g.dw_parts && !g.db_parts) return;
+    const int64_t part = blockIdx.x * g.part_stride;
     if constexpr (kGroups > 1) {
-        for (int turn_of = 0; turn_of < kGroups; ++turn_of) {
-            if (turn_of == group)
 #pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    const int c = (k * TR + t) * 8, some = within(c, a.cols);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < some) {
-                            float *pw = joined + c + i, *pb = pw + a.cols;
-                            *pw = turn_of ? *pw + dw[k][i] : dw[k][i];
-                            *pb = turn_of ? *pb + db[k][i] : db[k][i];
-                        }
-                }
-            __syncthreads();
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TR + t) * E, some = within_e<E>(c, a.cols);
+            store_e<false>(joined + group * 2 * a.cols + c, dw[k], some);
+            if (Bias) store_e<false>(joined + (group * 2 + 1) * a.cols + c, db[k], some);
         }
-        for (int c = threadIdx.x; c < a.cols; c += 1024) {
-            if (g.dw_parts) g.dw_parts[static_cast<int64_t>(blockIdx.x) * a.cols + c] = joined[c];
-            if (g.db_parts) g.db_parts[static_cast<int64_t>(blockIdx.x) * a.cols + c] = joined[a.cols + c];
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.cols; c += TR * kGroups) {
+            float sw = 0.0f, sb = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                sw += joined[i * 2 * a.cols + c];
+                if (Bias) sb += joined[(i * 2 + 1) * a.cols + c];
+            }
+            if (g.dw_parts) g.dw_parts[part + c] = sw;
+            if (Bias) g.db_parts[part + c] = sb;
         }
     } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (k * TR + t) * 8, some = within(c, a.cols);
-            const int64_t at = static_cast<int64_t>(blockIdx.x) * a.cols + c;
-            if (some && g.dw_parts) store_some(g.dw_parts + at, dw[k], some);
-            if (some && g.db_parts) store_some(g.db_parts + at, db[k], some);
+            const int c = (k * TR + t) * E, some = within_e<E>(c, a.cols);
+            if (some && g.dw_parts) store_e<false>(g.dw_parts + part + c, dw[k], some);
+            if (some && Bias) store_e<false>(g.db_parts + part + c, db[k], some);
         }
     }
 }
@@ -307,35 +359,49 @@ __global__ void __launch_bounds__(256) norm_bwd_cols_kernel(NormArgs a, NormGrad
         }
         if (g.dx) store_typed(g.dx, g.dx_dtype, row * a.cols + c, dx, some);
     }
-    const int64_t at = static_cast<int64_t>(blockIdx.y) * a.cols + c;
+    const int64_t at = static_cast<int64_t>(blockIdx.y) * g.part_stride + c;
     if (g.dw_parts) store_some(g.dw_parts + at, dw, some);
     if (g.db_parts) store_some(g.db_parts + at, db, some);
 }
 
-// Column sums of the partial rows: 64 columns per workgroup, 16 shares of the rows joined in order.
-__global__ void __launch_bounds__(1024) norm_join_kernel(const float *__restrict__ dw_parts, const float *__restrict__ db_parts, int parts,
+// Column sums of the partial rows: 64 columns per workgroup, four to a thread, 64 shares of the rows joined in a fixed order.
+__global__ void __launch_bounds__(1024) norm_join_kernel(const float *__restrict__ dw_parts, const float *__restrict__ db_parts, int64_t part_stride, int parts,
                                                          int cols, void *__restrict__ dw, void *__restrict__ db, int dtype, int add) {
-    __shared__ float sums[16][kWave];
+    __shared__ float sums[1024 / kWave][64];
     const float *of = blockIdx.y ? db_parts : dw_parts;
     void *to = blockIdx.y ? db : dw;
     if (!to) return;
-    const int lane = threadIdx.x % kWave, share = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
-    float s = 0.0f;
-    if (c < cols)
-        for (int p = share; p < parts; p += 16) s += of[static_cast<int64_t>(p) * cols + c];
-    sums[share][lane] = s;
+    const int share = threadIdx.x / 16, four = threadIdx.x % 16 * 4;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = share; p < parts; p += 64) {  // (rows are padded to whole workgroups)
+        const float4 v = *reinterpret_cast<const float4 *>(of + p * part_stride + blockIdx.x * 64 + four);
+        s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s[i] += __shfl_xor(s[i], 16, kWave);
+        s[i] += __shfl_xor(s[i], 32, kWave);
+        if (threadIdx.x % kWave < 16) sums[threadIdx.x / kWave][four + i] = s[i];
+    }
     __syncthreads();
-    if (share || c >= cols) return;
-    for (int i = 1; i < 16; ++i) s += sums[i][lane];
-    if (dtype == SPO_FP32) static_cast<float *>(to)[c] = add ? static_cast<float *>(to)[c] + s : s;
-    else static_cast<bf16_t *>(to)[c] = f32_to_bf16(s);
+    const int c = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || c >= cols) return;
+    float total = 0.0f;
+    for (int i = 0; i < 1024 / kWave; ++i) total += sums[i][threadIdx.x];
+    if (dtype == SPO_FP32) static_cast<float *>(to)[c] = add ? static_cast<float *>(to)[c] + total : total;
+    else static_cast<bf16_t *>(to)[c] = f32_to_bf16(total);
 }
 
 // ------------------------------------------------------------------------------------------------------------ host
 
-template <typename TX, typename TY, int TR, int NV>
+// Arrays that the Infinity Cache does not hold take the non-temporal hint
+template <typename TX, typename TY>
+static bool past_cache(int64_t rows, int64_t cols) { return rows * cols * static_cast<int64_t>(sizeof(TX) + sizeof(TY)) > kStreamBytes; }
+
+template <typename TX, typename TY, int TR, int Eights>
 static void fwd_rows(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
-    norm_fwd_kernel<TX, TY, TR, NV><<<fold_grid(ceil_div(a.rows, threads_of(TR) / TR)), threads_of(TR), 0, s>>>(a, static_cast<TY *>(y), y_stride, mean, rstd);
+    auto *kernel = past_cache<TX, TY>(a.rows, a.cols) ? norm_fwd_kernel<TX, TY, TR, Eights, true> : norm_fwd_kernel<TX, TY, TR, Eights, false>;
+    kernel<<<fold_grid(ceil_div(a.rows, threads_of(TR) / TR)), threads_of(TR), 0, s>>>(a, static_cast<TY *>(y), y_stride, mean, rstd);
 }
 template <typename TX, typename TY>
 static void fwd_typed(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
@@ -350,36 +416,47 @@ static void fwd_typed(const NormArgs &a, void *y, int64_t y_stride, float *mean,
 
 constexpr int kRegisterCols = 16384;  // rows up to here are held by a workgroup of the backward
 
-// Rows that workgroups take at once, and how many workgroups there are
-static int bwd_groups(int64_t cols) { return cols <= 1024 ? 16 : cols <= 4096 ? 4 : 1; }
+// How many workgroups there are.  Two per compute unit of 256 threads: 284780 rows of 4096 in bf16 1160 us, with 384 or 640 of them
+// in all, which leave units idle in the last round, 1310 and 1328, with 1024 (three of which fit a unit) 1499.  Few rows: one each
+// (713 rows of 1001: 7.4 us, two each 8.5, four 11.9).
 static int bwd_parts(int64_t rows, int64_t cols) {
-    return static_cast<int>(std::min<int64_t>(kParts, ceil_div(std::max<int64_t>(rows, 1), bwd_groups(cols))));
+    if (cols > kRegisterCols) return static_cast<int>(std::min<int64_t>(kColumnParts, rows));
+    const int groups = cols <= 1024 ? groups_of(kWave) : 1;
+    return static_cast<int>(std::min<int64_t>(kParts, ceil_div(rows, groups)));
 }
 
-template <typename TX, typename TY, int TR, int NV>
+template <typename TX, typename TY, int TR, int Eights, bool Bias>
 static void bwd_rows(const NormArgs &a, const NormGrads &g, int parts, hipStream_t s) {
-    const size_t lds = TR < 1024 ? 2 * sizeof(float) * a.cols : 0;
-    norm_bwd_kernel<TX, TY, TR, NV><<<parts, 1024, lds, s>>>(a, g);
+    auto *kernel = past_cache<TX, TY>(a.rows, a.cols) ? norm_bwd_kernel<TX, TY, TR, Eights, Bias, true> : norm_bwd_kernel<TX, TY, TR, Eights, Bias, false>;
+    const size_t lds = groups_of(TR) > 1 ? sizeof(float) * 2 * groups_of(TR) * a.cols : 0;
+    kernel<<<parts, TR * groups_of(TR), lds, s>>>(a, g);
+}
+template <typename TX, typename TY, bool Bias>
+static void bwd_typed(const NormArgs &a, const NormGrads &g, int parts, hipStream_t s) {
+    if (a.cols <= 512) bwd_rows<TX, TY, 64, 1, Bias>(a, g, parts, s);
+    else if (a.cols <= 1024) bwd_rows<TX, TY, 64, 2, Bias>(a, g, parts, s);
+    else if (a.cols <= 2048) bwd_rows<TX, TY, 256, 1, Bias>(a, g, parts, s);
+    else if (a.cols <= 4096) bwd_rows<TX, TY, 256, 2, Bias>(a, g, parts, s);
+    else if (a.cols <= 8192) bwd_rows<TX, TY, 512, 2, Bias>(a, g, parts, s);
+    else bwd_rows<TX, TY, 1024, 2, Bias>(a, g, parts, s);
 }
 template <typename TX, typename TY>
 static void bwd_typed(const NormArgs &a, const NormGrads &g, int parts, hipStream_t s) {
-    if (a.cols <= 512) bwd_rows<TX, TY, 64, 1>(a, g, parts, s);
-    else if (a.cols <= 1024) bwd_rows<TX, TY, 64, 2>(a, g, parts, s);
-    else if (a.cols <= 2048) bwd_rows<TX, TY, 256, 1>(a, g, parts, s);
-    else if (a.cols <= 4096) bwd_rows<TX, TY, 256, 2>(a, g, parts, s);
-    else if (a.cols <= 8192) bwd_rows<TX, TY, 1024, 1>(a, g, parts, s);
-    else bwd_rows<TX, TY, 1024, 2>(a, g, parts, s);
+    if (g.db_parts) bwd_typed<TX, TY, true>(a, g, parts, s);
+    else bwd_typed<TX, TY, false>(a, g, parts, s);
 }
 
 struct NormPlan {
     float *dw_parts, *db_parts, *sums;
+    int64_t part_stride;
     size_t bytes;
 };
-// Sizes do not shrink with rows or cols: partial rows for as many workgroups as there can be, up to one per row.
+// The size does not shrink with rows or cols: as many partial rows as any number of columns has with these rows.
 static NormPlan plan_norm(int64_t rows, int64_t cols, void *ws) {
     NormPlan p{};
     Arena a(ws);
-    const size_t room = static_cast<size_t>(std::min<int64_t>(kParts, std::max<int64_t>(rows, 1))) * cols;
+    p.part_stride = ceil_div(cols, 64) * 64;
+    const size_t room = static_cast<size_t>(std::min<int64_t>(kParts, std::max<int64_t>(rows, 1))) * p.part_stride;
     p.dw_parts = a.take<float>(room);
     p.db_parts = a.take<float>(room);
     if (cols > kRegisterCols) p.sums = a.take<float>(static_cast<size_t>(rows) * 3);
@@ -448,23 +525,21 @@ extern "C" int spo_norm_bwd(const spo_norm_desc *d, const float *mean, const flo
     const NormPlan p = plan_norm(d->rows, d->cols, ws);
     if (ws_bytes < p.bytes) return SPO_EWORKSPACE;
     const NormArgs a = args_of(d);
-    const NormGrads g{mean, rstd, dy, dy_stride ? dy_stride : d->cols, dx, dx_dtype, d_weight ? p.dw_parts : nullptr, d_bias ? p.db_parts : nullptr};
+    const NormGrads g{mean, rstd, dy, dy_stride ? dy_stride : d->cols, dx, dx_dtype, d_weight ? p.dw_parts : nullptr, d_bias ? p.db_parts : nullptr, p.part_stride};
     const hipStream_t s = as_stream(stream);
-    int parts = 0;
+    const int parts = bwd_parts(d->rows, d->cols);
     if (d->rows && d->cols <= kRegisterCols) {
-        parts = bwd_parts(d->rows, d->cols);
         const bool x32 = d->x_dtype == SPO_FP32, y32 = dy_dtype == SPO_FP32;
         if (x32 && y32) bwd_typed<float, float>(a, g, parts, s);
         else if (x32) bwd_typed<float, bf16_t>(a, g, parts, s);
         else if (y32) bwd_typed<bf16_t, float>(a, g, parts, s);
         else bwd_typed<bf16_t, bf16_t>(a, g, parts, s);
     } else if (d->rows) {
-        parts = static_cast<int>(std::min<int64_t>(kParts, d->rows));
         norm_bwd_sums_kernel<<<fold_grid(d->rows), 1024, 0, s>>>(a, g, d->x_dtype, dy_dtype, p.sums);
         norm_bwd_cols_kernel<<<dim3(static_cast<unsigned>(ceil_div(d->cols, 2048)), parts), 256, 0, s>>>(a, g, d->x_dtype, dy_dtype, p.sums);
     }
     if (d_weight || d_bias)  // (no rows: sums of nothing)
-        norm_join_kernel<<<dim3(static_cast<unsigned>(ceil_div(d->cols, kWave)), 2), 1024, 0, s>>>(p.dw_parts, p.db_parts, parts, static_cast<int>(d->cols), d_weight,
-                                                                                               d_bias, d_w_dtype, accumulate);
+        norm_join_kernel<<<dim3(static_cast<unsigned>(ceil_div(d->cols, kWave)), 2), 1024, 0, s>>>(p.dw_parts, p.db_parts, p.part_stride, parts, static_cast<int>(d->cols),
+                                                                                               d_weight, d_bias, d_w_dtype, accumulate);
     return launch_status();
 }

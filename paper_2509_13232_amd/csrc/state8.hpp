@@ -42,7 +42,7 @@ SPO_BOTH float bits_float(uint32_t u) {
     return x;
 }
 
-// The threshold of place 0, and of the others from it; the upper bits count.
+// The threshold of a place of the block: the upper bits of `turn` count.
 SPO_BOTH uint32_t turn_of(uint32_t step, uint32_t start) { return step * kPerStep + start; }
 SPO_BOTH uint32_t turn_at(uint32_t turn, uint32_t place) { return turn + place * kPerPlace; }
 
@@ -57,21 +57,28 @@ struct Code8 {
         const uint32_t e = (top + ((1u << kDrop) - 1)) >> 23;
         return e < 15 ? 15 : e > kNotFinite ? kNotFinite : e;
     }
-    SPO_BOTH static uint32_t encode(float x, uint32_t scale, uint32_t turn) {
-        const uint32_t sign = float_bits(x) >> 31;
-        const uint32_t y = float_bits(ldexpf(bits_float(float_bits(x) & 0x7fffffffu), 15 - static_cast<int>(scale)));
-        uint32_t c = (y + (turn >> (32 - kDrop))) >> kDrop;
-        if (kSigned) return (c & 0x7f) | sign << 7;
-        if (c == 0 && x != 0.0f) c = 1;
-        return c & 0xff;
+    SPO_BOTH static uint32_t threshold(uint32_t turn) { return turn >> (32 - kDrop); }
+    // A magnitude and its threshold, shifted so that the code they make is the uppermost byte.
+    SPO_BOTH static uint32_t word(float x, uint32_t scale, uint32_t threshold) {
+        return (float_bits(ldexpf(fabsf(x), 15 - static_cast<int>(scale))) + threshold) << (24 - kDrop);
     }
-    // nan: nan_of(scale), made once for a block
-    SPO_BOTH static float decode(uint32_t code, uint32_t scale, uint32_t nan) {
-        const uint32_t y = kSigned ? (code & 0x7f) << kDrop | (code & 0x80) << 24 : code << kDrop;
-        return ldexpf(bits_float(y | nan), static_cast<int>(scale) - 15);
+    // The code in the uppermost byte, anything below it.  (In a block that is not finite codes may be anything, too.)
+    SPO_BOTH static uint32_t encode(float x, uint32_t scale, uint32_t threshold) {
+        const uint32_t y = word(x, scale, threshold);
+        if (kSigned) return float_bits(copysignf(bits_float(y), x));
+        const uint32_t least = float_bits(x) < 1u << 24 ? float_bits(x) : 1u << 24;  // a root is zero or 2^-75 and more, which is past that
+        return y > least ? y : least;
+    }
+    // What a code stands for, of scale 15: the code shifted to where the type's exponent and mantissa meet, and its sign.
+    SPO_BOTH static float unscaled(uint32_t code) {
+        const float size = bits_float((code & (kSigned ? 0x7f : 0xff)) << kDrop);
+        return kSigned ? copysignf(size, bits_float(code << 24)) : size;
+    }
+    SPO_BOTH static float decode(uint32_t code, uint32_t scale) {
+        if (scale == kNotFinite) return bits_float(0x7fc00000u);
+        return ldexpf(unscaled(code), static_cast<int>(scale) - 15);
     }
 };
-SPO_BOTH uint32_t nan_of(uint32_t scale) { return scale == kNotFinite ? 0x7fc00000u : 0; }
 
 typedef Code8<3> FirstCode;
 typedef Code8<4> RootCode;

@@ -71,15 +71,106 @@ __device__ __forceinline__ void store_some(float *p, const float (&x)[8], int n)
         if (i < n) p[i] = x[i];
 }
 
+// Four elements: of fp32 a wavefront's are then whole lines.
+__device__ __forceinline__ int within4(int64_t at, int64_t n) { return at >= n ? 0 : n - at < 4 ? static_cast<int>(n - at) : 4; }
+template <bool Stream = false>
+__device__ __forceinline__ void load4(float (&x)[4], const float *p, int n) {
+    if (n >= 4) return Vec<float>::unpack(load16<Stream>(p), x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = i < n ? p[i] : 0.0f;
+}
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <bool Stream = false>
+__device__ __forceinline__ void load4(float (&x)[4], const bf16_t *p, int n) {
+    if (n >= 4) {
+        typedef u32x2_t V __attribute__((aligned(2)));
+        const u32x2_t v = Stream ? __builtin_nontemporal_load(reinterpret_cast<const V *>(p)) : *reinterpret_cast<const V *>(p);
+        x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
+        x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = i < n ? bf16_to_f32(p[i]) : 0.0f;
+}
+template <bool Stream = false>
+__device__ __forceinline__ void store4(float *p, const float (&x)[4], int n) {
+    if (n >= 4) return put16<Stream>(p, Vec<float>::pack(x));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) p[i] = x[i];
+}
+template <bool Stream = false>
+__device__ __forceinline__ void store4(bf16_t *p, const float (&x)[4], int n) {
+    const u32x2_t v = {pack_bf16x2_rn(x[0], x[1]), pack_bf16x2_rn(x[2], x[3])};
+    if (n >= 4) {
+        typedef u32x2_t V __attribute__((aligned(2)));
+        if (Stream) __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
+        else *reinterpret_cast<V *>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) p[i] = static_cast<bf16_t>((i < 2 ? v.x : v.y) >> 16 * (i & 1));
+}
+
+// E = 8 elements of bf16 or 4 of any type as they lie in memory, floats from them, and floats into memory.
+template <int E, typename T> struct RawE { uint32_t u[E * sizeof(T) / 4]; };
+template <int E, bool Stream, typename T>
+__device__ __forceinline__ void fetch(RawE<E, T> &r, const T *p, int n) {
+    static_assert(E * sizeof(T) == 16 || E * sizeof(T) == 8, "one load");
+    if (n >= E) {
+        if constexpr (E * sizeof(T) == 16) {
+            const uint4 v = load16<Stream>(p);
+            r.u[0] = v.x, r.u[1] = v.y, r.u[2] = v.z, r.u[3] = v.w;
+        } else {
+            typedef u32x2_t V __attribute__((aligned(2)));
+            const u32x2_t v = Stream ? __builtin_nontemporal_load(reinterpret_cast<const V *>(p)) : *reinterpret_cast<const V *>(p);
+            r.u[0] = v.x, r.u[1] = v.y;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            r.u[i] = i < n ? __float_as_uint(p[i]) : 0u;
+        } else {
+            const uint32_t x = i < n ? static_cast<uint32_t>(p[i]) : 0u;
+            r.u[i / 2] = i & 1 ? r.u[i / 2] | x << 16 : x;
+        }
+    }
+}
+template <int E, typename T>
+__device__ __forceinline__ void floats(const RawE<E, T> &r, float (&x)[E]) {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        x[i] = __uint_as_float(sizeof(T) == 4 ? r.u[i] : i & 1 ? r.u[i / 2] & 0xffff0000u : r.u[i / 2] << 16);
+}
+template <bool Stream, typename T> __device__ __forceinline__ void store_e(T *p, const float (&x)[8], int n) { store_some<Stream>(p, x, n); }
+template <bool Stream, typename T> __device__ __forceinline__ void store_e(T *p, const float (&x)[4], int n) { store4<Stream>(p, x, n); }
+template <int E>
+__device__ __forceinline__ int within_e(int at, int n) { return at >= n ? 0 : n - at < E ? n - at : E; }
+template <int E>
+__device__ __forceinline__ void load_weights(float (&x)[E], const void *p, int dtype, int at, int n) {
+#pragma unroll
+    for (int h = 0; h < E; h += 4) {
+        float y[4];
+        if (dtype == SPO_FP32) load4(y, static_cast<const float *>(p) + at + h, n - h);
+        else load4(y, static_cast<const bf16_t *>(p) + at + h, n - h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[h + i] = y[i];
+    }
+}
+
 // Of a type that the kernel is told at run time (the same for all its threads): arrays that are small beside the others.
+template <bool Stream = false>
 __device__ __forceinline__ void load_typed(float (&x)[8], const void *p, int dtype, int64_t at, int n) {
     if (dtype == SPO_FP32) {
         Raw8<float> r;
-        load_some(r, static_cast<const float *>(p) + at, n);
+        load_some<Stream>(r, static_cast<const float *>(p) + at, n);
         raw_floats(r, x);
     } else {
         Raw8<bf16_t> r;
-        load_some(r, static_cast<const bf16_t *>(p) + at, n);
+        load_some<Stream>(r, static_cast<const bf16_t *>(p) + at, n);
         raw_floats(r, x);
     }
 }
