@@ -13,9 +13,13 @@
 #include <ATen/ops/empty.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
+#include <vector>
 
 #include "spo.h"
 
@@ -353,6 +357,203 @@ PyObject *logprob_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// Of the device whose stream a call goes to.
+bool here(const at::Tensor *t) { return t->device().index() == c10::hip::current_device(); }
+// ... rows of consecutive elements that do not overlap, of a type that the library takes
+const at::Tensor *rows_of(PyObject *o, int64_t rows, int64_t cols, int64_t &apart) {
+    const at::Tensor *t = tensor(o);
+    if (!t || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16)) return nullptr;
+    apart = rows > 1 ? t->stride(0) : cols;
+    return (cols == 1 || t->stride(1) == 1) && apart >= cols && here(t) ? t : nullptr;
+}
+// The descriptor of a normalisation: its address, and its x.  False: not plain.
+bool normalised(PyObject *address, PyObject *of, const spo_norm_desc *&d, const at::Tensor *&x) {
+    if (!PyLong_CheckExact(address)) return false;
+    d = static_cast<const spo_norm_desc *>(PyLong_AsVoidPtr(address));
+    x = tensor(of);
+    return d && x && d->rows > 0 && here(x);
+}
+
+// (descriptor, x) -> (y, mean or None, rstd)
+PyObject *norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const spo_norm_desc *d;
+    const at::Tensor *x;
+    if (n != 2 || !plain_context() || !normalised(a[0], a[1], d, x)) return none();
+    const at::Tensor y = fresh({d->rows, d->cols}, type_of(d->y_dtype), *x), rstd = fresh({d->rows}, at::kFloat, *x);
+    at::Tensor mean;
+    if (d->kind == SPO_NORM_LAYER) mean = fresh({d->rows}, at::kFloat, *x);
+    const spo_stream_t s = stream();
+    const int rc = unlocked([&] { return spo_norm_fwd(d, y.data_ptr(), d->cols, mean.defined() ? ptr<float>(mean) : nullptr, ptr<float>(rstd), s); });
+    return rc ? refused(rc, "spo_norm_fwd") : pack(wrap(y), mean.defined() ? wrap(mean) : none(), wrap(rstd));
+    END_HANDLE_TH_ERRORS
+}
+
+// (descriptor, x, mean or None, rstd, dy, workspace) -> (dx in x's type, d_weight or None, d_bias or None in fp32)
+PyObject *norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const spo_norm_desc *d;
+    const at::Tensor *x;
+    if (n != 6 || !plain_context() || !normalised(a[0], a[1], d, x)) return none();
+    const bool layer = d->kind == SPO_NORM_LAYER;
+    const at::Tensor *mean = a[2] == Py_None ? nullptr : dense(a[2], at::kFloat, d->rows), *rstd = dense(a[3], at::kFloat, d->rows);
+    int64_t apart;
+    const at::Tensor *dy = rows_of(a[4], d->rows, d->cols, apart);
+    if (!rstd || !dy || (!mean && (layer || a[2] != Py_None))) return none();
+    const at::Tensor *ws = workspace(a[5], spo_norm_bwd_workspace_bytes(d));
+    if (!ws) return none();
+    const at::Tensor dx = fresh({d->rows, d->cols}, type_of(d->x_dtype), *x);
+    at::Tensor dw, db;
+    if (d->weight) dw = fresh({d->cols}, at::kFloat, *x);
+    if (d->bias) db = fresh({d->cols}, at::kFloat, *x);
+    auto given = [](const at::Tensor &t) { return t.defined() ? wrap(t) : none(); };
+    auto at_of = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+    const spo_stream_t s = stream();
+    const int rc = unlocked([&] {
+        return spo_norm_bwd(d, ptr<float>(mean), ptr<float>(rstd), dy->data_ptr(), code_of(*dy), apart, dx.data_ptr(), d->x_dtype, at_of(dw), at_of(db),
+                            SPO_FP32, 0, ws->data_ptr(), ws->numel(), s);
+    });
+    return rc ? refused(rc, "spo_norm_bwd") : pack(wrap(dx), given(dw), given(db));
+    END_HANDLE_TH_ERRORS
+}
+
+struct Span {
+    uintptr_t begin, end;
+    bool written;
+};
+// No array that is written shares memory with another one.
+bool disjoint(std::vector<Span> &of) {
+    std::sort(of.begin(), of.end(), [](const Span &a, const Span &b) { return a.begin < b.begin; });
+    uintptr_t reach = 0, reach_written = 0;
+    for (const Span &s : of) {
+        if (s.begin < (s.written ? reach : reach_written)) return false;
+        reach = std::max(reach, s.end);
+        if (s.written) reach_written = std::max(reach_written, s.end);
+    }
+    return true;
+}
+
+// (params, grads, states, weight decays, copies or None, address of the table) -> bits of the state; the lists of equal lengths
+PyObject *adamw_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 6 || !plain_context()) return none();
+    for (int i = 0; i < 4; ++i)
+        if (!PyList_CheckExact(a[i])) return none();
+    const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+    if (!PyList_CheckExact(a[4]) || !PyLong_CheckExact(a[5])) return none();
+    for (int i = 1; i < 5; ++i)
+        if (PyList_GET_SIZE(a[i]) != count) return none();
+    auto *table = static_cast<spo_adamw_tensor *>(PyLong_AsVoidPtr(a[5]));
+    int bits = 32;
+    std::vector<Span> spans;
+    spans.reserve(count * 7);
+    const auto known = [](const at::Tensor *t) { return t && (t->scalar_type() == at::kFloat || t->scalar_type() == at::kBFloat16) && t->is_contiguous() && here(t); };
+    const auto span = [&](const at::Tensor *t, bool written) {
+        if (t && t->numel()) {
+            const auto p = reinterpret_cast<uintptr_t>(t->data_ptr());
+            spans.push_back({p, p + t->numel() * t->element_size(), written});
+        }
+    };
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor *p = tensor(PyList_GET_ITEM(a[0], i)), *g = tensor(PyList_GET_ITEM(a[1], i));
+        PyObject *state = PyList_GET_ITEM(a[2], i), *decay = PyList_GET_ITEM(a[3], i), *copy_of = PyList_GET_ITEM(a[4], i);
+        if (!known(p) || !known(g) || g->numel() != p->numel() || !PyTuple_Check(state) || PyTuple_GET_SIZE(state) != 4 || !PyFloat_CheckExact(decay)) return none();
+        if (i == 0) {
+            const at::Tensor *m = tensor(PyTuple_GET_ITEM(state, 0));
+            bits = m && m->scalar_type() == at::kByte ? 8 : 32;
+        }
+        const int64_t size = p->numel(), blocks = (size + 63) / 64;
+        const at::Tensor *of[4];
+        for (int k = 0; k < 4; ++k) {
+            PyObject *o = PyTuple_GET_ITEM(state, k);
+            of[k] = o == Py_None ? nullptr : dense(o, bits == 8 ? at::kByte : at::kFloat, k < 2 ? size : blocks);
+            if ((of[k] == nullptr) != (k >= 2 && bits == 32) || (k >= 2 && bits == 32 && o != Py_None) || (of[k] && !here(of[k]))) return none();
+        }
+        const at::Tensor *copy = copy_of == Py_None ? nullptr : dense(copy_of, at::kBFloat16, size);
+        if ((copy_of != Py_None && (!copy || !here(copy) || p->scalar_type() != at::kFloat))) return none();
+        spo_adamw_tensor &t = table[i];
+        t.param = p->data_ptr();
+        t.grad = g->data_ptr();
+        t.m = of[0]->data_ptr();
+        t.v = of[1]->data_ptr();
+        t.m_scale = ptr<uint8_t>(of[2]);
+        t.v_scale = ptr<uint8_t>(of[3]);
+        t.copy = copy ? copy->data_ptr() : nullptr;
+        t.n = size;
+        t.weight_decay = PyFloat_AS_DOUBLE(decay);
+        t.param_dtype = code_of(*p);
+        t.grad_dtype = code_of(*g);
+        span(p, true), span(g, false), span(copy, true);
+        for (const at::Tensor *x : of) span(x, true);
+    }
+    return disjoint(spans) ? PyLong_FromLong(bits) : none();
+    END_HANDLE_TH_ERRORS
+}
+
+// The descriptor of a step: its address, and a tensor of its device.  False: not plain.
+bool stepped(PyObject *address, PyObject *of, const spo_adamw_desc *&d, const at::Tensor *&like) {
+    if (!PyLong_CheckExact(address)) return false;
+    d = static_cast<const spo_adamw_desc *>(PyLong_AsVoidPtr(address));
+    like = tensor(of);
+    return d && like && here(like);
+}
+
+// (descriptor, a gradient, workspace) -> norm
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const spo_adamw_desc *d;
+    const at::Tensor *like;
+    if (n != 3 || !plain_context() || !stepped(a[0], a[1], d, like)) return none();
+    const at::Tensor *ws = workspace(a[2], spo_grad_norm_workspace_bytes(d));
+    if (!ws) return none();
+    const at::Tensor norm = fresh({1}, at::kFloat, *like);
+    const spo_stream_t s = stream();
+    const int rc = unlocked([&] { return spo_grad_norm(d, ptr<float>(norm), ws->data_ptr(), ws->numel(), s); });
+    return rc ? refused(rc, "spo_grad_norm") : wrap(norm);
+    END_HANDLE_TH_ERRORS
+}
+
+// (descriptor, a gradient, lr, step, beta1, beta2, eps, norm or None, max_norm, rounding) -> True
+PyObject *adamw_update(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const spo_adamw_desc *d;
+    const at::Tensor *like, *norm = nullptr;
+    if (n != 10 || !plain_context() || !stepped(a[0], a[1], d, like)) return none();
+    double lr, beta1, beta2, eps, most;
+    int64_t step, rounding;
+    if (!number(a[2], lr) || !whole(a[3], INT64_MIN, INT64_MAX, step) || !number(a[4], beta1) || !number(a[5], beta2) || !number(a[6], eps) ||
+        !number(a[8], most) || !whole(a[9], INT32_MIN, INT32_MAX, rounding))
+        return none();
+    if (a[7] != Py_None && !((norm = dense(a[7], at::kFloat, 1)) && here(norm))) return none();
+    const spo_stream_t s = stream();
+    const int rc = unlocked([&] {
+        return spo_adamw_update(d, lr, nullptr, beta1, beta2, eps, step, nullptr, ptr<float>(norm), most, static_cast<int>(rounding), nullptr, 0, s);
+    });
+    if (rc) return refused(rc, "spo_adamw_update");
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// (m, v, m_scale, v_scale, type's code) -> (first moment, root of the second)
+PyObject *adamw_state_values(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 5 || !plain_context()) return none();
+    const at::Tensor *m = dense(a[0], at::kByte, -1);
+    int64_t type;
+    if (!m || !here(m) || !whole(a[4], SPO_FP32, SPO_BF16, type)) return none();
+    const int64_t size = m->numel(), blocks = (size + 63) / 64;
+    const at::Tensor *v = dense(a[1], at::kByte, size), *ms = dense(a[2], at::kByte, blocks), *vs = dense(a[3], at::kByte, blocks);
+    if (!size || !v || !ms || !vs) return none();
+    const at::Tensor first = fresh({size}, type_of(static_cast<int>(type)), *m), root = fresh({size}, type_of(static_cast<int>(type)), *m);
+    const spo_stream_t s = stream();
+    const int rc = unlocked([&] {
+        return spo_adamw_state_values(ptr<uint8_t>(m), ptr<uint8_t>(v), ptr<uint8_t>(ms), ptr<uint8_t>(vs), size, first.data_ptr(), root.data_ptr(),
+                                      static_cast<int>(type), s);
+    });
+    return rc ? refused(rc, "spo_adamw_state_values") : pack(wrap(first), wrap(root));
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject *set_error(PyObject *, PyObject *type) {
     Py_INCREF(type);
     Py_XSETREF(g_error, type);
@@ -361,7 +562,8 @@ PyObject *set_error(PyObject *, PyObject *type) {
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(sample_prompts), FAST(advantages), FAST(advantage_diagnostics), FAST(tracker_update), FAST(pg_loss_fwd),
-                         FAST(pg_loss_bwd), FAST(pg_loss_fwd_bwd), FAST(logprob_fwd), FAST(logprob_bwd), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         FAST(pg_loss_bwd), FAST(pg_loss_fwd_bwd), FAST(logprob_fwd), FAST(logprob_bwd), FAST(norm_fwd), FAST(norm_bwd),
+                         FAST(adamw_table), FAST(grad_norm), FAST(adamw_update), FAST(adamw_state_values), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_spo_calls", "plain calls of the binding", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
