@@ -1,0 +1,211 @@
+// Normalisation of rows, forward (norm.hpp).
+#include "norm.hpp"
+
+namespace spo {
+
+// Those that share a row (L lanes, or with L = 0 the workgroup) hold two rows side by side where their registers suffice: weight and
+// bias are read once for both, and their sums cross the lanes together.
+// Eights: eight elements per thread times this.  The k-th vector of the t-th of TR threads begins at column (k * TR + t) * E.
+template <int Eights>
+constexpr int kRowsHeld = Eights <= 2 ? 2 : 1;
+// Wavefronts per SIMD that the registers have to leave room for: what is held per thread matters less than how much is under way
+// (21845 rows of 12288 in bf16: 271 us with five, 226 with six).
+constexpr int fwd_occupancy(int E, int W, int eights) { return W == 16 || eights == 8 ? 4 : eights == 4 ? (E == 8 ? 6 : 5) : 4; }
+template <typename TX, typename TY, int L, int W, int Eights, bool Stream>
+__global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVector<TX, TY>, W, Eights)) norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd,
+                                                                             int64_t apart) {
+    constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E, kRows = L ? kThreads / (L ? L : 1) : 1, R = kRowsHeld<Eights>;
+    __shared__ float scratch[2][L ? 1 : 2 * R * W];
+    __shared__ double wide[L ? 1 : 2 * R * W];
+    constexpr int TR = L ? L : W * kWave;
+    const int t = L ? static_cast<int>(threadIdx.x) % L : static_cast<int>(threadIdx.x);
+    const int64_t first = flat_block() * kRows + (L ? threadIdx.x / (L ? L : 1) : 0);
+    if (L == 0 && first >= a.rows) return;
+    const auto row_of = [&](int r) { return first + r * apart; };
+    const auto some_of = [&](int r, int k) { return row_of(r) < a.rows ? within_e<E>((k * TR + t) * E, a.cols) : 0; };
+    const auto past_of = [&](int r) { return row_of(r) < a.rows - 1 && a.cols >= E; };  // (the next row's elements may be read)
+    const auto x_of = [&](int r) { return static_cast<const TX *>(a.x) + row_of(r) * a.x_stride; };
+    float v[R][NV][E], base[R];
+    // x - base
+    const auto differences = [&](int r, const RawE<E, TX> (&raw)[NV]) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int some = some_of(r, k);
+            floats(raw[k], v[r][k]);
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[r][k][i] -= base[r];
+            if (some < E)
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[r][k][i] = i < some ? v[r][k][i] : 0.0f;
+        }
+    };
+    {
+        RawE<E, TX> raw[R][NV], head[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) fetch<E, Stream>(raw[r][k], x_of(r) + (k * TR + t) * E, some_of(r, k), past_of(r));
+            if (a.layer) fetch<E, false>(head[r], x_of(r), row_of(r) < a.rows ? within_e<E>(0, a.cols) : 0, past_of(r));
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            base[r] = 0.0f;
+            if (a.layer) {
+                const int some = row_of(r) < a.rows ? within_e<E>(0, a.cols) : 0;
+                const float share = some == E ? 1.0f / E : 1.0f / static_cast<float>(max(some, 1));
+                float f[E];
+                floats_some(head[r], f, some);
+#pragma unroll
+                for (int i = 0; i < E; ++i) base[r] += f[i] * share;
+            }
+            differences(r, raw[r]);
+        }
+    }
+    const float n = static_cast<float>(a.cols);
+    float off[R], var[R], squares[R], rs[R];
+    const auto sum_up = [&](float *where) {
+        float s[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            s[2 * r] = s[2 * r + 1] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    s[2 * r] += v[r][k][i];
+                    s[2 * r + 1] += v[r][k][i] * v[r][k][i];
+                }
+        }
+        row_sums<L, W, 2 * R, float>(s, where);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            off[r] = a.layer ? s[2 * r] / n : 0.0f;
+            squares[r] = s[2 * r + 1];
+            var[r] = squares[r] / n - off[r] * off[r];
+            var[r] = var[r] < 0.0f ? 0.0f : var[r];
+        }
+    };
+    sum_up(scratch[0]);
+    bool far = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) far |= off[r] * off[r] > 4.0f * var[r];
+    if (any_row<L>(far)) {  // such rows about their mean; the others of the wavefront get what they had
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (off[r] * off[r] > 4.0f * var[r]) base[r] += off[r];
+            RawE<E, TX> raw[NV];
+#pragma unroll
+            for (int k = 0; k < NV; ++k) fetch<E, false>(raw[k], x_of(r) + (k * TR + t) * E, some_of(r, k), past_of(r));
+            differences(r, raw);
+        }
+        sum_up(scratch[1]);
+    }
+    bool odd = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        rs[r] = 1.0f / sqrtf(var[r] + a.eps);
+        odd |= !(squares[r] <= kSquaresHigh && var[r] + a.eps >= kSquaresLow);
+    }
+    if (any_row<L>(odd)) {  // squares, or their sum, that left fp32's range
+        double d[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            d[2 * r] = d[2 * r + 1] = 0.0;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    d[2 * r] += static_cast<double>(v[r][k][i]);
+                    d[2 * r + 1] += static_cast<double>(v[r][k][i]) * static_cast<double>(v[r][k][i]);
+                }
+        }
+        row_sums<L, W, 2 * R, double>(d, wide);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (!(squares[r] <= kSquaresHigh && var[r] + a.eps >= kSquaresLow)) {
+                const double o = a.layer ? d[2 * r] / a.cols : 0.0;
+                off[r] = static_cast<float>(o);
+                rs[r] = static_cast<float>(1.0 / sqrt(d[2 * r + 1] / a.cols - o * o + a.eps));
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (t == 0 && row_of(r) < a.rows) {
+            if (mean && a.layer) mean[row_of(r)] = base[r] + off[r];
+            if (rstd) rstd[row_of(r)] = rs[r];
+        }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * TR + t) * E, inside = within_e<E>(c, a.cols);
+        float w[E], b[E];
+        if (a.w) load_weights(w, a.w, a.w_dtype, c, inside);
+        if (a.b) load_weights(b, a.b, a.w_dtype, c, inside);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int some = some_of(r, k);
+            if (some == 0) continue;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                v[r][k][i] = (v[r][k][i] - off[r]) * rs[r];
+                if (a.w) v[r][k][i] *= w[i];
+                if (a.b) v[r][k][i] += b[i];
+            }
+            store_e<Stream>(y + row_of(r) * y_stride + c, v[r][k], some);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------ host
+
+template <typename TX, typename TY, int L, int W, int Eights>
+static void fwd_rows(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
+    auto *kernel = past_cache<TX, TY>(a.rows, a.cols) ? norm_fwd_kernel<TX, TY, L, W, Eights, true> : norm_fwd_kernel<TX, TY, L, W, Eights, false>;
+    // two rows each once there are workgroups enough
+    constexpr int kRows = L ? kThreads / (L ? L : 1) : 1;
+    const int64_t sets = ceil_div(a.rows, kRows);
+    const dim3 grid = fold_grid(sets > kFwdBlocks ? ceil_div(sets, kRowsHeld<Eights>) : sets);
+    kernel<<<grid, L ? kThreads : W * kWave, 0, s>>>(a, static_cast<TY *>(y), y_stride, mean, rstd, static_cast<int64_t>(grid.x) * grid.y * kRows);
+}
+template <typename TX, typename TY>
+static void fwd_typed(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
+    const int64_t eights = ceil_div(a.cols, 8);
+    if (eights <= kWave)
+        switch (lanes_of(eights)) {
+            case 4: return fwd_rows<TX, TY, 4, 0, 1>(a, y, y_stride, mean, rstd, s);
+            case 8: return fwd_rows<TX, TY, 8, 0, 1>(a, y, y_stride, mean, rstd, s);
+            case 16: return fwd_rows<TX, TY, 16, 0, 1>(a, y, y_stride, mean, rstd, s);
+            case 32: return fwd_rows<TX, TY, 32, 0, 1>(a, y, y_stride, mean, rstd, s);
+            default: return fwd_rows<TX, TY, kWave, 0, 1>(a, y, y_stride, mean, rstd, s);
+        }
+    if (eights <= 2 * kWave) return fwd_rows<TX, TY, kWave, 0, 2>(a, y, y_stride, mean, rstd, s);
+    if (eights <= kLaneEights) return fwd_rows<TX, TY, kWave, 0, 3>(a, y, y_stride, mean, rstd, s);
+    if (eights <= 256) return fwd_rows<TX, TY, 0, 4, 1>(a, y, y_stride, mean, rstd, s);
+    if (eights <= 512) return fwd_rows<TX, TY, 0, 4, 2>(a, y, y_stride, mean, rstd, s);
+    if (eights <= 1024) return fwd_rows<TX, TY, 0, 4, 4>(a, y, y_stride, mean, rstd, s);
+    if (eights <= 2048) return fwd_rows<TX, TY, 0, 8, 4>(a, y, y_stride, mean, rstd, s);
+    if (eights <= 3072) return fwd_rows<TX, TY, 0, 12, 4>(a, y, y_stride, mean, rstd, s);
+    if (eights <= 4096) return fwd_rows<TX, TY, 0, 16, 4>(a, y, y_stride, mean, rstd, s);
+    fwd_rows<TX, TY, 0, 16, 8>(a, y, y_stride, mean, rstd, s);
+}
+
+}  // namespace spo
+
+using namespace spo;
+
+extern "C" int spo_norm_fwd(const spo_norm_desc *d, void *y, int64_t y_stride, float *mean, float *rstd, spo_stream_t stream) {
+    if (int rc = validate(d)) return rc;
+    if (y_stride && y_stride < d->cols) return SPO_EINVAL;
+    if (y_stride > int64_t(1) << 40) return SPO_ERANGE;
+    if (d->rows == 0) return SPO_OK;
+    if (!d->x || !y) return SPO_ENULL;
+    if (!aligned_to(y, d->y_dtype)) return SPO_EINVAL;
+    const NormArgs a = args_of(d);
+    const int64_t ys = y_stride ? y_stride : d->cols;
+    const hipStream_t s = as_stream(stream);
+    const bool x32 = d->x_dtype == SPO_FP32, y32 = d->y_dtype == SPO_FP32;
+    if (x32 && y32) fwd_typed<float, float>(a, y, ys, mean, rstd, s);
+    else if (x32) fwd_typed<float, bf16_t>(a, y, ys, mean, rstd, s);
+    else if (y32) fwd_typed<bf16_t, float>(a, y, ys, mean, rstd, s);
+    else fwd_typed<bf16_t, bf16_t>(a, y, ys, mean, rstd, s);
+    return launch_status();
+}
