@@ -3,18 +3,17 @@
 
 namespace spo {
 
-// Those that share a row (L lanes, or with L = 0 the workgroup) hold two rows side by side where their registers suffice: weight and
-// bias are read once for both, and their sums cross the lanes together.
+// Those that share a row (L lanes, or with L = 0 the workgroup) hold R rows: two side by side where their registers suffice and rows
+// are many; weight and bias are read once for both, and their sums cross the lanes together (65536 rows of 4096 in bf16: 206 -> 195 us;
+// 8192 rows of 1024, which are there at once: 11.4 -> 13.5).
 // Eights: eight elements per thread times this.  The k-th vector of the t-th of TR threads begins at column (k * TR + t) * E.
-template <int Eights>
-constexpr int kRowsHeld = Eights <= 2 ? 2 : 1;
 // Wavefronts per SIMD that the registers have to leave room for: what is held per thread matters less than how much is under way
 // (21845 rows of 12288 in bf16: 271 us with five, 226 with six).
 constexpr int fwd_occupancy(int E, int W, int eights) { return W == 16 || eights == 8 ? 4 : eights == 4 ? (E == 8 ? 6 : 5) : 4; }
-template <typename TX, typename TY, int L, int W, int Eights, bool Stream>
+template <typename TX, typename TY, int L, int W, int Eights, int R, bool Stream>
 __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVector<TX, TY>, W, Eights)) norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd,
                                                                              int64_t apart) {
-    constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E, kRows = L ? kThreads / (L ? L : 1) : 1, R = kRowsHeld<Eights>;
+    constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E, kRows = L ? kThreads / (L ? L : 1) : 1;
     __shared__ float scratch[2][L ? 1 : 2 * R * W];
     __shared__ double wide[L ? 1 : 2 * R * W];
     constexpr int TR = L ? L : W * kWave;
@@ -157,14 +156,19 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
 
 // ------------------------------------------------------------------------------------------------------------ host
 
+template <typename TX, typename TY, int L, int W, int Eights, int R, bool Stream>
+static void fwd_launch(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
+    constexpr int kRows = L ? kThreads / (L ? L : 1) : 1;
+    const dim3 grid = fold_grid(ceil_div(ceil_div(a.rows, kRows), R));
+    norm_fwd_kernel<TX, TY, L, W, Eights, R, Stream><<<grid, L ? kThreads : W * kWave, 0, s>>>(a, static_cast<TY *>(y), y_stride, mean, rstd,
+                                                                                          static_cast<int64_t>(grid.x) * grid.y * kRows);
+}
 template <typename TX, typename TY, int L, int W, int Eights>
 static void fwd_rows(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
-    auto *kernel = past_cache<TX, TY>(a.rows, a.cols) ? norm_fwd_kernel<TX, TY, L, W, Eights, true> : norm_fwd_kernel<TX, TY, L, W, Eights, false>;
-    // two rows each once there are workgroups enough
-    constexpr int kRows = L ? kThreads / (L ? L : 1) : 1;
-    const int64_t sets = ceil_div(a.rows, kRows);
-    const dim3 grid = fold_grid(sets > kFwdBlocks ? ceil_div(sets, kRowsHeld<Eights>) : sets);
-    kernel<<<grid, L ? kThreads : W * kWave, 0, s>>>(a, static_cast<TY *>(y), y_stride, mean, rstd, static_cast<int64_t>(grid.x) * grid.y * kRows);
+    constexpr int R = Eights <= 2 ? 2 : 1;
+    if (R == 2 && a.rows <= kFwdBlocks * (L ? kThreads / (L ? L : 1) : 1)) return fwd_launch<TX, TY, L, W, Eights, 1, false>(a, y, y_stride, mean, rstd, s);
+    if (past_cache<TX, TY>(a.rows, a.cols)) fwd_launch<TX, TY, L, W, Eights, R, true>(a, y, y_stride, mean, rstd, s);
+    else fwd_launch<TX, TY, L, W, Eights, R, false>(a, y, y_stride, mean, rstd, s);
 }
 template <typename TX, typename TY>
 static void fwd_typed(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
