@@ -514,7 +514,7 @@ typedef struct {
     void *m, *v;                 /* [n] fp32 or uint8                                         */
     uint8_t *m_scale, *v_scale;  /* state_bits = 8                                            */
     void *copy;                  /* [n] bf16 or NULL; needs param_dtype = SPO_FP32            */
-    int64_t n;                   /* elements, 0 <= n <= 2^36; 0: nothing else is looked at    */
+    int64_t n;                   /* elements, 0 <= n <= 2^35; 0: nothing else is looked at    */
     double weight_decay;         /* >= 0                                                      */
     int32_t param_dtype, grad_dtype;
 } spo_adamw_tensor;

@@ -15,7 +15,7 @@
 namespace spo {
 
 constexpr int kThreads = 256;
-constexpr int64_t kMostElements = int64_t(1) << 36;
+constexpr int64_t kMostElements = int64_t(1) << 35;
 constexpr size_t kTableBytes = 3840;  // of a launch's 4 KiB of arguments
 
 struct Tensor32 {
@@ -48,6 +48,7 @@ struct TensorNorm {
 template <typename T>
 struct Table {
     static constexpr int kMost = kTableBytes / sizeof(T);
+    static_assert(kMost * (kMostElements / T::kChunk) < INT32_MAX, "chunks of a launch");
     T t[kMost];
     int32_t count, chunks;
     // the tensor of a chunk
@@ -360,7 +361,7 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(Table<TensorNorm> t
     for (int chunk = blockIdx.x; chunk < table.chunks; chunk += gridDim.x) {
         const TensorNorm t = table.t[table.find(chunk)];
         const int64_t begin = static_cast<int64_t>(chunk - t.first) * TensorNorm::kChunk;
-if (t.types & 2) {
+        if (t.types & 2) {
             constexpr int kEights = TensorNorm::kChunk / kThreads / 8;
             Raw8<bf16_t> r[kEights];
 #pragma unroll
@@ -450,7 +451,7 @@ static int in_tables(const spo_adamw_desc *d, F launch) {
         e.n = t.n;
         e.first = table.chunks;
         e.types = (t.param_dtype == SPO_BF16 ? 1 : 0) | (t.grad_dtype == SPO_BF16 ? 2 : 0);
-        table.chunks += static_cast<int32_t>(ceil_div(t.n, T::kChunk));  // (below 2^31 for as many tensors as there can be)
+        table.chunks += static_cast<int32_t>(ceil_div(t.n, T::kChunk));
         if (table.count == Table<T>::kMost) {
             if (int rc = launch(table)) return rc;
             table.count = table.chunks = 0;
@@ -461,10 +462,12 @@ static int in_tables(const spo_adamw_desc *d, F launch) {
 
 // Steps over more than the Infinity Cache holds take the non-temporal hint: in 32 bits for the moments (151936 x 1024 in bf16:
 // 597 -> 551 us), in 8 bits for what is no code (151936 x 4096 in bf16: 1189 -> 1115 us).
-static bool past_cache(const spo_adamw_desc *d) {
+static bool past_cache(const spo_adamw_desc *d, int64_t elements) { return elements > kStreamBytes / (d->state_bits == 32 ? 8 : 6); }
+
+static int64_t elements_of(const spo_adamw_desc *d) {
     int64_t n = 0;
     for (int64_t i = 0; i < d->count; ++i) n += d->tensors[i].n;
-    return n * (d->state_bits == 32 ? 8 : 6) > kStreamBytes;
+    return n;
 }
 
 static int64_t norm_launches(const spo_adamw_desc *d) { return std::max<int64_t>(1, ceil_div(d->count, Table<TensorNorm>::kMost)); }
@@ -544,6 +547,8 @@ extern "C" int spo_adamw_update(const spo_adamw_desc *d, double lr, const float 
         if (!ws || ws_bytes < spo_adamw_update_workspace_bytes()) return SPO_EWORKSPACE;
         if (reinterpret_cast<uintptr_t>(ws) % 256) return SPO_EINVAL;
     }
+    const int64_t elements = elements_of(d);
+    if (elements == 0 && !step_device) return SPO_OK;
     const hipStream_t s = as_stream(stream);
     AdamwScalars a{};
     a.b1 = static_cast<float>(beta1);
@@ -567,7 +572,7 @@ extern "C" int spo_adamw_update(const spo_adamw_desc *d, double lr, const float 
             return SPO_OK;
         };
     };
-    const bool past = past_cache(d);
+    const bool past = past_cache(d, elements);
     const int rc = d->state_bits == 32 ? (past ? in_tables<Tensor32>(d, launch(adamw_kernel<Tensor32, true>)) : in_tables<Tensor32>(d, launch(adamw_kernel<Tensor32, false>)))
                                        : (past ? in_tables<Tensor8>(d, launch(adamw_kernel<Tensor8, true>)) : in_tables<Tensor8>(d, launch(adamw_kernel<Tensor8, false>)));
     return rc ? rc : launch_status();

@@ -62,9 +62,10 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return static_cast<uint32_t>(f32_to_bf16(lo)) | (static_cast<uint32_t>(f32_to_bf16(hi)) << 16);
 }
 
-// 1-D grids may be longer than a launch's 2^32 threads per dimension: they are folded into two
-static inline dim3 fold_grid(int64_t blocks) {
-    constexpr int64_t kRow = int64_t(1) << 22;
+// 1-D grids may be longer than a launch's 2^32 threads per dimension: they are folded into two, of rows of 2^30
+// threads
+static inline dim3 fold_grid(int64_t blocks, int threads = 256) {
+    const int64_t kRow = (int64_t(1) << 30) / threads;
     return blocks <= kRow ? dim3(static_cast<unsigned>(blocks)) : dim3(static_cast<unsigned>(kRow), static_cast<unsigned>(ceil_div(blocks, kRow)));
 }
 __device__ __forceinline__ int64_t flat_block() { return static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x; }

@@ -384,7 +384,7 @@ extern "C" int spo_norm_bwd(const spo_norm_desc *d, const float *mean, const flo
         else rc = bwd_typed<bf16_t, bf16_t>(a, g, parts, s);
         if (rc) return rc;
     } else if (d->rows) {
-        norm_bwd_sums_kernel<<<fold_grid(d->rows), 1024, 0, s>>>(a, g, d->x_dtype, dy_dtype, p.sums);
+        norm_bwd_sums_kernel<<<fold_grid(d->rows, 1024), 1024, 0, s>>>(a, g, d->x_dtype, dy_dtype, p.sums);
         norm_bwd_cols_kernel<<<dim3(static_cast<unsigned>(ceil_div(d->cols, 2048)), parts), 256, 0, s>>>(a, g, d->x_dtype, dy_dtype, p.sums);
     }
     if (d_weight || d_bias)  // (no rows: sums of nothing)

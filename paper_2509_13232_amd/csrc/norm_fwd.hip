@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
 template <typename TX, typename TY, int L, int W, int Eights, int R, bool Stream>
 static void fwd_launch(const NormArgs &a, void *y, int64_t y_stride, float *mean, float *rstd, hipStream_t s) {
     constexpr int kRows = L ? kThreads / (L ? L : 1) : 1;
-    const dim3 grid = fold_grid(ceil_div(ceil_div(a.rows, kRows), R));
+    const dim3 grid = fold_grid(ceil_div(ceil_div(a.rows, kRows), R), L ? kThreads : W * kWave);
     norm_fwd_kernel<TX, TY, L, W, Eights, R, Stream><<<grid, L ? kThreads : W * kWave, 0, s>>>(a, static_cast<TY *>(y), y_stride, mean, rstd,
                                                                                           static_cast<int64_t>(grid.x) * grid.y * kRows);
 }
@@ -187,7 +187,7 @@ static void fwd_typed(const NormArgs &a, void *y, int64_t y_stride, float *mean,
     if (eights <= 512) return fwd_rows<TX, TY, 0, 4, 2>(a, y, y_stride, mean, rstd, s);
     if (eights <= 1024) return fwd_rows<TX, TY, 0, 4, 4>(a, y, y_stride, mean, rstd, s);
     if (eights <= 2048) return fwd_rows<TX, TY, 0, 8, 4>(a, y, y_stride, mean, rstd, s);
-    if (eights <= 3072) return fwd_rows<TX, TY, 0, 12, 4>(a, y, y_stride, mean, rstd, s);
+    if (eights <= 12 * 4 * kWave) return fwd_rows<TX, TY, 0, 12, 4>(a, y, y_stride, mean, rstd, s);
     if (eights <= 4096) return fwd_rows<TX, TY, 0, 16, 4>(a, y, y_stride, mean, rstd, s);
     fwd_rows<TX, TY, 0, 16, 8>(a, y, y_stride, mean, rstd, s);
 }

@@ -63,7 +63,7 @@ def encode(x, mantissa, step):
     code = torch.where(y < 1, y * 2 ** mantissa, power_y.double() * 2 ** mantissa + (part * 2 - 1) * 2 ** mantissa)
     code = code.to(torch.int64)
     if mantissa == 3:
-        code = code | ((blocks(x) < 0).to(torch.int64) << 7)
+        code = code | (torch.signbit(blocks(x)).to(torch.int64) << 7)
     n = x.numel()
     scale = torch.where(ok, power + 127, torch.full_like(power, 255))[:, 0]
     return code.view(-1)[:n].to(torch.uint8), scale.to(torch.uint8)
