@@ -7,6 +7,7 @@ fallback: a missing library or a non-zero status raises.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from collections import namedtuple
 
@@ -952,11 +953,14 @@ def spo_adamw_update(desc, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_norm
     _want(lr_t, torch.float32, "lr", 1)
     _want(step_t, torch.int64, "step", 1)
     _want(grad_norm, torch.float32, "grad_norm", 1)
+    number = 0 if step_t is not None else operator.index(step)
+    if not -1 << 63 <= number < 1 << 63:
+        raise ValueError(f"step: {number} is beyond 64 bits")
     ws, dev = workspace, _step_device(desc)
     if lr_t is not None or step_t is not None:
         ws = _workspace(lib().spo_adamw_update_workspace_bytes(), dev, workspace)
     _check(lib().spo_adamw_update(C.byref(desc[0]), 0.0 if lr_t is not None else float(lr), _ptr(lr_t), float(beta1), float(beta2), float(eps),
-                                  0 if step_t is not None else int(step), _ptr(step_t), _ptr(grad_norm), float(max_norm), int(rounding), _ptr(ws),
+                                  number, _ptr(step_t), _ptr(grad_norm), float(max_norm), int(rounding), _ptr(ws),
                                   0 if ws is None else ws.numel(), _stream()), "spo_adamw_update")
 
 

@@ -77,7 +77,7 @@ class Case:
                 v64 = self.v[i].double()
                 new_state = m, v
             else:
-                (mc, ms), (vc, vs) = tc.encode(m, 3, step), tc.encode(torch.sqrt(v), 4, step)
+                (mc, ms), (vc, vs) = tc.encode(m, 3, step), tc.encode(tc.root(v), 4, step)
                 for got, want, name in ((s.m, mc, "m"), (s.m_scale, ms, "m_scale"), (s.v, vc, "v"), (s.v_scale, vs, "v_scale")):
                     bad = (got.cpu() != want).nonzero()
                     assert not bad.numel(), (i, n, name, len(bad), bad[:4].tolist())
@@ -327,6 +327,27 @@ def test_every_step_reaches_codes_as_defined(spo):
     for step in (1, 2, 3, 4, 5, 1000, 12345678, (1 << 32) + 7, (1 << 40) + 3):
         c.update(step, lr=0.0)
         c.check(step, lr=0.0)
+
+
+@pytest.mark.parametrize("scale", [1.0, 1e-19, 1e-22])
+def test_codes_of_many_elements(spo, scale):
+    # enough roots that hundreds lie beside a code's border, and squares down to where fp32 has no more of them
+    say(f"8-bit codes of many elements, {scale}")
+    n = 6 << 20
+    g = torch.Generator().manual_seed(11)
+    grad = torch.randn(n, generator=g) * torch.exp(2 * torch.randn(n, generator=g)) * scale
+    p = torch.zeros(n, device="cuda")
+    state = spo.adamw_state(p, 8)
+    desc = spo.make_adamw_desc([p], [grad.cuda()], [state])
+    m, v = torch.zeros(n), torch.zeros(n)
+    for step in (1, 2, 3):
+        spo.spo_adamw_update(desc, 1e-3, step, beta1=B1, beta2=B2, eps=EPS)
+        torch.cuda.synchronize()
+        m, v = tc.moments(grad, m, v, B1, B2, root=True)
+        (mc, ms), (vc, vs) = tc.encode(m, 3, step), tc.encode(tc.root(v), 4, step)
+        assert torch.equal(state.m_scale.cpu(), ms) and torch.equal(state.v_scale.cpu(), vs), step
+        assert torch.equal(state.m.cpu(), mc) and torch.equal(state.v.cpu(), vc), step
+        m, v = tc.decode(mc, ms, 3), tc.decode(vc, vs, 4)
 
 
 def test_small_changes_add_up_over_steps(spo):

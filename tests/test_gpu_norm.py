@@ -219,6 +219,64 @@ def test_in_place(spo, T, N):
     assert spo.spo_norm_fwd(dz, out=z)[0] is z and torch.equal(z, y)
 
 
+# rows enough that a group of threads takes two of them side by side, with a last one that is alone; widths of every such group
+MANY = [(131080, 32), (131073, 17), (65601, 64), (32801, 128), (32769, 100), (16401, 256), (8201, 512), (8197, 511), (8199, 1000), (2055, 2000), (2051, 4000),
+        (2053, 3999)]
+
+
+@pytest.mark.parametrize("layer", [True, False], ids=["layer", "rms"])
+@pytest.mark.parametrize("T,N", MANY)
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+def test_many_rows(spo, T, N, dtype, layer):
+    say(f"norm of many rows {T} x {N} {dtype} layer={layer}")
+    x, dy = rows(T, N, dtype), rows(T, N, dtype, seed=1, mean=0.05)
+    check(spo, x, vector(N, dtype, 2, 1.0), vector(N, dtype, 3), dy, layer, dtype)
+
+
+@pytest.mark.parametrize("layer", [True, False], ids=["layer", "rms"])
+@pytest.mark.parametrize("T,N", [(131073, 32), (32, 64), (8199, 1000), (50, 1400), (2051, 2000), (2053, 4000), (40, 6000), (30, 8192), (20, 12288), (11, 20000)])
+def test_rows_of_all_kinds_side_by_side(spo, T, N, layer):
+    # ordinary rows beside rows that begin with an outlier, that lie far from zero, and whose squares leave fp32
+    say(f"norm of rows of all kinds {T} x {N} layer={layer}")
+    x, dy = rows(T, N, F32), rows(T, N, F32, seed=1)
+    x[1::5, 0] = 1e4
+    x[2::5, 0] *= 1e-3
+    x[3::5] *= 1e25
+    x[4::5] += 1e3
+    dy[3::5] *= 1e-3
+    check(spo, x, vector(N, F32, 2, 1.0), vector(N, F32, 3), dy, layer, F32)
+    y, dx, _, _ = check(spo, x, None, None, dy, layer, F32)
+    # a row's result is its own: alone, and in any order
+    order = torch.randperm(T, generator=torch.Generator().manual_seed(4)).cuda()
+    kind = spo.SPO_NORM_LAYER if layer else spo.SPO_NORM_RMS
+    d = spo.make_norm_desc(x[order], kind=kind)
+    other, mean, rstd = spo.spo_norm_fwd(d)
+    d_other, _, _ = spo.spo_norm_bwd(d, mean, rstd, dy[order])
+    assert torch.equal(other, y[order]) and torch.equal(d_other, dx[order])
+
+
+@pytest.mark.parametrize("N", [1100, 1280, 1536, 1537, 2560, 5120, 6000, 8192, 10240, 12288, 24577, 33000])
+def test_widths(spo, N):
+    say(f"norm widths {N}")
+    for dtype in (F32, BF16):
+        x, dy = rows(25, N, dtype), rows(25, N, dtype, seed=1)
+        check(spo, x, vector(N, dtype, 2, 1.0), vector(N, dtype, 3), dy, True, dtype)
+
+
+@pytest.mark.parametrize("T,N", [(131073, 20), (8199, 700), (2051, 3000)])
+def test_many_rows_in_place_and_into_others(spo, T, N):
+    say(f"norm of many rows in place {T} x {N}")
+    x, w = rows(T, N, BF16), vector(N, BF16, 2, 1.0)
+    d = spo.make_norm_desc(x, w, None)
+    y, mean, rstd = spo.spo_norm_fwd(d)
+    out = torch.full((T + 2, N + 3), 7.0, device="cuda", dtype=BF16)
+    got, _, _ = spo.spo_norm_fwd(d, out=out[1:-1, 2:-1])
+    assert torch.equal(got, y) and bool((out[0] == 7).all()) and bool((out[-1] == 7).all())
+    assert bool((out[:, :2] == 7).all()) and bool((out[:, -1] == 7).all())
+    z = x.clone()
+    assert torch.equal(spo.spo_norm_fwd(spo.make_norm_desc(z, w, None), out=z)[0], y)
+
+
 def test_gradient_against_differences(spo):
     # central differences of sum(dy y) along random directions, in fp32 calls: y is off by 1e-5, a step of 2^-6 of the row's size,
     # third derivatives of order one: (2e-5 / 2^-5 + 2^-12) of the directions' norms

@@ -41,6 +41,11 @@ def turns(step, start):
     return ((step % (1 << 32)) * 0x9E3779B9 + start + place * 0xC13FA9A9) % (1 << 32)
 
 
+def root(v):
+    """The rounded root of fp32 numbers: rounded once from 64 bits, since torch's own on the CPU is off by a place for one number in six."""
+    return v.double().sqrt().float()
+
+
 def encode(x, mantissa, step):
     """x fp32 [n]: (codes, scales), by the places of values between codes; mantissa 3: with a sign, 4: a root."""
     size = blocks(x).double().abs()
