@@ -487,7 +487,8 @@ int spo_norm_fwd(const spo_norm_desc *d, void *y, int64_t y_stride, float *mean,
 /* Backward.  mean (SPO_NORM_LAYER), rstd from the forward of the same desc; dy in dy_dtype, rows dy_stride apart (0: cols).
  * dx [rows][cols] contiguous in dx_dtype, d_weight, d_bias [cols] in d_w_dtype: each may be NULL; dx may be dy, or x, if
  * that is contiguous and of its type.  accumulate = 1: d_weight and d_bias are added to (needs d_w_dtype = SPO_FP32).
- * No rows: d_weight and d_bias are zeros.  The workspace size never shrinks with rows or cols. */
+ * No rows: d_weight and d_bias are zeros.  The workspace size never shrinks with rows or cols.
+ * Of both calls: no other overlap of what is written with anything else; what lies between rows may be read, and is not written. */
 size_t spo_norm_bwd_workspace_bytes(const spo_norm_desc *d);
 int spo_norm_bwd(const spo_norm_desc *d, const float *mean, const float *rstd, const void *dy, int dy_dtype, int64_t dy_stride,
                  void *dx, int dx_dtype, void *d_weight, void *d_bias, int d_w_dtype, int accumulate, void *ws, size_t ws_bytes,

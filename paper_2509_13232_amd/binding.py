@@ -741,6 +741,31 @@ def _row_stride(t, name, shape=None):
     return apart
 
 
+def _lies(t):
+    """Where a tensor's elements lie: (first byte, bytes of a row, rows, bytes from row to row)."""
+    size = t.element_size()
+    rows, cols = t.shape if t.dim() == 2 else (1, t.numel())
+    return t.data_ptr(), cols * size, rows, (t.stride(0) if rows > 1 else cols) * size
+
+
+def _own_place(t, name, others, same=()):
+    """t is written: refused if it shares memory with another tensor, but for those in `same` that are where it is, of its type."""
+    if t is None or not t.numel():
+        return
+    at, row, rows, apart = _lies(t)
+    for other, its_name in others:
+        if other is None or not other.numel():
+            continue
+        at2, row2, rows2, apart2 = _lies(other)
+        if at + (rows - 1) * apart + row <= at2 or at2 + (rows2 - 1) * apart2 + row2 <= at:
+            continue
+        if any(other is s for s in same) and (at, row, rows, apart, t.dtype) == (at2, row2, rows2, apart2, other.dtype):
+            continue
+        if apart == apart2 and rows > 1 and rows2 > 1 and row <= (at2 - at) % apart <= apart - row2:   # columns of one buffer
+            continue
+        raise ValueError(f"{name}: overlaps {its_name}")
+
+
 def make_norm_desc(x, weight=None, bias=None, eps=1e-6, kind=SPO_NORM_LAYER, y_dtype=None):
     """Builds the C descriptor; returns (desc, keepalive tuple).  x: [rows, cols], rows of consecutive elements, any distance of at
     least cols apart.  weight, bias: [cols] of one type, or None for ones and zeros.  y_dtype: of the outputs (x's)."""
@@ -774,6 +799,7 @@ def spo_norm_fwd(desc, out=None, want_stats=True):
         apart = _row_stride(out, "out", (d.rows, d.cols))
         if out.dtype != keep[3]:
             raise TypeError(f"out: expected {keep[3]}")
+        _own_place(out, "out", ((x, "x"), (keep[1], "weight"), (keep[2], "bias")), (x,))
     rstd = _per_token(d.rows, x.device) if want_stats else None
     mean = _per_token(d.rows, x.device) if want_stats and d.kind == SPO_NORM_LAYER else None
     _check(lib().spo_norm_fwd(C.byref(d), _ptr(out), apart, _ptr(mean), _ptr(rstd), _stream()), "spo_norm_fwd")
@@ -802,6 +828,7 @@ def spo_norm_bwd(desc, mean, rstd, dy, dx=None, dx_dtype=None, d_weight=None, d_
         raise TypeError("mean: expected the forward's")
     _want(rstd, torch.float32, "rstd", d.rows)
     _want(mean, torch.float32, "mean", d.rows)
+    _here(rstd, "rstd"), _here(mean, "mean")
     if not want_dx:
         dx = None
     elif dx is None:
@@ -810,6 +837,8 @@ def spo_norm_bwd(desc, mean, rstd, dy, dx=None, dx_dtype=None, d_weight=None, d_
         _want_float(dx, "dx", d.rows * d.cols)
         if tuple(dx.shape) != (d.rows, d.cols):
             raise ValueError(f"dx: expected {(d.rows, d.cols)}, got {tuple(dx.shape)}")
+    read = [(x, "x"), (dy, "dy"), (weight, "weight"), (bias, "bias"), (mean, "mean"), (rstd, "rstd")]
+    _own_place(dx, "dx", read, (x, dy))
     grads = []
     for name, of, given in (("d_weight", weight, d_weight), ("d_bias", bias, d_bias)):
         if of is None or not want_dw:
@@ -820,6 +849,7 @@ def spo_norm_bwd(desc, mean, rstd, dy, dx=None, dx_dtype=None, d_weight=None, d_
             raise ValueError(f"accumulate needs an existing {name}")
         else:
             given = torch.empty(d.cols, dtype=d_w_dtype, device=dev)
+        _own_place(given, name, [*read, (dx, "dx"), *((g, "d_weight") for g in grads)])
         grads.append(given)
     types = {g.dtype for g in grads if g is not None}
     if len(types) > 1:
@@ -953,6 +983,7 @@ def spo_adamw_update(desc, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_norm
     _want(lr_t, torch.float32, "lr", 1)
     _want(step_t, torch.int64, "step", 1)
     _want(grad_norm, torch.float32, "grad_norm", 1)
+    _here(lr_t, "lr"), _here(step_t, "step"), _here(grad_norm, "grad_norm")
     number = 0 if step_t is not None else operator.index(step)
     if not -1 << 63 <= number < 1 << 63:
         raise ValueError(f"step: {number} is beyond 64 bits")

@@ -203,8 +203,8 @@ __device__ __forceinline__ Coded encode8(const float (&x)[8], const uint32_t (&t
 // Roots and their codes.  The hardware's root is off by a place at most; a rounded one takes twice the instructions of all the
 // rest of its code.  Its last place decides a code only where root and threshold together lie within a place of the next code
 // (one value of 2^18), or the block's largest within a place of the next scale: then, and where a square is so small that the
-// hardware's root is not good, the wavefront's roots are made again.  (The kernel is bound by its instructions: 1180 us for 151936 x
-// 4096 with rounded roots throughout.)
+// hardware's root is not good, the wavefront's roots are made again.  (Vector instructions per element of the whole kernel: 56.5 with
+// rounded roots throughout, 47 so.)
 __device__ __forceinline__ Coded encode_roots(const float (&v)[8], float (&root)[8], const uint32_t (&threshold)[8]) {
     constexpr uint32_t kSmall = 0x0f800000;  // 2^-96
     constexpr uint32_t kPlace = 1u << (24 - RootCode::kDrop);  // of a magnitude, in a code's word
@@ -260,7 +260,8 @@ __device__ __forceinline__ void update32(const Tensor32 &t, int64_t begin, const
     if (t.copy) store4(t.copy + at, p, some);
 }
 
-// 8-bit states.  Eight lanes hold a block.  Whole: the workgroup's elements are all there.  (Weights and gradients in fp32 take no
+// 8-bit states.  Eight lanes hold a block, so that its scales are three moves between lanes away (151936 x 4096 in bf16: 1065-1126 us,
+// 10 bytes per element at 5.6-5.9 TB/s).  Whole: the workgroup's elements are all there.  (Weights and gradients in fp32 take no
 // non-temporal hint: both halves of a line are asked for, one after the other.)
 template <typename TP, typename TG, bool Whole, bool Stream>
 __device__ __forceinline__ void update8(const Tensor8 &t, int64_t begin, const AdamwScalars &a, const Shared &s) {
@@ -354,7 +355,8 @@ __device__ __forceinline__ double squares(const float (&g)[N], double sum) {
     for (int i = 0; i < N; ++i) sum = fma(static_cast<double>(g[i]), static_cast<double>(g[i]), sum);
     return sum;
 }
-// Squares of fp32 numbers are exact in 64 bits, and so nearly are their sums: the norm is the rounded true one.
+// Squares of fp32 numbers are exact in 64 bits, and so nearly are their sums: the norm is the rounded true one.  (78 million gradients
+// in bf16: 31 us where the Infinity Cache holds them; 44-49 behind a step that left it full of lines to be written back.)
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(Table<TensorNorm> table, double *__restrict__ parts) {
     __shared__ double scratch[kThreads / kWave];
     double sum = 0.0;
@@ -399,6 +401,7 @@ __global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *__re
 }
 
 // ------------------------------------------------------------------------------------------- values of an 8-bit state
+// HBM: 2 bytes read and 4 written per element (622 million: 592-613 us, 6.1-6.3 TB/s).
 __global__ void __launch_bounds__(kThreads) state_values_kernel(const uint8_t *m, const uint8_t *m_scale, const uint8_t *v, const uint8_t *v_scale, int64_t n,
                                                                 void *m_out, void *root_out, int dtype) {
     const int64_t at = (flat_block() * kThreads + threadIdx.x) * 8;

@@ -185,7 +185,8 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
     }
 }
 
-// Rows that the registers of a workgroup do not hold beside the sums of their columns: the sums of a row first ...
+// Rows that the registers of a workgroup do not hold beside the sums of their columns: the sums of a row first (13421 rows of 20000 in
+// bf16: 2.9 TB/s of what is read once and written once; both passes read at the rate of a copy) ...
 __global__ void __launch_bounds__(1024) norm_bwd_sums_kernel(NormArgs a, NormGrads g, int x_dtype, int dy_dtype, float *__restrict__ sums) {
     __shared__ float scratch[3 * 1024 / kWave];
     const int64_t row = flat_block();
@@ -278,8 +279,8 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const float *__restrict
 // ------------------------------------------------------------------------------------------------------------ host
 
 // How many workgroups the backward has: as many as the chip holds at once, in whole numbers per compute unit (284780 rows of 4096
-// in bf16: two of 4 wavefronts each 1160 us; 1.5, 2.5 or 3 of them, which leave units idle at the end, 1310 to 1320, and
-// 4, of which three fit, 1499).  Few rows: one each (713 rows of 1001: 7.4 us, two each 8.5, four 11.9).
+// in bf16, on one card: two of 8 wavefronts per unit 1284 us, one 1340, three 1320, four 1409; two of 4 wavefronts with two eights
+// per thread 1398).  Few rows: one to each group of lanes (713 rows of 1001: 6.1 us, two 7.7).
 static int bwd_parts(int64_t rows, int64_t cols) {
     const int64_t eights = ceil_div(cols, 8);
     int64_t most, each = 1;

@@ -84,11 +84,10 @@ __device__ __forceinline__ void load4(float (&x)[4], const float *p, int n) {
         if (i < n) x[i] = p[i];
 }
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-template <bool Stream = false>
 __device__ __forceinline__ void load4(float (&x)[4], const bf16_t *p, int n) {
     if (n >= 4) {
         typedef u32x2_t V __attribute__((aligned(2)));
-        const u32x2_t v = Stream ? __builtin_nontemporal_load(reinterpret_cast<const V *>(p)) : *reinterpret_cast<const V *>(p);
+        const u32x2_t v = *reinterpret_cast<const V *>(p);
         x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
         x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
         return;
@@ -107,13 +106,11 @@ __device__ __forceinline__ void store4(float *p, const float (&x)[4], int n) {
     for (int i = 0; i < 4; ++i)
         if (i < n) p[i] = x[i];
 }
-template <bool Stream = false>
 __device__ __forceinline__ void store4(bf16_t *p, const float (&x)[4], int n) {
     const u32x2_t v = {pack_bf16x2_rn(x[0], x[1]), pack_bf16x2_rn(x[2], x[3])};
     if (n >= 4) {
         typedef u32x2_t V __attribute__((aligned(2)));
-        if (Stream) __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
-        else *reinterpret_cast<V *>(p) = v;
+        *reinterpret_cast<V *>(p) = v;
         return;
     }
 #pragma unroll
@@ -245,22 +242,20 @@ __device__ __forceinline__ void load_weights(float (&x)[E], const void *p, int d
 }
 
 // Of a type that the kernel is told at run time (the same for all its threads): arrays that are small beside the others.
-template <bool Stream = false>
 __device__ __forceinline__ void load_typed(float (&x)[8], const void *p, int dtype, int64_t at, int n) {
     if (dtype == SPO_FP32) {
         Raw8<float> r;
-        load_some<Stream>(r, static_cast<const float *>(p) + at, n);
+        load_some(r, static_cast<const float *>(p) + at, n);
         raw_floats(r, x);
     } else {
         Raw8<bf16_t> r;
-        load_some<Stream>(r, static_cast<const bf16_t *>(p) + at, n);
+        load_some(r, static_cast<const bf16_t *>(p) + at, n);
         raw_floats(r, x);
     }
 }
-template <bool Stream = false>
 __device__ __forceinline__ void store_typed(void *p, int dtype, int64_t at, const float (&x)[8], int n) {
-    if (dtype == SPO_FP32) store_some<Stream>(static_cast<float *>(p) + at, x, n);
-    else store_some<Stream>(static_cast<bf16_t *>(p) + at, x, n);
+    if (dtype == SPO_FP32) store_some(static_cast<float *>(p) + at, x, n);
+    else store_some(static_cast<bf16_t *>(p) + at, x, n);
 }
 __device__ __forceinline__ int within(int64_t at, int64_t n) { return at >= n ? 0 : n - at < 8 ? static_cast<int>(n - at) : 8; }
 

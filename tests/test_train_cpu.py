@@ -163,7 +163,22 @@ def test_normalisations_look_at_their_tensors(reached):  # noqa: F811
     _refused(ValueError, "accumulate", back, d, mean, rstd, dy, accumulate=True)
     _refused(ValueError, "accumulate", back, d, mean, rstd, dy, d_weight=_dev(100), accumulate=True)
     _refused(ValueError, "workspace", back, d, mean, rstd, dy, workspace=_dev(8, dtype=torch.uint8))
+    # what is written has a place of its own, or is the input itself
+    wide = torch.zeros(6, 220)
+    part = lambda t: OnDevice(t)   # noqa: E731
+    dw = make(part(wide[:5, :100]), w, b)
+    _refused(ValueError, "out: overlaps x", spo.spo_norm_fwd, dw, out=part(wide[1:, :100]))
+    _refused(ValueError, "out: overlaps x", spo.spo_norm_fwd, dw, out=part(wide[:5, 99:199]))
+    _refused(ValueError, "out: overlaps weight", spo.spo_norm_fwd, make(x, part(wide.view(-1)[:100])), out=part(wide[:5, :100]))
+    _refused(ValueError, "dx: overlaps x", back, make(part(wide.view(-1)[:500].view(5, 100))), mean, rstd, dy, dx=part(wide.view(-1)[8:508].view(5, 100)))
+    _refused(ValueError, "d_weight: overlaps dy", back, d, mean, rstd, part(wide[:5, :100]), d_weight=part(wide[0, :100]))
+    _refused(ValueError, "d_bias: overlaps d_weight", back, d, mean, rstd, dy, d_weight=part(wide[0, :100]), d_bias=part(wide[0, 99:199]))
     assert not reached
+    spo.spo_norm_fwd(dw, out=part(wide[:5, 100:200]))                               # other columns of the same rows
+    spo.spo_norm_fwd(dw, out=dw[1][0])
+    back(d, mean, rstd, dy, dx=dy)
+    assert reached == ["spo_norm_fwd", "spo_norm_fwd", "spo_norm_bwd"]
+    reached.clear()
     spo.spo_norm_fwd(d, out=OnDevice(torch.zeros(5, 120)[:, 3:103]))
     back(d, mean, rstd, dy, dx=_dev(5, 100), d_weight=_dev(100), d_bias=_dev(100), accumulate=True)
     back(make(x, kind=spo.SPO_NORM_RMS), None, rstd, dy)
@@ -236,6 +251,9 @@ def test_a_tensor_of_another_device_is_refused(reached, monkeypatch):  # noqa: F
     _refused(ValueError, "current device", spo.make_norm_desc, x, Elsewhere(torch.zeros(100)))
     d = spo.make_norm_desc(x)
     _refused(ValueError, "current device", spo.spo_norm_bwd, d, _dev(5), _dev(5), far)
+    _refused(ValueError, "current device", spo.spo_norm_bwd, d, Elsewhere(torch.zeros(5)), _dev(5), _dev(5, 100))
+    step = spo.make_adamw_desc([_dev(5)], [_dev(5)], [_state(5)])
+    _refused(ValueError, "grad_norm: is on", spo.spo_adamw_update, step, 0.1, 1, grad_norm=Elsewhere(torch.zeros(1)))
     _refused(ValueError, "current device", spo.make_adamw_desc, [Elsewhere(torch.zeros(5))], [_dev(5)], [_state(5)])
     _refused(ValueError, "current device", spo.make_adamw_desc, [_dev(5)], [Elsewhere(torch.zeros(5))], [_state(5)])
     assert not reached
