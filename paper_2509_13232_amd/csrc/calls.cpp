@@ -399,7 +399,7 @@ PyObject *norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor *mean = a[2] == Py_None ? nullptr : dense(a[2], at::kFloat, d->rows), *rstd = dense(a[3], at::kFloat, d->rows);
     int64_t apart;
     const at::Tensor *dy = rows_of(a[4], d->rows, d->cols, apart);
-    if (!rstd || !dy || (!mean && (layer || a[2] != Py_None))) return none();
+    if (!rstd || !here(rstd) || !dy || (mean ? !here(mean) : layer || a[2] != Py_None)) return none();
     const at::Tensor *ws = workspace(a[5], spo_norm_bwd_workspace_bytes(d));
     if (!ws) return none();
     const at::Tensor dx = fresh({d->rows, d->cols}, type_of(d->x_dtype), *x);
