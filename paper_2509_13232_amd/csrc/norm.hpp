@@ -34,7 +34,7 @@ struct NormArgs {
     int64_t x_stride, rows;
     int cols, layer, w_dtype;
     const void *w, *b;
-    float eps;
+    float eps, inv_n;  // 1 / cols
 };
 
 template <int M, typename Move>
@@ -133,7 +133,7 @@ static int validate(const spo_norm_desc *d) {
 }
 static NormArgs args_of(const spo_norm_desc *d) {
     return NormArgs{d->x, d->x_stride ? d->x_stride : d->cols, d->rows, static_cast<int>(d->cols), d->kind == SPO_NORM_LAYER, d->w_dtype,
-                    d->weight, d->bias, d->eps};
+                    d->weight, d->bias, d->eps, 1.0f / static_cast<float>(d->cols)};
 }
 
 }  // namespace spo

@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
             floats(raw[k], v[r][k]);
 #pragma unroll
             for (int i = 0; i < E; ++i) v[r][k][i] -= base[r];
-            if (some < E)
+            if (__any(some < E))  // (few wavefronts)
 #pragma unroll
                 for (int i = 0; i < E; ++i) v[r][k][i] = i < some ? v[r][k][i] : 0.0f;
         }
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
             base[r] = 0.0f;
             if (a.layer) {
                 const int some = row_of(r) < a.rows ? within_e<E>(0, a.cols) : 0;
-                const float share = some == E ? 1.0f / E : 1.0f / static_cast<float>(max(some, 1));
+                const float share = some == E ? 1.0f / E : __builtin_amdgcn_rcpf(static_cast<float>(max(some, 1)));  // (any pivot will do)
                 float f[E];
                 floats_some(head[r], f, some);
 #pragma unroll
@@ -60,7 +60,6 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
             differences(r, raw[r]);
         }
     }
-    const float n = static_cast<float>(a.cols);
     float off[R], var[R], squares[R], rs[R];
     const auto sum_up = [&](float *where) {
         float s[2 * R];
@@ -78,9 +77,9 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
         row_sums<L, W, 2 * R, float>(s, where);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            off[r] = a.layer ? s[2 * r] / n : 0.0f;
+            off[r] = a.layer ? s[2 * r] * a.inv_n : 0.0f;
             squares[r] = s[2 * r + 1];
-            var[r] = squares[r] / n - off[r] * off[r];
+            var[r] = squares[r] * a.inv_n - off[r] * off[r];
             var[r] = var[r] < 0.0f ? 0.0f : var[r];
         }
     };
@@ -102,7 +101,7 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
     bool odd = false;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        rs[r] = 1.0f / sqrtf(var[r] + a.eps);
+        rs[r] = __builtin_amdgcn_rsqf(var[r] + a.eps);  // (off by a place at most)
         odd |= !(squares[r] <= kSquaresHigh && var[r] + a.eps >= kSquaresLow);
     }
     if (any_row<L>(odd)) {  // squares, or their sum, that left fp32's range
@@ -137,18 +136,17 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
     for (int k = 0; k < NV; ++k) {
         const int c = (k * TR + t) * E, inside = within_e<E>(c, a.cols);
         float w[E], b[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) w[i] = 1.0f, b[i] = 0.0f;
         if (a.w) load_weights(w, a.w, a.w_dtype, c, inside);
         if (a.b) load_weights(b, a.b, a.w_dtype, c, inside);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int some = some_of(r, k);
             if (some == 0) continue;
+            const float shift = -off[r] * rs[r];  // (of two deviations at most, so that its rounding is small beside h's bound)
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                v[r][k][i] = (v[r][k][i] - off[r]) * rs[r];
-                if (a.w) v[r][k][i] *= w[i];
-                if (a.b) v[r][k][i] += b[i];
-            }
+            for (int i = 0; i < E; ++i) v[r][k][i] = fmaf(fmaf(v[r][k][i], rs[r], shift), w[i], b[i]);
             store_e<Stream>(y + row_of(r) * y_stride + c, v[r][k], some);
         }
     }
