@@ -91,6 +91,14 @@ __device__ __forceinline__ void join_waves(T (&v)[M], T *scratch) {
         for (int i = 0; i < waves; ++i) add(i);
     }
 }
+// The value of the first of L neighbouring lanes, for all of them.
+template <int L>
+__device__ __forceinline__ float first_lane(float v) {
+    const int x = __float_as_int(v);
+    if constexpr (L == kWave) return __int_as_float(__builtin_amdgcn_readfirstlane(x));
+    else if constexpr (L == 4) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x00, 0xf, 0xf, true));
+    else return __shfl(v, static_cast<int>(threadIdx.x) & ~(L - 1) & (kWave - 1), kWave);
+}
 // Sums over the L lanes that share a row, or with L = 0 over the W wavefronts of the workgroup.
 template <int L, int W, int M, typename T>
 __device__ __forceinline__ void row_sums(T (&v)[M], T *scratch) {

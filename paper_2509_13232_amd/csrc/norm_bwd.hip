@@ -73,16 +73,30 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TR + t) * E, some = live ? within_e<E>(c, a.cols) : 0;
             float h[E], d[E];
-            floats_some(rx[k], h, some);
-            floats_some(ry[k], d, some);
-            if constexpr (InLds)
+            if constexpr (InLds) {  // (registers are short: masks cost less than a branch)
+                floats_some(rx[k], h, some);
+                floats_some(ry[k], d, some);
                 if (a.w) load_weights(w[k], a.w, a.w_dtype, c, some);
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float hi = i < some ? (h[i] - mu) * rs : 0.0f, gi = d[i] * w[k][i];
-                s[0] += gi * hi;
-                s[1] += gi;
-                s[2] += hi;
+                for (int i = 0; i < E; ++i) {
+                    const float hi = i < some ? (h[i] - mu) * rs : 0.0f, gi = d[i] * w[k][i];
+                    s[0] += gi * hi;
+                    s[1] += gi;
+                    s[2] += hi;
+                }
+            } else {
+                floats(rx[k], h);
+                floats(ry[k], d);
+#pragma unroll
+                for (int i = 0; i < E; ++i) h[i] = (h[i] - mu) * rs, d[i] *= w[k][i];
+                if (__any(some < E))  // (few wavefronts)
+#pragma unroll
+                    for (int i = 0; i < E; ++i) h[i] = i < some ? h[i] : 0.0f, d[i] = i < some ? d[i] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < E; ++i) s[0] += d[i] * h[i];
+                if (a.layer)
+#pragma unroll
+                    for (int i = 0; i < E; ++i) s[1] += d[i], s[2] += h[i];
             }
         }
         float off = 0.0f, mean_g = 0.0f, mean_gh;
@@ -97,21 +111,20 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
             mean_gh = one[0] * inv_n;
         }
         turn ^= 1;
+        const float of_g = -rs * mean_g, of_h = -rs * mean_gh;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TR + t) * E, some = live ? within_e<E>(c, a.cols) : 0;
             float h[E], d[E], dx[E], dyh[E];
-            if constexpr (L) {  // (a row that is not there adds nothing)
-                floats_some(rx[k], h, some);
-                floats_some(ry[k], d, some);
-            } else {  // (what lies behind the columns goes nowhere)
-                floats(rx[k], h);
-                floats(ry[k], d);
-            }
+            floats(rx[k], h);
+            floats(ry[k], d);
+            if (L && __any(some < E))  // (a row that is not there adds nothing; what lies behind the columns goes nowhere)
+#pragma unroll
+                for (int i = 0; i < E; ++i) h[i] = i < some ? h[i] : 0.0f, d[i] = i < some ? d[i] : 0.0f;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float hi = (h[i] - mu) * rs - off;
-                dx[i] = rs * (d[i] * w[k][i] - mean_g - hi * mean_gh);
+                const float hi = fmaf(h[i] - mu, rs, -off);
+                dx[i] = fmaf(hi, of_h, fmaf(d[i] * w[k][i], rs, of_g));
                 if constexpr (InLds) {
                     dyh[i] = d[i] * hi;
                 } else {

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
         for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) fetch<E, Stream>(raw[r][k], x_of(r) + (k * TR + t) * E, some_of(r, k), past_of(r));
-            if (a.layer) fetch<E, false>(head[r], x_of(r), row_of(r) < a.rows ? within_e<E>(0, a.cols) : 0, past_of(r));
+            if (L == 0 && a.layer) fetch<E, false>(head[r], x_of(r), row_of(r) < a.rows ? within_e<E>(0, a.cols) : 0, past_of(r));
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -53,9 +53,10 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVecto
                 const int some = row_of(r) < a.rows ? within_e<E>(0, a.cols) : 0;
                 const float share = some == E ? 1.0f / E : __builtin_amdgcn_rcpf(static_cast<float>(max(some, 1)));  // (any pivot will do)
                 float f[E];
-                floats_some(head[r], f, some);
+                floats_some(L ? raw[r][0] : head[r], f, some);
 #pragma unroll
                 for (int i = 0; i < E; ++i) base[r] += f[i] * share;
+                if constexpr (L) base[r] = first_lane<L>(base[r]);
             }
             differences(r, raw[r]);
         }
