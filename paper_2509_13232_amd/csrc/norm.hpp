@@ -5,9 +5,9 @@
 //
 // Bound by HBM.  A row is held in registers from its one read to its one write: by 4 to 64 lanes of a wavefront (rows of up to
 // 1536 elements in the forward, 1024 in the backward), or by 4 to 16 wavefronts of a workgroup.  Rows that are longer than the
-// registers of a backward's workgroup are read twice there.  (284780 rows of 4096 in bf16: forward 766-790 us, 6.0 TB/s, backward
-// 1191-1240, 5.8; 17043 rows of 4096 from fp32 to bf16: forward 77, 5.4; 8192 of 1024, which the caches hold: 11.4 and 15.4.  One row:
-// 2.9 us, a launch and its chain of loads and sums.)
+// registers of a backward's workgroup are read twice there.  (284780 rows of 4096 in bf16: forward 751-785 us, 6.1 TB/s, backward
+// 1180-1290 from card to card, 5.4 to 5.9; 17043 rows of 4096 from fp32 to bf16: forward 74, 5.7; 8192 of 1024, which the caches hold:
+// 9.6 and 14.4.  One row: 2.6 us, a launch and its chain of loads and sums.)
 //
 // The forward takes its sums about a pivot, the mean of the row's first elements: one exchange between the lanes gives mean and
 // variance.  Where the pivot was off by more than two deviations the row is read once more and summed about its mean, so that no
@@ -111,7 +111,7 @@ __device__ __forceinline__ bool any_row(bool one) { return L == 0 ? one : __any(
 
 constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e38f;  // a variance below, sums of squares above: formed again in 64 bits
 // Elements of a vector: 16 bytes of bf16; four where fp32 is among the arrays, so that a wavefront's loads are whole lines
-// (17043 rows of 4096 from fp32 to bf16 with eight neighbours per thread: 81 us).
+// (17043 rows of 4096 from fp32 to bf16: 78 us, with eight neighbours per thread 81).
 template <typename TX, typename TY>
 constexpr int kVector = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
 
@@ -121,7 +121,7 @@ static bool past_cache(int64_t rows, int64_t cols) { return rows * cols * static
 
 // Lanes that hold a row of so many eights, one each (or two or three, with all lanes of a wavefront); and wavefronts where a workgroup
 // holds it.  These come in fours: a workgroup's wavefronts are dealt to the four SIMDs of a compute unit from the first one on, so
-// that five of them leave room for fewer workgroups (52428 rows of 5120 in bf16 by five wavefronts: 298 us).
+// that five of them leave room for fewer workgroups (52428 rows of 5120 in bf16 by five wavefronts: 298 us, by eight 233).
 static int lanes_of(int64_t eights) { return eights <= 4 ? 4 : eights <= 8 ? 8 : eights <= 16 ? 16 : eights <= 32 ? 32 : kWave; }
 static int fours_of(int64_t eights, int each) { return static_cast<int>(ceil_div(eights, each * 4 * kWave)) * 4; }
 

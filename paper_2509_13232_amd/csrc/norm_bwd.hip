@@ -292,8 +292,8 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const float *__restrict
 // ------------------------------------------------------------------------------------------------------------ host
 
 // How many workgroups the backward has: as many as the chip holds at once, in whole numbers per compute unit (284780 rows of 4096
-// in bf16, on one card: two of 8 wavefronts per unit 1284 us, one 1340, three 1320, four 1409; two of 4 wavefronts with two eights
-// per thread 1398).  Few rows: one to each group of lanes (713 rows of 1001: 6.1 us, two 7.7).
+// in bf16, on one card: two of 8 wavefronts per unit 1280 us, one 1266 to 1340, three 1366; two of 4 wavefronts with two eights per
+// thread 1328).  Few rows: one to each group of lanes (713 rows of 1001: 5.9 us, two 7.4).
 static int bwd_parts(int64_t rows, int64_t cols) {
     const int64_t eights = ceil_div(cols, 8);
     int64_t most, each = 1;

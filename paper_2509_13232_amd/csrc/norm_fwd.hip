@@ -4,15 +4,14 @@
 namespace spo {
 
 // Those that share a row (L lanes, or with L = 0 the workgroup) hold R rows: two side by side where their registers suffice and rows
-// are many; weight and bias are read once for both, and their sums cross the lanes together (65536 rows of 4096 in bf16: 206 -> 195 us;
-// 8192 rows of 1024, which are there at once: 11.4 -> 13.5).
+// are many; weight and bias are read once for both, and their sums cross the lanes together (284780 rows of 4096 in bf16: 822 -> 770 us,
+// 131072 of 2048: 222 -> 185, 4194304 of 64: 222 -> 178; but 713 rows of 1001, which are there at once: 4.2 -> 5.2).
 // Eights: eight elements per thread times this.  The k-th vector of the t-th of TR threads begins at column (k * TR + t) * E.
-// Wavefronts per SIMD that the registers have to leave room for: what is held per thread matters less than how much is under way
-// (21845 rows of 12288 in bf16: 271 us with five, 226 with six).
-constexpr int fwd_occupancy(int E, int W, int eights) { return W == 16 || eights == 8 ? 4 : eights == 4 ? (E == 8 ? 6 : 5) : 4; }
+// Instructions count beside the bytes: with divisions, masks for all and an epilogue of four instructions per element, 262144 rows of
+// 1024 took 188 us instead of 176, 131072 of 2048 210 instead of 185.
 template <typename TX, typename TY, int L, int W, int Eights, int R, bool Stream>
-__global__ void __launch_bounds__(L ? kThreads : W * kWave, fwd_occupancy(kVector<TX, TY>, W, Eights)) norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd,
-                                                                             int64_t apart) {
+__global__ void __launch_bounds__(L ? kThreads : W * kWave, 4) norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd,
+                                                                         int64_t apart) {
     constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E, kRows = L ? kThreads / (L ? L : 1) : 1;
     __shared__ float scratch[2][L ? 1 : 2 * R * W];
     __shared__ double wide[L ? 1 : 2 * R * W];
