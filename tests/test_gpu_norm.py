@@ -314,9 +314,9 @@ def test_results_do_not_depend_on_the_run_nor_on_what_the_workspace_held(spo):
     assert all(torch.equal(p, q) for p, q in zip(first, second))
 
 
-def test_on_another_stream_and_in_a_graph(spo):
-    say("norm on a stream and in a graph")
-    T, N = 500, 1200
+@pytest.mark.parametrize("T,N", [(500, 1200), (40, 12000), (20, 20000)])
+def test_on_another_stream_and_in_a_graph(spo, T, N):
+    say(f"norm on a stream and in a graph, {T} x {N}")
     x, dy, w, b = rows(T, N, BF16), rows(T, N, BF16, seed=1), vector(N, BF16, 2, 1.0), vector(N, BF16, 3)
     d = spo.make_norm_desc(x, w, b)
     ws = torch.empty(spo.spo_norm_bwd_workspace_bytes(d), dtype=torch.uint8, device="cuda")
