@@ -217,3 +217,54 @@ def test_errors_are_those_of_the_general_way(monkeypatch):
                 except Exception as err:
                     seen.append((type(err), str(err), getattr(err, "status", None)))
         assert isinstance(seen[0], tuple) and seen[0] == seen[1], (i, seen)
+
+
+def test_calls_on_two_streams_at_once():
+    say("normalisations and steps on two streams at once")
+    g = torch.Generator().manual_seed(6)
+    make = lambda *s: torch.randn(s, generator=g).cuda()   # noqa: E731
+
+    class Lane:
+        def __init__(self, N):
+            self.x, self.dy, self.w, self.b = make(3000, N), make(3000, N), make(N), make(N)
+            self.p, self.grads = [make(N), make(70000)], [make(N), make(70000)]
+            self.norm = spo.make_norm_desc(self.x, self.w, self.b)
+            self.ws = torch.empty(spo.spo_norm_bwd_workspace_bytes(self.norm), dtype=torch.uint8, device="cuda")
+            self.states, self.first = [spo.adamw_state(t, 8) for t in self.p], [t.clone() for t in self.p]
+            self.step = spo.make_adamw_desc(self.p, self.grads, self.states)
+            self.count, self.room = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.empty(1 << 18, dtype=torch.uint8, device="cuda")
+
+        def run(self):
+            y, mean, rstd = spo.spo_norm_fwd(self.norm)
+            out = spo.spo_norm_bwd(self.norm, mean, rstd, self.dy, workspace=self.ws)
+            size = spo.spo_grad_norm(self.step, workspace=self.room)
+            spo.spo_adamw_update(self.step, 1e-3, self.count, grad_norm=size, max_norm=1.0)
+            return [y, *out, size]
+
+        def again(self):
+            for t, u in zip(self.p, self.first):
+                t.copy_(u)
+            for s in self.states:
+                for t in s:
+                    t.zero_()
+            self.count.zero_()
+
+        def held(self):
+            return [t.clone() for t in (*self.p, *(t for s in self.states for t in s), self.count)]
+
+    lanes, streams = [Lane(1000), Lane(5000)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    want = []
+    for lane in lanes:
+        for _ in range(6):
+            out = lane.run()
+        want.append((out, lane.held()))
+        lane.again()
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = lanes[i].run()
+    torch.cuda.synchronize()
+    for i, lane in enumerate(lanes):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want[i][0])) and all(torch.equal(a, b) for a, b in zip(lane.held(), want[i][1])), i
