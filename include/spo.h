@@ -461,8 +461,8 @@ int spo_muon_update(const spo_orth_desc *d, void *W, int w_dtype, float *momentu
  * and, with g = dy w:
  *   dx = rstd (g - sum g / cols - h sum (g h) / cols), SPO_NORM_RMS without the second term;
  *   d_weight = sum over rows of dy h;  d_bias = sum over rows of dy.
- * Sums in fp32 in a fixed order (results are bitwise reproducible), in 64 bits where squares leave fp32's range.  A mean far
- * from zero costs no digits: what rounding it takes off is found again from the row, in the backward too.  A row that holds
+ * Sums in fp32 in a fixed order (results are bitwise reproducible), in 64 bits where squares or differences leave fp32's range.
+ * A mean far from zero costs no digits: what rounding it takes off is found again from the row, in the backward too.  A row that holds
  * a NaN, or with SPO_NORM_LAYER an infinity, gives NaN throughout (with SPO_NORM_RMS an infinity gives NaN there and zeros
  * elsewhere); its dx is NaN, and so is d_weight where its h is.  A row of equal elements with eps = 0 gives NaN.
  * ------------------------------------------------------------------------- */

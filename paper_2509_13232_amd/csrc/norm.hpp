@@ -11,8 +11,9 @@
 //
 // The forward takes its sums about a pivot, the mean of the row's first elements: one exchange between the lanes gives mean and
 // variance.  Where the pivot was off by more than two deviations the row is read once more and summed about its mean, so that no
-// digits are lost.  The backward has the mean as fp32; what rounding it took off is common to all elements of a row and small,
-// but not beside the deviations of rows far from zero, so that the sum of (x - mean) rstd is taken along and put right.
+// digits are lost; where squares or differences leave fp32's range, it is read once more in 64 bits.  The backward has the mean as
+// fp32; what rounding it took off is common to all elements of a row and small, but not beside the deviations of rows far from zero,
+// so that the sum of (x - mean) rstd is taken along and put right.
 #pragma once
 
 #include <algorithm>
@@ -110,6 +111,7 @@ template <int L>
 __device__ __forceinline__ bool any_row(bool one) { return L == 0 ? one : __any(one) != 0; }
 
 constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e38f;  // a variance below, sums of squares above: formed again in 64 bits
+constexpr float kLargest = 3.402823466e38f;
 // Elements of a vector: 16 bytes of bf16; four where fp32 is among the arrays, so that a wavefront's loads are whole lines
 // (17043 rows of 4096 from fp32 to bf16: 78 us, with eight neighbours per thread 81).
 template <typename TX, typename TY>

@@ -8,13 +8,17 @@ namespace spo {
 // 131072 of 2048: 222 -> 185, 4194304 of 64: 222 -> 178; but 713 rows of 1001, which are there at once: 4.2 -> 5.2).
 // Eights: eight elements per thread times this.  The k-th vector of the t-th of TR threads begins at column (k * TR + t) * E.
 // Instructions count beside the bytes: with divisions, masks for all and an epilogue of four instructions per element, 262144 rows of
-// 1024 took 188 us instead of 176, 131072 of 2048 210 instead of 185.
+// 1024 took 188 us instead of 176, 131072 of 2048 210 instead of 185.  Registers, too, which the path of rows in 64 bits takes more of
+// than the others: without the bounds on scalar ones 131072 rows of 2048 in bf16, rms, took 177 us instead of 168, 1342177 of 200
+// 194 instead of 187; without those on vector ones 345476 of 777 234 instead of 220.  (fp32 needs more of these and does not gain.)
+template <typename TX, typename TY, int L, int Eights, int R>
+constexpr int kFwdWaves = R == 1 || kVector<TX, TY> == 4 ? 4 : Eights == 1 ? 8 : L ? 6 : 5;  // per SIMD, at least
 template <typename TX, typename TY, int L, int W, int Eights, int R, bool Stream>
-__global__ void __launch_bounds__(L ? kThreads : W * kWave, 4) norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd,
-                                                                         int64_t apart) {
+__global__ void __attribute__((amdgpu_num_sgpr(80))) __launch_bounds__(L ? kThreads : W * kWave, (kFwdWaves<TX, TY, L, Eights, R>))
+    norm_fwd_kernel(NormArgs a, TY *y, int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd, int64_t apart) {
     constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E, kRows = L ? kThreads / (L ? L : 1) : 1;
     __shared__ float scratch[2][L ? 1 : 2 * R * W];
-    __shared__ double wide[L ? 1 : 2 * R * W];
+    __shared__ double wide[R][L ? 1 : 2 * W];
     constexpr int TR = L ? L : W * kWave;
     const int t = L ? static_cast<int>(threadIdx.x) % L : static_cast<int>(threadIdx.x);
     const int64_t first = flat_block() * kRows + (L ? threadIdx.x / (L ? L : 1) : 0);
@@ -98,33 +102,45 @@ __global__ void __launch_bounds__(L ? kThreads : W * kWave, 4) norm_fwd_kernel(N
         }
         sum_up(scratch[1]);
     }
-    bool odd = false;
+    // Squares or differences that left fp32's range, where the comparison above says nothing, or so small a variance
+    bool odd[R], any_odd = false;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         rs[r] = __builtin_amdgcn_rsqf(var[r] + a.eps);  // (off by a place at most)
-        odd |= !(squares[r] <= kSquaresHigh && var[r] + a.eps >= kSquaresLow);
+        odd[r] = !(squares[r] <= kSquaresHigh && var[r] + a.eps >= kSquaresLow);
+        any_odd |= odd[r];
     }
-    if (any_row<L>(odd)) {  // squares, or their sum, that left fp32's range
-        double d[2 * R];
+    if (any_row<L>(any_odd)) {
+        // Such rows once more from memory, in 64 bits, element by element; the others of the wavefront along with them, as below.  The
+        // pivot lies within sqrt(cols / E) <= 128 deviations of the mean, as the mean of E of the row's elements does: one exchange keeps all
+        // digits that matter, 2^-53 128^2 being 2e-12.
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            d[2 * r] = d[2 * r + 1] = 0.0;
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    d[2 * r] += static_cast<double>(v[r][k][i]);
-                    d[2 * r + 1] += static_cast<double>(v[r][k][i]) * static_cast<double>(v[r][k][i]);
+            const bool there = row_of(r) < a.rows;
+            const TX *const x = x_of(r);
+            double d[2] = {0.0, 0.0};
+            const double pivot = __builtin_amdgcn_fmed3f(base[r], -kLargest, kLargest);  // (a row that holds an infinity has no finite sum either way)
+            if (there && odd[r])
+#pragma unroll 1
+                for (int c = t; c < a.cols; c += TR) {
+                    const double from_pivot = static_cast<double>(Vec<TX>::get(x + c)) - pivot;
+                    d[0] += from_pivot;
+                    d[1] = fma(from_pivot, from_pivot, d[1]);
                 }
-        }
-        row_sums<L, W, 2 * R, double>(d, wide);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (!(squares[r] <= kSquaresHigh && var[r] + a.eps >= kSquaresLow)) {
-                const double o = a.layer ? d[2 * r] / a.cols : 0.0;
-                off[r] = static_cast<float>(o);
-                rs[r] = static_cast<float>(1.0 / sqrt(d[2 * r + 1] / a.cols - o * o + a.eps));
+            row_sums<L, W, 2, double>(d, wide[r]);
+            if (!there) continue;
+            // (true divisions: of equal elements beside the pivot they give no variance at all)
+            const double o = a.layer ? d[0] / a.cols : 0.0, mu = pivot + o, spread = d[1] / a.cols - o * o, gain = 1.0 / sqrt((spread < 0.0 ? 0.0 : spread) + a.eps);
+            if (t == 0 && mean && a.layer) mean[row_of(r)] = odd[r] ? static_cast<float>(mu) : base[r] + off[r];
+            if (t == 0 && rstd) rstd[row_of(r)] = odd[r] ? static_cast<float>(gain) : rs[r];
+#pragma unroll 1
+            for (int c = t; c < a.cols; c += TR) {
+                const float f = Vec<TX>::get(x + c);
+                const float h = odd[r] ? static_cast<float>((static_cast<double>(f) - mu) * gain) : fmaf(f - base[r], rs[r], -off[r] * rs[r]);
+                Vec<TY>::put(y + row_of(r) * y_stride + c, fmaf(h, a.w ? load_weight(a.w, a.w_dtype, c) : 1.0f, a.b ? load_weight(a.b, a.w_dtype, c) : 0.0f));
             }
+        }
+        return;
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)

@@ -221,6 +221,9 @@ __device__ __forceinline__ void store_e(bf16_t *p, const float (&x)[E], int n) {
 template <int E>
 __device__ __forceinline__ int within_e(int at, int n) { return at >= n ? 0 : n - at < E ? n - at : E; }
 // Weights of a type that the kernel is told at run time; zeros behind the n-th.
+__device__ __forceinline__ float load_weight(const void *p, int dtype, int at) {
+    return dtype == SPO_FP32 ? static_cast<const float *>(p)[at] : bf16_to_f32(static_cast<const bf16_t *>(p)[at]);
+}
 template <int E>
 __device__ __forceinline__ void load_weights(float (&x)[E], const void *p, int dtype, int at, int n) {
 #pragma unroll
