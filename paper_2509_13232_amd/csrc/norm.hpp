@@ -112,6 +112,9 @@ __device__ __forceinline__ bool any_row(bool one) { return L == 0 ? one : __any(
 
 constexpr float kSquaresLow = 1e-30f, kSquaresHigh = 1e38f;  // a variance below, sums of squares above: formed again in 64 bits
 constexpr float kLargest = 3.402823466e38f;
+// Half of x - mean, of half the mean: finite for all finite rows.  The backward works with halves of h and doubles what it makes of them;
+// but for subnormal numbers that changes no rounding.
+__device__ __forceinline__ float half_from(float x, float half_mean) { return fmaf(x, 0.5f, -half_mean); }
 // Elements of a vector: 16 bytes of bf16; four where fp32 is among the arrays, so that a wavefront's loads are whole lines
 // (17043 rows of 4096 from fp32 to bf16: 78 us, with eight neighbours per thread 81).
 template <typename TX, typename TY>

@@ -10,19 +10,19 @@ struct NormGrads {
     int64_t dy_stride;
     void *dx;
     int dx_dtype;
-    float *dw_parts, *db_parts;  // a row of partial sums per workgroup, or NULL
+    float *dw_parts, *db_parts;  // a row of partial sums per workgroup (of dy h / 2, of dy), or NULL
     int64_t part_stride;
 };
 
 // Those that share a row (L lanes, or with L = 0 the workgroup) take every so-manieth one, and ask for the next before they work on
 // the one that they hold.  A thread keeps its columns' sums of dy h and dy over all of its rows, in registers or, where those do
-// not suffice (InLds), in LDS; at the end those of a workgroup are added in order.
+// not suffice (InLds), in LDS; at the end those of a workgroup are added in order.  (h, off and mean_gh are halves here: half_from.)
 // (InLds: W = 0, as many wavefronts as the row needs; one workgroup fills a compute unit, and what is asked for ahead would not fit
 // its registers.)
 template <typename TX, typename TY, int L, int W, int Eights, bool Bias, bool Stream>
 __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_kernel(NormArgs a, NormGrads g) {
     constexpr int E = kVector<TX, TY>, NV = Eights * 8 / E, kRows = L ? kThreads / (L ? L : 1) : 1;
-    constexpr bool InLds = L == 0 && W == 0;
+    constexpr bool InLds = L == 0 && W == 0, HalfEarly = InLds && sizeof(TX) != sizeof(TY);
     __shared__ float scratch[2][L ? 1 : 3 * (W ? W : 16)];
     extern __shared__ __align__(16) float joined[];  // [2][cols, padded] of each wavefront (L), or of the workgroup (InLds)
     const int TR = L ? L : W ? W * kWave : static_cast<int>(blockDim.x), t = L ? static_cast<int>(threadIdx.x) % L : static_cast<int>(threadIdx.x);
@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
             fetch<E, Stream>(y[k], py + c, some, past);
         }
         m = a.layer && live ? g.mean[at] : 0.0f;
+        if (HalfEarly) m = first_lane<kWave>(0.5f * m);  // (into a scalar register: 12288 columns from fp32 to bf16 297 us, so 287)
         r = live ? g.rstd[at] : 0.0f;
     };
     get(row, rx, ry, mu, rs);
@@ -68,7 +69,8 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
     for (; row - (L ? threadIdx.x % kWave / (L ? L : 1) : 0) < a.rows; row += stride) {
         if constexpr (!InLds) get(row + stride, next_x, next_y, next_mu, next_rs);
         const bool live = row < a.rows;
-        float s[3] = {0.0f, 0.0f, 0.0f};  // of g h, g, h
+        const float half_mu = HalfEarly ? mu : 0.5f * mu;
+        float s[3] = {0.0f, 0.0f, 0.0f};  // of g h / 2, g, h / 2
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TR + t) * E, some = live ? within_e<E>(c, a.cols) : 0;
@@ -79,7 +81,7 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
                 if (a.w) load_weights(w[k], a.w, a.w_dtype, c, some);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const float hi = i < some ? (h[i] - mu) * rs : 0.0f, gi = d[i] * w[k][i];
+                    const float hi = i < some ? half_from(h[i], half_mu) * rs : 0.0f, gi = d[i] * w[k][i];
                     s[0] += gi * hi;
                     s[1] += gi;
                     s[2] += hi;
@@ -88,7 +90,7 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
                 floats(rx[k], h);
                 floats(ry[k], d);
 #pragma unroll
-                for (int i = 0; i < E; ++i) h[i] = (h[i] - mu) * rs, d[i] *= w[k][i];
+                for (int i = 0; i < E; ++i) h[i] = half_from(h[i], half_mu) * rs, d[i] *= w[k][i];
                 if (__any(some < E))  // (few wavefronts)
 #pragma unroll
                     for (int i = 0; i < E; ++i) h[i] = i < some ? h[i] : 0.0f, d[i] = i < some ? d[i] : 0.0f;
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
             mean_gh = one[0] * inv_n;
         }
         turn ^= 1;
-        const float of_g = -rs * mean_g, of_h = -rs * mean_gh;
+        const float of_g = -rs * mean_g, of_h = -4.0f * (rs * mean_gh);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TR + t) * E, some = live ? within_e<E>(c, a.cols) : 0;
@@ -123,7 +125,7 @@ __global__ void __launch_bounds__(L ? kThreads : W ? W * kWave : 1024) norm_bwd_
                 for (int i = 0; i < E; ++i) h[i] = i < some ? h[i] : 0.0f, d[i] = i < some ? d[i] : 0.0f;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float hi = fmaf(h[i] - mu, rs, -off);
+                const float hi = fmaf(half_from(h[i], half_mu), rs, -off);
                 dx[i] = fmaf(hi, of_h, fmaf(d[i] * w[k][i], rs, of_g));
                 if constexpr (InLds) {
                     dyh[i] = d[i] * hi;
@@ -204,7 +206,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_sums_kernel(NormArgs a, NormGra
     __shared__ float scratch[3 * 1024 / kWave];
     const int64_t row = flat_block();
     if (row >= a.rows) return;
-    const float mu = a.layer ? g.mean[row] : 0.0f, rs = g.rstd[row];
+    const float half_mu = a.layer ? 0.5f * g.mean[row] : 0.0f, rs = g.rstd[row];
     float s[3] = {0.0f, 0.0f, 0.0f};
     for (int c = static_cast<int>(threadIdx.x) * 8; c < a.cols; c += 8 * 1024) {
         const int some = within(c, a.cols);
@@ -214,7 +216,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_sums_kernel(NormArgs a, NormGra
         if (a.w) load_typed(w, a.w, a.w_dtype, c, some);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float hi = i < some ? (h[i] - mu) * rs : 0.0f, gi = a.w ? d[i] * w[i] : d[i];
+            const float hi = i < some ? half_from(h[i], half_mu) * rs : 0.0f, gi = a.w ? d[i] * w[i] : d[i];
             s[0] += hi;
             s[1] += gi;
             s[2] += gi * hi;
@@ -242,15 +244,15 @@ __global__ void __launch_bounds__(256) norm_bwd_cols_kernel(NormArgs a, NormGrad
         dw[i] = db[i] = 0.0f;
     }
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        const float mu = a.layer ? g.mean[row] : 0.0f, rs = g.rstd[row];
+        const float half_mu = a.layer ? 0.5f * g.mean[row] : 0.0f, rs = g.rstd[row];
         const float off = sums[row * 3], mean_g = sums[row * 3 + 1], mean_gh = sums[row * 3 + 2];
         float h[8], d[8], dx[8];
         load_typed(h, a.x, x_dtype, row * a.x_stride + c, some);
         load_typed(d, g.dy, dy_dtype, row * g.dy_stride + c, some);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float hi = (h[i] - mu) * rs - off;
-            dx[i] = rs * (d[i] * w[i] - mean_g - hi * mean_gh);
+            const float hi = half_from(h[i], half_mu) * rs - off;
+            dx[i] = rs * (d[i] * w[i] - mean_g - 4.0f * hi * mean_gh);
             dw[i] += d[i] * hi;
             db[i] += d[i];
         }
@@ -285,6 +287,7 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const float *__restrict
     if (threadIdx.x >= 64 || c >= cols) return;
     float total = 0.0f;
     for (int i = 0; i < 1024 / kWave; ++i) total += sums[i][threadIdx.x];
+    if (!blockIdx.y) total *= 2.0f;  // (of halves of h)
     if (dtype == SPO_FP32) static_cast<float *>(to)[c] = add ? static_cast<float *>(to)[c] + total : total;
     else static_cast<bf16_t *>(to)[c] = f32_to_bf16(total);
 }

@@ -92,3 +92,34 @@ def test_in_place_beyond_fp32(spo, T, N, dtype):  # noqa: F811
     y, _, _ = spo.spo_norm_fwd(spo.make_norm_desc(x))
     z = x.clone()
     assert bool(torch.isfinite(y).all()) and torch.equal(spo.spo_norm_fwd(spo.make_norm_desc(z), out=z)[0], y)
+
+
+@TYPES
+@KINDS
+@pytest.mark.parametrize("N,many", WIDE)
+def test_gradients_of_differences_beyond_fp32(spo, N, many, dtype, layer):  # noqa: F811
+    say(f"norm gradients of rows wider than fp32, {many} x {N} {dtype} layer={layer}")
+    dy = rows(many, N, dtype, seed=1)
+    dy[0] *= 1e20    # (gradients are divided by the rows' deviations)
+    dy[2] *= 1e20
+    check(spo, wide_rows(N, many, dtype), vector(N, F32, 2, 1.0), vector(N, F32, 3), dy, layer, dtype)
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [(F32, BF16), (BF16, F32)])
+@pytest.mark.parametrize("N", [100, 1000, 5000, 9000, 17000])
+def test_gradients_of_differences_beyond_fp32_of_two_types(spo, N, x_dtype, y_dtype):  # noqa: F811
+    say(f"norm gradients of rows wider than fp32, {N} {x_dtype} {y_dtype}")
+    dy = rows(9, N, y_dtype, seed=1)
+    dy[0] *= 1e20
+    dy[2] *= 1e20
+    check(spo, wide_rows(N, 9, x_dtype), vector(N, F32, 2, 1.0), vector(N, F32, 3), dy, True, y_dtype)
+
+
+@KINDS
+@pytest.mark.parametrize("N", [100, 1000, 5000, 9000, 17000])
+def test_gradients_of_subnormal_rows(spo, N, layer):  # noqa: F811
+    # deviations of 2^-128: rstd is near fp32's end, and half of an element loses its last place, 2^-150 or 2^-22 = 2.4e-7 of a deviation
+    say(f"norm gradients of rows of 3e-39, {N} layer={layer}")
+    x = torch.randn((9, N), generator=torch.Generator().manual_seed(N)).cuda() * 4e-39
+    dy = rows(9, N, F32, seed=1, scale=1e-30)
+    check(spo, x, vector(N, F32, 2, 1.0), vector(N, F32, 3), dy, layer, F32, eps=0.0)
