@@ -506,7 +506,8 @@ int spo_norm_bwd(const spo_norm_desc *d, const float *mean, const float *rstd, c
  * range of 2^14 below its block's largest, the root 5 over 2^14 (2^28 of the second moment), with subnormals below; a root
  * that is not zero stays above it.  Codes are rounded by thresholds that move with the step, so that changes smaller than a
  * code add up over steps; a step's codes depend on its number and on an element's place modulo 64 alone.  Zeros in all arrays
- * are the state before the first step.  A value that is not finite makes the 64 of its block NaN, one of 3.29e38 or more too.
+ * are the state before the first step.  A value that is not finite makes the 64 of its block NaN, and so does a first moment beyond
+ * 3.19e38 or a root beyond 3.29e38.
  * Arrays that are written must not overlap each other or what is read.
  * ------------------------------------------------------------------------- */
 typedef struct {

@@ -192,7 +192,7 @@ __device__ __forceinline__ Coded encode8(const float (&x)[8], const uint32_t (&t
     Coded c;
     c.top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c.top = max(c.top, C::kSigned ? __float_as_uint(x[i]) & 0x7fffffffu : __float_as_uint(x[i]));
+    for (int i = 0; i < 8; ++i) c.top = max(c.top, C::magnitude(x[i]));
     c.top = max_of_eight_lanes(c.top);
     c.scale = C::scale(c.top);
 #pragma unroll

@@ -52,10 +52,13 @@ struct Code8 {
     static constexpr bool kSigned = Mantissa == 3;
     static constexpr int kDrop = 23 - Mantissa;
 
-    // top: the largest magnitude's bits (as whole numbers magnitudes compare alike, and NaN is the largest)
+    // A value's part in its block's largest: as whole numbers magnitudes compare alike, and NaN is the largest.  A root has no sign, but a
+    // NaN that takes its place may.
+    SPO_BOTH static uint32_t magnitude(float x) { return kSigned ? float_bits(x) & 0x7fffffffu : float_bits(x); }
+    // top: the block's largest
     SPO_BOTH static uint32_t scale(uint32_t top) {
-        const uint32_t e = (top + ((1u << kDrop) - 1)) >> 23;
-        return e < 15 ? 15 : e > kNotFinite ? kNotFinite : e;
+        const uint32_t infinite = 0x7f800000u, e = ((top < infinite ? top : infinite) + ((1u << kDrop) - 1)) >> 23;  // (of NaNs with a sign the sum would wrap)
+        return e < 15 ? 15 : e;
     }
     SPO_BOTH static uint32_t threshold(uint32_t turn) { return turn >> (32 - kDrop); }
     // A magnitude and its threshold, shifted so that the code they make is the uppermost byte.
