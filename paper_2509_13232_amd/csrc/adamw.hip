@@ -8,6 +8,7 @@
 // single roundings to fp32 (no contracted multiply-add): their codes in 8 bits have one answer on any machine.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "state8.hpp"
 #include "vec8.hpp"
@@ -558,7 +559,9 @@ extern "C" int spo_adamw_update(const spo_adamw_desc *d, double lr, const float 
     a.c1 = static_cast<float>(1.0 - beta1);
     a.b2 = static_cast<float>(beta2);
     a.c2 = static_cast<float>(1.0 - beta2);
+    // an eps above zero stays there, so that moments of zero are no 0 / 0: in 8 bits where the hardware's reciprocal takes it
     a.eps = static_cast<float>(eps);
+    if (eps > 0.0) a.eps = std::max(a.eps, d->state_bits == 8 ? std::numeric_limits<float>::min() : std::numeric_limits<float>::denorm_min());
     a.rounding = rounding;
     a.norm = grad_norm;
     a.max_norm = static_cast<float>(max_norm);

@@ -35,3 +35,20 @@ def test_gradients_of_any_nan_spoil_their_blocks(spo, dtype, u, zero_state):  # 
     c.dev_g[0].zero_()
     c.update(3)
     assert all(bool(torch.isnan(t.cpu()[spoilt]).all()) for t in spo.spo_adamw_state_values(c.states[0]))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-37, 1e-40, 1e-46, 1e-300])
+@pytest.mark.parametrize("on_device", [False, True])
+def test_any_eps_above_zero_keeps_what_has_no_moments(spo, bits, eps, on_device):  # noqa: F811
+    say(f"adamw, {bits} bits, eps {eps}")
+    n = 1000
+    p0 = torch.linspace(-1, 1, n).cuda()
+    p, g = p0.clone(), torch.zeros(n, device="cuda")
+    g[100:400] = 1e-3
+    d = spo.make_adamw_desc([p], [g], [spo.adamw_state(p, bits)])
+    spo.spo_adamw_update(d, 1e-2, torch.zeros(1, dtype=torch.int64, device="cuda") if on_device else 1, eps=eps)
+    still = g == 0
+    assert torch.equal(p[still], p0[still])
+    # the others take the first step's lr: 12 roundings of 2^-24 of it, and one of p's
+    assert float((p0[~still] - p[~still] - 1e-2).abs().max()) < 1e-2 * 1e-6 + 2.0 ** -24
