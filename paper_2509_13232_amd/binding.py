@@ -235,11 +235,18 @@ def _want(t, dtype, name, n=None):
         raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
 
 
+def _room(given, device):
+    """What kernels write to lies in one piece on the device of the call's tensors."""
+    if given is not None and not (given.is_cuda and given.is_contiguous() and given.device == device):
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    return given
+
+
 def _workspace(nbytes: int, device, given=None):
     if given is not None:
         if given.dtype != torch.uint8 or given.numel() < nbytes or given.data_ptr() % 256:
             raise ValueError("workspace must be a 256-byte aligned uint8 tensor of sufficient size")
-        return given
+        return _room(given, device)
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
@@ -315,6 +322,7 @@ def spo_advantages(alpha, beta, idx, reward, ddof=0, eps_norm=0.0, use_baseline=
     raw = torch.empty(B, dtype=torch.float32, device=reward.device)
     nrm = torch.empty(B, dtype=torch.float32, device=reward.device)
     st = torch.empty(2, dtype=torch.float32, device=reward.device)
+    _room(workspace, reward.device)
     _check(lib().spo_advantages(_ptr(alpha), _ptr(beta), N, _ptr(idx), _ptr(reward), B, int(ddof),
                                 float(eps_norm), int(bool(use_baseline)), _ptr(raw), _ptr(nrm), _ptr(st),
                                 _ptr(info), _ptr(workspace), workspace.numel() if workspace is not None else 0,
@@ -348,7 +356,7 @@ def _tracker_update(fn, name, a, b, idx, reward, kl, d_half, rho_min, rho_max, i
     _want(n_obs, torch.int32, "n_obs", N)
     _want(info, torch.int32, "info", 1)
     vprev = torch.empty(B, dtype=torch.float32, device=a.device) if want_v_prev else None
-    ws = workspace
+    ws = _room(workspace, a.device)
     if ws is None and (not ids_unique or check_repeats):   # the table of one int32 per prompt
         ws = _workspace(lib().spo_tracker_update_workspace_bytes(N), a.device)
     _check(fn(_ptr(a), _ptr(b), N, _ptr(idx), _ptr(reward), _ptr(kl), B, float(d_half), float(rho_min),

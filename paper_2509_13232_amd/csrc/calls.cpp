@@ -64,8 +64,13 @@ const at::Tensor *dense(PyObject *o, at::ScalarType type, int64_t n) {
     const at::Tensor *t = tensor(o);
     return t && t->scalar_type() == type && t->is_contiguous() && (n < 0 || t->numel() == n) ? t : nullptr;
 }
-const at::Tensor *workspace(PyObject *o, size_t bytes) {
+// ... whatever it holds, in one piece on the device of another
+const at::Tensor *beside(PyObject *o, const at::Tensor *like) {
     const at::Tensor *t = tensor(o);
+    return t && t->is_contiguous() && t->device() == like->device() ? t : nullptr;
+}
+const at::Tensor *workspace(PyObject *o, size_t bytes, const at::Tensor *like) {
+    const at::Tensor *t = beside(o, like);
     return t && t->scalar_type() == at::kByte && static_cast<size_t>(t->numel()) >= bytes &&
                    reinterpret_cast<uintptr_t>(t->data_ptr()) % 256 == 0 ? t : nullptr;
 }
@@ -125,7 +130,7 @@ PyObject *sample_prompts(PyObject *, PyObject *const *a, Py_ssize_t n) {
         !flag(a[6], replace) || !whole(a[7], 0, UINT32_MAX, most))
         return none();
     const int64_t N = alpha->numel();
-    const at::Tensor *ws = workspace(a[8], spo_sample_prompts_workspace_bytes(N, static_cast<int32_t>(B)));
+    const at::Tensor *ws = workspace(a[8], spo_sample_prompts_workspace_bytes(N, static_cast<int32_t>(B)), alpha);
     if (!ws) return none();
     const uint64_t seed = PyLong_AsUnsignedLongLongMask(a[4]), iteration = PyLong_AsUnsignedLongLongMask(a[5]);
     const at::Tensor idx = fresh({B}, at::kInt, *alpha), info = fresh({2}, at::kInt, *alpha);
@@ -146,7 +151,7 @@ PyObject *advantages(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!reward || !alpha) return none();
     const int64_t B = reward->numel(), N = alpha->numel();
     const at::Tensor *beta = dense(a[1], at::kFloat, N), *idx = dense(a[2], at::kInt, B);
-    const at::Tensor *ws = a[6] == Py_None ? nullptr : tensor(a[6]);
+    const at::Tensor *ws = a[6] == Py_None ? nullptr : beside(a[6], reward);
     int64_t ddof;
     double eps;
     if (!beta || !idx || B < 1 || B > INT32_MAX || (!ws && a[6] != Py_None) || !whole(a[4], INT32_MIN, INT32_MAX, ddof) || !number(a[5], eps))
@@ -187,7 +192,7 @@ PyObject *tracker_update(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!alpha || !idx) return none();
     const int64_t N = alpha->numel(), B = idx->numel();
     const at::Tensor *beta = dense(a[1], at::kFloat, N), *reward = dense(a[3], at::kFloat, B), *kl = dense(a[4], at::kFloat, B);
-    const at::Tensor *ws = a[9] == Py_None ? nullptr : tensor(a[9]);
+    const at::Tensor *ws = a[9] == Py_None ? nullptr : beside(a[9], alpha);
     double d_half, lo, hi;
     int unique;
     if (!beta || !reward || !kl || B < 1 || B > INT32_MAX || !number(a[5], d_half) || !number(a[6], lo) || !number(a[7], hi) ||
@@ -225,7 +230,7 @@ PyObject *pg_loss_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const spo_pg_desc *d;
     const at::Tensor *like;
     if (n != 3 || !plain_context() || !descriptor(a[0], a[1], d, like)) return none();
-    const at::Tensor *ws = workspace(a[2], spo_pg_loss_fwd_workspace_bytes(d));
+    const at::Tensor *ws = workspace(a[2], spo_pg_loss_fwd_workspace_bytes(d), like);
     if (!ws) return none();
     const at::Tensor loss = fresh({1}, at::kFloat, *like), logp = fresh({d->T}, at::kFloat, *like), lse = fresh({d->T}, at::kFloat, *like),
                      st = fresh({4}, at::kFloat, *like);
@@ -249,7 +254,7 @@ PyObject *pg_loss_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int accumulate;
     int64_t chunk;
     if (!logp || !lse || !number(a[4], grad) || !flag(a[6], accumulate) || !whole(a[7], INT64_MIN, INT64_MAX, chunk)) return none();
-    const at::Tensor *ws = workspace(a[8], spo_pg_loss_bwd_workspace_bytes(d, chunk));
+    const at::Tensor *ws = workspace(a[8], spo_pg_loss_bwd_workspace_bytes(d, chunk), like);
     if (!ws) return none();
     if (d->logits) {
         const at::Tensor dl = fresh({d->T, d->V}, type_of(d->dtype), *like);
@@ -285,7 +290,7 @@ PyObject *pg_loss_fwd_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int accumulate;
     int64_t chunk;
     if (!dw || !number(a[2], grad) || !flag(a[4], accumulate) || !whole(a[5], INT64_MIN, INT64_MAX, chunk)) return none();
-    const at::Tensor *ws = workspace(a[6], spo_pg_loss_fwd_bwd_workspace_bytes(d, chunk));
+    const at::Tensor *ws = workspace(a[6], spo_pg_loss_fwd_bwd_workspace_bytes(d, chunk), like);
     if (!ws) return none();
     const at::Tensor loss = fresh({1}, at::kFloat, *like), logp = fresh({d->T}, at::kFloat, *like), lse = fresh({d->T}, at::kFloat, *like),
                      st = fresh({4}, at::kFloat, *like), dx = fresh({d->T, d->H}, type_of(d->dtype), *like);
@@ -314,7 +319,7 @@ PyObject *logprob_fwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const spo_logprob_desc *d;
     const at::Tensor *like;
     if (n != 3 || !plain_context() || !scored(a[0], a[1], d, like) || d->top_k < 0) return none();
-    const at::Tensor *ws = workspace(a[2], spo_logprob_fwd_workspace_bytes(d));
+    const at::Tensor *ws = workspace(a[2], spo_logprob_fwd_workspace_bytes(d), like);
     if (!ws) return none();
     const at::Tensor lse = fresh({d->T}, at::kFloat, *like), entropy = fresh({d->T}, at::kFloat, *like);
     at::Tensor logp, ids, top;
@@ -400,7 +405,7 @@ PyObject *norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int64_t apart;
     const at::Tensor *dy = rows_of(a[4], d->rows, d->cols, apart);
     if (!rstd || !here(rstd) || !dy || (mean ? !here(mean) : layer || a[2] != Py_None)) return none();
-    const at::Tensor *ws = workspace(a[5], spo_norm_bwd_workspace_bytes(d));
+    const at::Tensor *ws = workspace(a[5], spo_norm_bwd_workspace_bytes(d), x);
     if (!ws) return none();
     const at::Tensor dx = fresh({d->rows, d->cols}, type_of(d->x_dtype), *x);
     at::Tensor dw, db;
@@ -504,7 +509,7 @@ PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const spo_adamw_desc *d;
     const at::Tensor *like;
     if (n != 3 || !plain_context() || !stepped(a[0], a[1], d, like)) return none();
-    const at::Tensor *ws = workspace(a[2], spo_grad_norm_workspace_bytes(d));
+    const at::Tensor *ws = workspace(a[2], spo_grad_norm_workspace_bytes(d), like);
     if (!ws) return none();
     const at::Tensor norm = fresh({1}, at::kFloat, *like);
     const spo_stream_t s = stream();

@@ -52,3 +52,29 @@ def test_any_eps_above_zero_keeps_what_has_no_moments(spo, bits, eps, on_device)
     assert torch.equal(p[still], p0[still])
     # the others take the first step's lr: 12 roundings of 2^-24 of it, and one of p's
     assert float((p0[~still] - p[~still] - 1e-2).abs().max()) < 1e-2 * 1e-6 + 2.0 ** -24
+
+
+def test_workspaces_in_host_memory_or_with_holes_are_refused(spo):  # noqa: F811
+    say("workspaces that are refused")
+    U8 = torch.uint8
+    x, w, p = torch.zeros((5, 100), device="cuda"), torch.zeros(100, device="cuda"), torch.zeros(5, device="cuda")
+    norm, step = spo.make_norm_desc(x, w), spo.make_adamw_desc([p], [torch.zeros_like(p)], [spo.adamw_state(p)])
+    a, idx, r = torch.ones(16, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda")
+    score = spo.make_logprob_desc(None, None, idx, logits=torch.zeros((4, 64), device="cuda"))
+    count = torch.zeros(1, dtype=torch.int64, device="cuda")
+    calls = [
+        lambda ws: spo.spo_norm_bwd(norm, p, p, x, workspace=ws),
+        lambda ws: spo.spo_grad_norm(step, workspace=ws),
+        lambda ws: spo.spo_adamw_update(step, 0.1, count, workspace=ws),
+        lambda ws: spo.spo_logprob_fwd(score, workspace=ws),
+        lambda ws: spo.spo_sample_prompts(a, a.clone(), 4, workspace=ws),
+        lambda ws: spo.spo_advantages(a, a.clone(), idx, r, workspace=ws),
+        lambda ws: spo.spo_tracker_update(a, a.clone(), idx, r, r, 0.25, 0.875, 0.96, ids_unique=False, workspace=ws),
+    ]
+    room = torch.zeros(1 << 21, dtype=U8, device="cuda")
+    for k, call in enumerate(calls):
+        for bad in (torch.zeros(1 << 20, dtype=U8), torch.zeros(1 << 20, dtype=U8, pin_memory=True), room[::2], room[:1].expand(1 << 20)):
+            with pytest.raises(ValueError, match="workspace"):
+                call(bad)
+        call(room)
+    torch.cuda.synchronize()

@@ -5,7 +5,10 @@ import subprocess
 import pytest
 import torch
 
+from paper_2509_13232_amd import binding as spo
 from paper_2509_13232_amd import build
+from test_binding_cpu import _desc
+from test_score_update_cpu import OnDevice, _dev, _refused, reached  # noqa: F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -41,3 +44,51 @@ def test_every_nan_and_infinity_spoils_its_block(tops, mantissa):
     largest = 0x7f800000 - (1 << (23 - mantissa))
     assert tops([ones[1:] + [largest]], mantissa) == [(254, 0)] and tops([ones[1:] + [largest + 1]], mantissa) == [(255, 1)]
     assert tops([ones, [0] * 64, [1] * 64], mantissa) == [(127, 0), (15, 0), (15, 0)]
+
+
+# -------------------------------------------------------- the binding's checks
+class Elsewhere(OnDevice):
+    device = torch.device("cuda", 1)
+
+
+def _state(n, bits=32):
+    if bits == 32:
+        return spo.AdamwState(_dev(n), _dev(n))
+    u8 = lambda k: _dev(k, dtype=torch.uint8)   # noqa: E731
+    return spo.AdamwState(u8(n), u8(n), u8(-(-n // 64)), u8(-(-n // 64)))
+
+
+def test_a_workspace_is_looked_at(reached):  # noqa: F811
+    # kernels write to it: in host memory, with holes, or on another device it is refused
+    U8 = torch.uint8
+    x, w, f, i, r = _dev(5, 100), _dev(100), _dev(16), _dev(4, dtype=torch.int32), _dev(4)
+    norm, step = spo.make_norm_desc(x, w), spo.make_adamw_desc([_dev(5)], [_dev(5)], [_state(5)])
+    loss, logp, lse = _desc(spo.SPO_W_VH)
+    calls = [
+        lambda ws: spo.spo_norm_bwd(norm, _dev(5), _dev(5), _dev(5, 100), workspace=ws),
+        lambda ws: spo.spo_norm_bwd(norm, _dev(5), _dev(5), _dev(5, 100), want_dx=False, workspace=ws),
+        lambda ws: spo.spo_grad_norm(step, workspace=ws),
+        lambda ws: spo.spo_pg_loss_fwd(loss, workspace=ws),
+        lambda ws: spo.spo_pg_loss_bwd(loss, logp, lse, d_W=_dev(100, 64), workspace=ws),
+        lambda ws: spo.spo_pg_loss_fwd_bwd(loss, d_W=_dev(100, 64), workspace=ws),
+        lambda ws: spo.spo_sample_prompts(f, f, 4, workspace=ws),
+        lambda ws: spo.spo_advantages(f, f, i, r, workspace=ws),
+        lambda ws: spo.spo_tracker_update(f, f, i, r, r, 0.25, 0.875, 0.96, ids_unique=False, workspace=ws),
+    ]
+
+    def at256(t, of=OnDevice):
+        if of is not None:
+            t = of(t)
+            t.data_ptr = lambda: 256
+        return t
+
+    host = torch.zeros(1 << 20, dtype=U8)
+    host = host[-host.data_ptr() % 256:]
+    for k, call in enumerate(calls):
+        for bad in (host, at256(torch.zeros(1 << 21, dtype=U8)[::2]), at256(torch.zeros(1, dtype=U8).expand(1 << 20)), at256(torch.zeros(1 << 20, dtype=U8), Elsewhere)):
+            with pytest.raises(ValueError, match="workspace"):
+                call(bad)
+        assert not reached, k
+        call(at256(torch.zeros(1 << 20, dtype=U8)))
+        assert len(reached) == 1, k
+        reached.clear()
