@@ -731,10 +731,14 @@ def _here(t, name):
         raise ValueError(f"{name}: is on {t.device}, and the current device is {torch.cuda.current_device()}")
 
 
+def _want_here(t, dtype, name, n=None):
+    _want(t, dtype, name, n)
+    _here(t, name)
+
+
 def _want_float(t, name, n=None):
     if t is not None:
-        _want(t, t.dtype if t.dtype in _FLOATS else torch.float32, name, n)
-        _here(t, name)
+        _want_here(t, t.dtype if t.dtype in _FLOATS else torch.float32, name, n)
 
 
 def _row_stride(t, name, shape=None):
@@ -834,9 +838,8 @@ def spo_norm_bwd(desc, mean, rstd, dy, dx=None, dx_dtype=None, d_weight=None, d_
     apart = _row_stride(dy, "dy", (d.rows, d.cols))
     if d.kind == SPO_NORM_LAYER and mean is None:
         raise TypeError("mean: expected the forward's")
-    _want(rstd, torch.float32, "rstd", d.rows)
-    _want(mean, torch.float32, "mean", d.rows)
-    _here(rstd, "rstd"), _here(mean, "mean")
+    _want_here(rstd, torch.float32, "rstd", d.rows)
+    _want_here(mean, torch.float32, "mean", d.rows)
     if not want_dx:
         dx = None
     elif dx is None:
@@ -930,13 +933,13 @@ def make_adamw_desc(params, grads, states, weight_decay=0.0, copies=None):
             t = getattr(s, name)
             if t is None:
                 raise TypeError(f"states[{i}].{name}: expected a tensor")
-            _want(t, kind, f"states[{i}].{name}", size)
+            _want_here(t, kind, f"states[{i}].{name}", size)
         for name in ("m_scale", "v_scale"):
             if (getattr(s, name) is not None) != eight:
                 raise TypeError(f"states[{i}].{name}: expected {'a tensor' if eight else 'None'}")
-            _want(getattr(s, name), torch.uint8, f"states[{i}].{name}", -(-size // SPO_STATE_BLOCK))
+            _want_here(getattr(s, name), torch.uint8, f"states[{i}].{name}", -(-size // SPO_STATE_BLOCK))
         if copy is not None:
-            _want(copy, torch.bfloat16, f"copies[{i}]", size)
+            _want_here(copy, torch.bfloat16, f"copies[{i}]", size)
             if p.dtype != torch.float32:
                 raise TypeError(f"copies[{i}]: the tensor itself is not of torch.float32")
         t = table[i]
@@ -988,10 +991,9 @@ def spo_adamw_update(desc, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_norm
     if desc[0].count and _plain_calls().adamw_update(C.addressof(desc[0]), desc[1][2][0], lr, step, beta1, beta2, eps, grad_norm, max_norm, rounding):
         return
     lr_t, step_t = (x if isinstance(x, torch.Tensor) else None for x in (lr, step))
-    _want(lr_t, torch.float32, "lr", 1)
-    _want(step_t, torch.int64, "step", 1)
-    _want(grad_norm, torch.float32, "grad_norm", 1)
-    _here(lr_t, "lr"), _here(step_t, "step"), _here(grad_norm, "grad_norm")
+    _want_here(lr_t, torch.float32, "lr", 1)
+    _want_here(step_t, torch.int64, "step", 1)
+    _want_here(grad_norm, torch.float32, "grad_norm", 1)
     number = 0 if step_t is not None else operator.index(step)
     if not -1 << 63 <= number < 1 << 63:
         raise ValueError(f"step: {number} is beyond 64 bits")
@@ -1013,8 +1015,7 @@ def spo_adamw_state_values(state, dtype=torch.bfloat16):
                           (state.v_scale, "v_scale", -(-n // SPO_STATE_BLOCK))):
         if t is None:
             raise TypeError(f"{name}: expected a state in 8 bits")
-        _want(t, torch.uint8, name, size)
-    _here(state.m, "state")
+        _want_here(t, torch.uint8, name, size)
     m, root = (torch.empty(n, dtype=dtype, device=state.m.device) for _ in range(2))
     _check(lib().spo_adamw_state_values(_ptr(state.m), _ptr(state.v), _ptr(state.m_scale), _ptr(state.v_scale), n, _ptr(m), _ptr(root), _dt(dtype),
                                         _stream()), "spo_adamw_state_values")

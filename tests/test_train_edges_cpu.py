@@ -92,3 +92,20 @@ def test_a_workspace_is_looked_at(reached):  # noqa: F811
         call(at256(torch.zeros(1 << 20, dtype=U8)))
         assert len(reached) == 1, k
         reached.clear()
+
+
+def test_states_and_copies_of_another_device_are_refused(reached, monkeypatch):  # noqa: F811
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    U8 = torch.uint8
+    make = lambda s, **kw: spo.make_adamw_desc([_dev(100)], [_dev(100)], [s], **kw)   # noqa: E731
+    for bits in (32, 8):
+        whole = _state(100, bits)
+        make(whole)
+        for name, t in zip(whole._fields, whole):
+            if t is not None:
+                _refused(ValueError, rf"states\[0\].{name}: is on cuda:1", make, whole._replace(**{name: Elsewhere(torch.zeros(t.shape, dtype=t.dtype))}))
+    _refused(ValueError, r"copies\[0\]: is on cuda:1", make, _state(100), copies=[Elsewhere(torch.zeros(100, dtype=torch.bfloat16))])
+    for name in spo.AdamwState._fields:
+        whole = _state(100, 8)
+        _refused(ValueError, f"{name}: is on cuda:1", spo.spo_adamw_state_values, whole._replace(**{name: Elsewhere(torch.zeros(getattr(whole, name).shape, dtype=U8))}))
+    assert not reached
