@@ -539,6 +539,7 @@ int spo_grad_norm(const spo_adamw_desc *d, float *norm, void *ws, size_t ws_byte
  *               256-byte aligned, is needed (otherwise it may be NULL).
  * grad_norm     device fp32[1] as spo_grad_norm leaves it, or NULL.  If it is not finite nothing is written, and
  *               step_device is not counted up.
+ * max_norm      of grad_norm, >= 0: gradients are scaled down to it; INFINITY: they are not.
  * eps           in fp32; one above zero counts as 2^-126 at least in 8 bits, as 2^-149 in 32.
  * rounding      of params in bf16: SPO_ROUND_NEAREST, or SPO_ROUND_THRESHOLD, by thresholds that move with the step, as the
  *               states are: without a copy in fp32, changes below half a place add up over steps instead of being lost.

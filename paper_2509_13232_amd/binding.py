@@ -7,6 +7,7 @@ fallback: a missing library or a non-zero status raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import operator
 import os
 from collections import namedtuple
@@ -984,10 +985,13 @@ def spo_adamw_update_workspace_bytes() -> int:
     return int(lib().spo_adamw_update_workspace_bytes())
 
 
-def spo_adamw_update(desc, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_norm=None, max_norm=0.0, rounding=SPO_ROUND_NEAREST, workspace=None):
+def spo_adamw_update(desc, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_norm=None, max_norm=None, rounding=SPO_ROUND_NEAREST, workspace=None):
     """One step, IN PLACE on the descriptor's params, states and copies.  step: the number of this step, 1 for the first, or a CUDA
     int64[1] that holds the steps taken and is counted up; lr: a number or a CUDA fp32[1].  grad_norm: fp32[1] as spo_grad_norm
-    leaves it, gradients are then scaled down to max_norm; None: they are taken as they are."""
+    leaves it: a step whose norm is not finite is left out, and gradients are scaled down to max_norm (None: they are not); without it
+    they are taken as they are."""
+    if max_norm is None:
+        max_norm = math.inf
     if desc[0].count and _plain_calls().adamw_update(C.addressof(desc[0]), desc[1][2][0], lr, step, beta1, beta2, eps, grad_norm, max_norm, rounding):
         return
     lr_t, step_t = (x if isinstance(x, torch.Tensor) else None for x in (lr, step))

@@ -78,3 +78,17 @@ def test_workspaces_in_host_memory_or_with_holes_are_refused(spo):  # noqa: F811
                 call(bad)
         call(room)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("on_device", [False, True])
+def test_a_norm_without_a_limit_clips_nothing(spo, bits, on_device):  # noqa: F811
+    say(f"adamw with a norm and no limit, {bits} bits")
+    c, bad = Case(spo, [5000, 64], bits), float("inf")
+    number = torch.full((1,), 1, dtype=torch.int64, device="cuda") if on_device else 2
+    c.update(number, grad_norm=spo.spo_grad_norm(c.desc))
+    c.check(2, factor=torch.tensor(1.0))
+    c.dev_g[0][17] = bad
+    before = [t.clone() for t in (*c.dev_p, *(x for s in c.states for x in s if x is not None))]
+    c.update(number if on_device else 3, grad_norm=spo.spo_grad_norm(c.desc))
+    assert all(torch.equal(a, b) for a, b in zip((*c.dev_p, *(x for s in c.states for x in s if x is not None)), before))

@@ -109,3 +109,22 @@ def test_states_and_copies_of_another_device_are_refused(reached, monkeypatch): 
         whole = _state(100, 8)
         _refused(ValueError, f"{name}: is on cuda:1", spo.spo_adamw_state_values, whole._replace(**{name: Elsewhere(torch.zeros(getattr(whole, name).shape, dtype=U8))}))
     assert not reached
+
+
+def test_a_norm_without_a_limit_clips_nothing(reached, monkeypatch):  # noqa: F811
+    # a norm alone is for leaving out steps that are not finite; a limit of zero has to be asked for
+    step, given = spo.make_adamw_desc([_dev(5)], [_dev(5)], [_state(5)]), []
+
+    class Steps:
+        def spo_adamw_update(self, *a):
+            given.append(a[9])
+            return 0
+
+    monkeypatch.setattr(spo, "lib", Steps)
+    plain = []
+    for calls in (lambda *a: None, lambda *a: plain.append(a[8]) or True):
+        monkeypatch.setattr(spo, "_calls", type("Calls", (), {"adamw_update": staticmethod(calls)}))
+        for kw in ({}, {"max_norm": None}, {"max_norm": 0.0}, {"max_norm": 2.5}):
+            spo.spo_adamw_update(step, 0.1, 1, grad_norm=_dev(1), **kw)
+    infinite = float("inf")
+    assert given == plain == [infinite, infinite, 0.0, 2.5]
