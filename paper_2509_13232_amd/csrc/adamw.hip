@@ -16,7 +16,7 @@
 namespace spo {
 
 constexpr int kThreads = 256;
-constexpr int64_t kMostElements = int64_t(1) << 35;
+constexpr int64_t kMostElements = int64_t(1) << 35, kMostTensors = int64_t(1) << 24;
 constexpr size_t kTableBytes = 3840;  // of a launch's 4 KiB of arguments
 
 struct Tensor32 {
@@ -491,7 +491,7 @@ static int validate(const spo_adamw_desc *d, bool state) {
     if (d->struct_size != sizeof(spo_adamw_desc)) return SPO_EINVAL;
     if (d->state_bits != 32 && d->state_bits != 8) return SPO_EINVAL;
     if (d->count < 0) return SPO_EINVAL;
-    if (d->count > int64_t(1) << 24) return SPO_ERANGE;
+    if (d->count > kMostTensors) return SPO_ERANGE;
     if (d->count && !d->tensors) return SPO_ENULL;
     for (int64_t i = 0; i < d->count; ++i) {
         const spo_adamw_tensor &t = d->tensors[i];
@@ -511,7 +511,7 @@ static int validate(const spo_adamw_desc *d, bool state) {
 }
 
 extern "C" size_t spo_grad_norm_workspace_bytes(const spo_adamw_desc *d) {
-    return d && d->struct_size == sizeof(spo_adamw_desc) && d->count >= 0 ? sizeof(double) * kNormParts * norm_launches(d) : 0;
+    return d && d->struct_size == sizeof(spo_adamw_desc) && d->count >= 0 && d->count <= kMostTensors ? sizeof(double) * kNormParts * norm_launches(d) : 0;
 }
 
 extern "C" int spo_grad_norm(const spo_adamw_desc *d, float *norm, void *ws, size_t ws_bytes, spo_stream_t stream) {

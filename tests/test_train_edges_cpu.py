@@ -1,4 +1,5 @@
 """Normalisations and AdamW steps on the host, at their edges (no GPU needed)."""
+import ctypes as C
 import os
 import subprocess
 
@@ -128,3 +129,20 @@ def test_a_norm_without_a_limit_clips_nothing(reached, monkeypatch):  # noqa: F8
             spo.spo_adamw_update(step, 0.1, 1, grad_norm=_dev(1), **kw)
     infinite = float("inf")
     assert given == plain == [infinite, infinite, 0.0, 2.5]
+
+
+def test_workspace_queries_of_what_is_refused_say_nothing():
+    if not os.path.exists(spo.LIB_PATH):
+        build.build()
+    L = C.CDLL(spo.LIB_PATH)
+    L.spo_grad_norm_workspace_bytes.restype = C.c_size_t
+    d = spo.AdamwDesc()
+    d.struct_size, d.state_bits = C.sizeof(spo.AdamwDesc), 32
+    sizes = []
+    for count in (0, 1, 160, 161, 1 << 24):
+        d.count = count
+        sizes.append(L.spo_grad_norm_workspace_bytes(C.byref(d)))
+    assert sizes == sorted(sizes) and sizes[0] > 0
+    for count in ((1 << 24) + 1, 1 << 45, 1 << 62, (1 << 63) - 1, -1):
+        d.count = count
+        assert L.spo_grad_norm_workspace_bytes(C.byref(d)) == 0, count
