@@ -69,7 +69,6 @@ struct AdamwStep {
     double lr;
     float rate, root_scale;  // lr / (1 - b1^t), (1 - b2^t)^-1/2
     uint32_t step;
-    int32_t skip;
 };
 struct AdamwScalars {
     float b1, c1, b2, c2, eps;  // c = 1 - b
@@ -86,19 +85,16 @@ static __host__ __device__ AdamwStep step_of(double lr, double beta1, double bet
     s.rate = static_cast<float>(lr / -expm1(static_cast<double>(t) * log(beta1)));
     s.root_scale = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(t) * log(beta2))));
     s.step = static_cast<uint32_t>(t);
-    s.skip = 0;
     return s;
 }
 
 __global__ void adamw_prepare_kernel(double lr, const float *lr_device, double beta1, double beta2, int64_t t, int64_t *t_device, const float *norm,
                                      AdamwStep *out) {
-    const bool skip = norm && !isfinite(*norm);
     if (t_device) {
         t = *t_device + 1;
-        if (!skip) *t_device = t;
+        if (!norm || isfinite(*norm)) *t_device = t;  // (as the step's kernel decides whether anything moves)
     }
     *out = step_of(lr_device ? static_cast<double>(*lr_device) : lr, beta1, beta2, t);
-    out->skip = skip;
 }
 
 __device__ __forceinline__ float first_moment(float m, float g, const AdamwScalars &a) {
