@@ -1,6 +1,7 @@
 """Normalisations and AdamW steps on the host, at their edges (no GPU needed)."""
 import ctypes as C
 import os
+import re
 import subprocess
 
 import pytest
@@ -146,3 +147,29 @@ def test_workspace_queries_of_what_is_refused_say_nothing():
     for count in ((1 << 24) + 1, 1 << 45, 1 << 62, (1 << 63) - 1, -1):
         d.count = count
         assert L.spo_grad_norm_workspace_bytes(C.byref(d)) == 0, count
+
+
+# ------------------------------------------------------------------- registers
+# What is kept outside of registers, in bytes per lane at most: rows beyond 32768 elements in the forward, and the sums of two types in LDS
+OUTSIDE = {"norm_fwd.hip": [(r"norm_fwd_kernelI..Li0ELi16ELi8E", 256)], "norm_bwd.hip": [(r"norm_bwd_kernelI(ft|tf)Li0ELi0ELi2ELb1E", 32)]}
+
+
+@pytest.mark.timeout(900)
+@pytest.mark.parametrize("src", list(OUTSIDE))
+def test_little_is_kept_outside_of_registers(tmp_path, src):
+    r = subprocess.run([build._hipcc(), *build.FLAGS, "--cuda-device-only", "-Rpass-analysis=kernel-resource-usage", "-c",
+                        os.path.join(build.CSRC, src), "-o", str(tmp_path / "k.o")], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    scratch, scalars, name = {}, {}, None
+    for line in r.stderr.splitlines():
+        if m := re.search(r"remark: .*Function Name: (\S+)", line):
+            name = m[1]
+        elif m := re.search(r"remark: .*ScratchSize \[bytes/lane\]: (\d+)", line):
+            scratch[name] = int(m[1])
+        elif m := re.search(r"remark: .*TotalSGPRs: (\d+)", line):
+            scalars[name] = int(m[1])
+    assert len(scratch) > 100
+    too_much = {k: v for k, v in scratch.items() if v > max([most for kernel, most in OUTSIDE[src] if re.search(kernel, k)], default=0)}
+    assert not too_much
+    if src == "norm_fwd.hip":     # (the kernels' own bound)
+        assert max(scalars.values()) <= 80
