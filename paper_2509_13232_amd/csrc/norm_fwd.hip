@@ -137,7 +137,7 @@ __global__ void __attribute__((amdgpu_num_sgpr(80))) __launch_bounds__(L ? kThre
             for (int c = t; c < a.cols; c += TR) {
                 const float f = Vec<TX>::get(x + c);
                 const float h = odd[r] ? static_cast<float>((static_cast<double>(f) - mu) * gain) : fmaf(f - base[r], rs[r], -off[r] * rs[r]);
-                Vec<TY>::put(y + row_of(r) * y_stride + c, fmaf(h, a.w ? load_weight(a.w, a.w_dtype, c) : 1.0f, a.b ? load_weight(a.b, a.w_dtype, c) : 0.0f));
+                store_one(y + row_of(r) * y_stride + c, fmaf(h, a.w ? load_weight(a.w, a.w_dtype, c) : 1.0f, a.b ? load_weight(a.b, a.w_dtype, c) : 0.0f));
             }
         }
         return;

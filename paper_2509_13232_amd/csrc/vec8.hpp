@@ -218,6 +218,9 @@ __device__ __forceinline__ void store_e(bf16_t *p, const float (&x)[E], int n) {
     }
     if (n & 1) *p = static_cast<bf16_t>(a);
 }
+// One element, rounded as those of store_e are
+__device__ __forceinline__ void store_one(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store_one(bf16_t *p, float x) { *p = static_cast<bf16_t>(pack_bf16x2_rn(x, x)); }
 template <int E>
 __device__ __forceinline__ int within_e(int at, int n) { return at >= n ? 0 : n - at < E ? n - at : E; }
 // Weights of a type that the kernel is told at run time; zeros behind the n-th.

@@ -123,3 +123,21 @@ def test_gradients_of_subnormal_rows(spo, N, layer):  # noqa: F811
     x = torch.randn((9, N), generator=torch.Generator().manual_seed(N)).cuda() * 4e-39
     dy = rows(9, N, F32, seed=1, scale=1e-30)
     check(spo, x, vector(N, F32, 2, 1.0), vector(N, F32, 3), dy, layer, F32, eps=0.0)
+
+
+@KINDS
+@pytest.mark.parametrize("T,N", [(131073, 20), (40, 64), (8199, 1000), (50, 1400), (2053, 4000), (12, 12288), (9, 40000)])
+def test_a_row_is_its_own_beside_any_other(spo, T, N, layer):  # noqa: F811
+    # ordinary rows, also with outputs at bf16's lower end, beside rows that are summed in 64 bits
+    say(f"norm of rows beside those in 64 bits, {T} x {N} layer={layer}")
+    x = rows(T, N, BF16)
+    x[3::7] *= 1e25
+    w, b = vector(N, F32, 2, 1.0), vector(N, F32, 3)
+    w[::3] *= 1e-38
+    b[::3] = 0
+    kind = spo.SPO_NORM_LAYER if layer else spo.SPO_NORM_RMS
+    want = spo.spo_norm_fwd(spo.make_norm_desc(x, w, b, kind=kind))
+    order = torch.cat([torch.arange(i, T, 7) for i in range(7)]).cuda()      # those of a kind together
+    got = spo.spo_norm_fwd(spo.make_norm_desc(x[order], w, b, kind=kind))
+    for p, q in zip(got, want):
+        assert p is None and q is None or torch.equal(p, q[order])
