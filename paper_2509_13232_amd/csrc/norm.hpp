@@ -4,8 +4,9 @@
 //   y = h w + b;  with g = dy w:  dx = rstd (g - mean g - h mean(g h)), rms without the mean of g;  dw = sum dy h,  db = sum dy
 //
 // Bound by HBM.  A row is held in registers from its one read to its one write: by 4 to 64 lanes of a wavefront (rows of up to
-// 1536 elements in the forward, 1024 in the backward), or by 4 to 16 wavefronts of a workgroup.  Rows that are longer than the
-// registers of a backward's workgroup are read twice there.  (284780 rows of 4096 in bf16: forward 751-785 us, 6.1 TB/s, backward
+// 1536 elements in the forward, 1024 in the backward), or by 4 to 16 wavefronts of a workgroup.  Registers end at 32768 elements in the
+// forward (beyond, some of a row waits in scratch memory: 4096 rows of 65536 in bf16 4.7 TB/s, 2048 in fp32 2.7) and at 16384 in the
+// backward, which reads longer rows twice (2.9 to 3.2).  (284780 rows of 4096 in bf16: forward 751-785 us, 6.1 TB/s, backward
 // 1180-1290 from card to card, 5.4 to 5.9; 17043 rows of 4096 from fp32 to bf16: forward 74, 5.7; 8192 of 1024, which the caches hold:
 // 9.6 and 14.4.  One row: 2.6 us, a launch and its chain of loads and sums.)
 //
@@ -124,9 +125,10 @@ constexpr int kVector = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
 template <typename TX, typename TY>
 static bool past_cache(int64_t rows, int64_t cols) { return rows * cols * static_cast<int64_t>(sizeof(TX) + sizeof(TY)) > kStreamBytes; }
 
-// Lanes that hold a row of so many eights, one each (or two or three, with all lanes of a wavefront); and wavefronts where a workgroup
-// holds it.  These come in fours: a workgroup's wavefronts are dealt to the four SIMDs of a compute unit from the first one on, so
-// that five of them leave room for fewer workgroups (52428 rows of 5120 in bf16 by five wavefronts: 298 us, by eight 233).
+// Lanes that hold a row of so many eights, one each (or two or three, with all lanes of a wavefront).  Rows of fewer than 24 elements leave
+// lanes idle (16777216 rows of 16 in bf16: 3.7 TB/s, of 9: 1.8).  And wavefronts of a workgroup that holds a row and its sums in LDS, in
+// fours, as they are dealt to the SIMDs of a compute unit (backward in bf16 with a bias, in fours and as many as the row needs: 19173 rows of
+// 14000 403 and 427 us, 20971 of 12800 402 and 405, 29826 of 9000 480 and 461).
 static int lanes_of(int64_t eights) { return eights <= 4 ? 4 : eights <= 8 ? 8 : eights <= 16 ? 16 : eights <= 32 ? 32 : kWave; }
 static int fours_of(int64_t eights, int each) { return static_cast<int>(ceil_div(eights, each * 4 * kWave)) * 4; }
 

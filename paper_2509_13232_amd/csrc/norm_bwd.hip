@@ -294,9 +294,9 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const float *__restrict
 
 // ------------------------------------------------------------------------------------------------------------ host
 
-// How many workgroups the backward has: as many as the chip holds at once, in whole numbers per compute unit (284780 rows of 4096
-// in bf16, on one card: two of 8 wavefronts per unit 1280 us, one 1266 to 1340, three 1366; two of 4 wavefronts with two eights per
-// thread 1328).  Few rows: one to each group of lanes (713 rows of 1001: 5.9 us, two 7.4).
+// How many workgroups the backward has: as many as the chip holds at once, in whole numbers per compute unit (on one card, one, two and
+// three of 8 wavefronts per unit: 65536 rows of 4096 in bf16 283, 271 and 311 us; 284780, rms, 1216 to 1258, 1251 to 1277 and
+// 1327 to 1332).  Few rows: one to each group of lanes (713 rows of 1001: 5.9 us, two 7.4).
 static int bwd_parts(int64_t rows, int64_t cols) {
     const int64_t eights = ceil_div(cols, 8);
     int64_t most, each = 1;

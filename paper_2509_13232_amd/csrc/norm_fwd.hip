@@ -4,8 +4,10 @@
 namespace spo {
 
 // Those that share a row (L lanes, or with L = 0 the workgroup) hold R rows: two side by side where their registers suffice and rows
-// are many; weight and bias are read once for both, and their sums cross the lanes together (284780 rows of 4096 in bf16: 822 -> 770 us,
-// 131072 of 2048: 222 -> 185, 4194304 of 64: 222 -> 178; but 713 rows of 1001, which are there at once: 4.2 -> 5.2).
+// are many; weight and bias are read once for both, and their sums cross the lanes together.  One row and two, layer and rms: in bf16
+// 131072 rows of 2048 227 -> 181 and 196 -> 169 us, 1342177 of 200 279 -> 211 and 234 -> 184, 65536 of 4096 192 -> 185 and 171 -> 177, 268435
+// of 1000 201 and 190 -> 197; in fp32, whose wavefronts hold half as much, 32768 of 4096 186 -> 179 and 177, 65536 of 2048 184 -> 181 and
+// 169 -> 178, 671088 of 200 215 -> 222 and 207 -> 226.  713 rows of 1001, which are there at once: 4.2 -> 5.2.
 // Eights: eight elements per thread times this.  The k-th vector of the t-th of TR threads begins at column (k * TR + t) * E.
 // Instructions count beside the bytes: with divisions, masks for all and an epilogue of four instructions per element, 262144 rows of
 // 1024 took 188 us instead of 176, 131072 of 2048 210 instead of 185.  Registers, too, which the path of rows in 64 bits takes more of
